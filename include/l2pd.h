@@ -406,6 +406,85 @@ l2pd_status l2pd_attention_bf16(void *stream, const void *q, const void *k, cons
                                 int32_t impl, int32_t check);
 
 /*
+ * Operators around a key/value cache held in 4 bits.  (The paper's cached decoding keeps keys and values in full; these are for
+ * users whose caches bound them: the same prefix and dual caches in 136 bytes a key and head instead of 512.)
+ *
+ * A row x of a key or value (one head's head_dim numbers) is kept as head_dim codes of 4 bits and two bf16 numbers:
+ *     m = min x,  s = bf16(fl32(fl32(max x - m) / 15)),  c = min(15, round half to even of (x - m) / s), 0 where s = 0
+ *     value = c s + m
+ * the quotient decided exactly.  A row with an infinity or NaN, or whose range passes fp32, reads back as NaN throughout.
+ *
+ * l2pd_kv4 (host memory, read during the call) describes a cache: slots sequences of up to `capacity` keys, `heads` key heads of
+ * head_dim 64 or 128.  data: DEVICE, 16-byte aligned, l2pd_kv4_bytes(...) bytes (0: sizes that are not supported), the caller's;
+ * its layout belongs to the library.  Zeroed memory is a cache of zeros; every call reads only keys below a sequence's length.
+ *
+ * A call's batch: B sequences (0 to 65535) whose rows lie packed in the row arrays; d_row_start: DEVICE int32 [B + 1], ascending,
+ * sequence i has rows d_row_start[i] .. d_row_start[i + 1] - 1, at most `rows` of them (NULL: i * rows .. ).  d_slots: DEVICE int32
+ * [B], the slot of each sequence (NULL: i).  Rows that belong to no sequence are neither read nor written.  A slot outside the
+ * cache holds nothing: it is not written and reads as a sequence without keys.  Row strides are in elements; [row][head][head_dim]
+ * within a row is contiguous; rows start on 16 bytes (strides multiples of 8), else L2PD_ERR_SHAPE.  Every call follows stream order,
+ * allocates nothing, runs on the current device and may be captured into a graph (attention: after one call outside a capture).
+ * B = 0 or rows = 0 is L2PD_OK and does nothing.  All arithmetic is fp32 or wider and the order of every sum is fixed: a call
+ * repeated on the same device gives the same bits.
+ */
+typedef struct {
+  void *data;
+  int32_t slots, heads, head_dim, capacity;
+} l2pd_kv4;
+int64_t l2pd_kv4_bytes(int32_t slots, int32_t heads, int32_t head_dim, int32_t capacity);
+/* Row r of sequence i becomes key d_key_start[i] + r of its slot (DEVICE int32 [B]; NULL: 0).  k, v: DEVICE bf16.  Keys outside
+ * [0, capacity) are not written.  No two rows of a call may name the same key. */
+l2pd_status l2pd_kv4_store(void *stream, const l2pd_kv4 *cache, const void *k, const void *v, int32_t B, int32_t rows,
+                           const int32_t *d_row_start, const int32_t *d_slots, const int32_t *d_key_start, int64_t k_stride,
+                           int64_t v_stride);
+/* The same rows read back, as L2PD_F32 (the values themselves) or L2PD_BF16; 0 for keys and slots that do not exist. */
+l2pd_status l2pd_kv4_load(void *stream, const l2pd_kv4 *cache, int32_t dtype, void *k, void *v, int32_t B, int32_t rows,
+                          const int32_t *d_row_start, const int32_t *d_slots, const int32_t *d_key_start, int64_t k_stride,
+                          int64_t v_stride);
+/* out[r, h] = softmax over the keys j < d_lens[i] of (scale q[r, h] . k_j) times v_j, without a causal mask: the rows of a block
+ * see the whole cache, their own keys among it where they were stored before.  q, out: DEVICE bf16 [row, Hq, head_dim]; query head
+ * h reads key head h / (Hq / heads).  d_lens: DEVICE int32 [B], clipped to [0, min(max_len, capacity)]; max_len (host) sizes the launch.
+ * d_lse: DEVICE float [row, Hq] or NULL, the natural logarithm of the sum of exponentials.  No keys: out 0, d_lse -inf.
+ * scratch: DEVICE, 16-byte aligned, of at least l2pd_attention_kv4_scratch_bytes(...) bytes (asked on the same device), for this
+ * call alone until it has run: calls that may overlap, and captured graphs that may, need their own.  check as elsewhere. */
+int64_t l2pd_attention_kv4_scratch_bytes(const l2pd_kv4 *cache, int32_t B, int32_t rows, int32_t Hq, int32_t max_len);
+l2pd_status l2pd_attention_kv4(void *stream, const l2pd_kv4 *cache, const void *q, void *out, float *d_lse, int32_t B, int32_t rows,
+                               const int32_t *d_row_start, const int32_t *d_slots, const int32_t *d_lens, int32_t max_len, int32_t Hq,
+                               int64_t q_stride, int64_t out_stride, float scale, void *scratch, int64_t scratch_bytes, int32_t check);
+/* d_out[slot, h, j] = d_in[slot, h, j] + the attention weight exp(scale q . k_j - lse) that key j of key head h receives, summed over
+ * the sequence's rows and the query heads of h; keys j < d_lens[i] alone.  d_in, d_out: DEVICE float [slots, heads, capacity], the same
+ * array or two apart.  d_lse: what l2pd_attention_kv4 gave for the same rows.  No slot twice in a call where d_in == d_out. */
+l2pd_status l2pd_kv4_weights(void *stream, const l2pd_kv4 *cache, const void *q, const float *d_lse, const float *d_in, float *d_out, int32_t B,
+                             int32_t rows, const int32_t *d_row_start, const int32_t *d_slots, const int32_t *d_lens, int32_t max_len,
+                             int32_t Hq, int64_t q_stride, float scale);
+/* Keeps min(d_lens[i], keep) keys of every head: protected keys first, then by weight, largest first (NaN last), equal ones
+ * by index.  A key is protected if its position is below `first` or not below d_protect_from[i] (DEVICE int32 [B] or NULL).
+ * d_positions: DEVICE int32 [slots, heads, capacity], or NULL: a key's position is its index.  Kept keys of index below the new length
+ * stay at their place; the others fill the free places, both in ascending order.  d_kept: DEVICE int32 [B, heads, keep], the index
+ * that place j was filled from, -1 behind the new length.  d_lens_out: DEVICE int32 [B], not d_lens itself.
+ * into: where the kept records go; NULL or the cache itself: in place, only the free places are written.  Another cache has the same
+ * heads and head_dim, its own memory and a capacity of at least min(keep, max_len, capacity); slots mean the same in both.
+ * d_weights_into, d_positions_into: DEVICE arrays [slots, heads, capacity of the destination] that receive the kept keys' weights
+ * and positions, or NULL; d_weights and d_positions themselves where the capacities agree.  max_len at most 524288.  No slot
+ * twice in a call. */
+l2pd_status l2pd_kv4_evict(void *stream, const l2pd_kv4 *cache, const l2pd_kv4 *into, const float *d_weights, float *d_weights_into,
+                           const int32_t *d_positions, int32_t *d_positions_into, int32_t B, const int32_t *d_slots, const int32_t *d_lens,
+                           int32_t max_len, int32_t keep, int32_t first, const int32_t *d_protect_from, int32_t *d_kept,
+                           int32_t *d_lens_out);
+
+/*
+ * Norms of queries and keys for each head, with the rotation by position in the same pass, for models that norm them before their
+ * attention: y = x g / sqrt(mean(x^2) + eps) over the head_dim numbers of a (row, head), then the pair (y_i, y_{i + head_dim/2})
+ * is turned by the angle position * theta^(-2i/head_dim), as the transformer above pairs them; the angle is reduced in 64 bits, whatever
+ * the position.  q [rows, Hq, head_dim], k [rows, Hk, head_dim]: DEVICE, L2PD_F32 or L2PD_BF16, row strides in elements; the outputs may
+ * be the inputs (same strides).  q_gain, k_gain: DEVICE float [head_dim]; NULL: no norm, the rotation alone.  d_positions: DEVICE int32
+ * [rows]; NULL: the row's number.  head_dim even, at most 256; Hq or Hk may be 0.  One rounding, at the store.
+ */
+l2pd_status l2pd_qk_norm_rope(void *stream, int32_t dtype, const void *q, const void *k, void *q_out, void *k_out, const float *q_gain,
+                              const float *k_gain, const int32_t *d_positions, int32_t rows, int32_t Hq, int32_t Hk, int32_t head_dim,
+                              int64_t q_stride, int64_t k_stride, int64_t q_out_stride, int64_t k_out_stride, float eps, float theta);
+
+/*
  * Environment switches (read once, at l2pd_init or at the first call that uses them; diagnostics and
  * comparisons only — the defaults are the product):
  *   L2PD_FORCE_SIMT=1       bf16 configurations run their GEMMs and attention on the CUDA-core cross-check kernels

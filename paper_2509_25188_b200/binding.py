@@ -52,6 +52,10 @@ class TrainConfig(C.Structure):
                 ("weight_decay", C.c_float), ("epochs", C.c_int32), ("batch_size", C.c_int32)]
 
 
+class Kv4(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("slots", C.c_int32), ("heads", C.c_int32), ("head_dim", C.c_int32), ("capacity", C.c_int32)]
+
+
 class StepOut(C.Structure):
     _fields_ = [("d_conf", C.c_void_p), ("d_pred", C.c_void_p), ("d_p", C.c_void_p),
                 ("d_unmask", C.c_void_p), ("d_logits", C.c_void_p),
@@ -64,7 +68,9 @@ EXPORTS = ["l2pd_init", "l2pd_state_reset", "l2pd_denoise_step", "l2pd_decode", 
            "l2pd_launch_count", "l2pd_last_step_ms", "l2pd_profile_enable", "l2pd_profile_read", "l2pd_last_error", "l2pd_destroy",
            "l2pd_gemm_bf16", "l2pd_gemm_bf16_residual", "l2pd_gemm_bf16_swiglu", "l2pd_lm_head_bf16",
            "l2pd_lm_head_scratch_elems", "l2pd_attention_bf16", "l2pd_lm_head_bf16_static",
-           "l2pd_set_chain", "l2pd_chain_trace_enable", "l2pd_chain_trace_read", "l2pd_debug_set_device_status", "l2pd_debug_filter_train"]
+           "l2pd_set_chain", "l2pd_chain_trace_enable", "l2pd_chain_trace_read", "l2pd_debug_set_device_status", "l2pd_debug_filter_train",
+           "l2pd_kv4_bytes", "l2pd_kv4_store", "l2pd_kv4_load", "l2pd_attention_kv4", "l2pd_attention_kv4_scratch_bytes",
+           "l2pd_kv4_weights", "l2pd_kv4_evict", "l2pd_qk_norm_rope"]
 
 
 KINDS = ["embed", "gemm_qkv", "rope", "attention", "gemm_o", "rmsnorm", "gemm_gate_up", "gemm_down",
@@ -119,6 +125,16 @@ def _load() -> C.CDLL:
     lib.l2pd_chain_trace_enable.argtypes = [vp, i32]
     lib.l2pd_chain_trace_read.argtypes = [vp, vp, i64, C.POINTER(i32), C.POINTER(i32), C.POINTER(i32)]
     lib.l2pd_chain_trace_read.restype = i64
+    lib.l2pd_kv4_bytes.argtypes = [i32, i32, i32, i32]
+    lib.l2pd_kv4_bytes.restype = i64
+    lib.l2pd_kv4_store.argtypes = [vp, vp, vp, vp, i32, i32, vp, vp, vp, i64, i64]
+    lib.l2pd_kv4_load.argtypes = [vp, vp, i32, vp, vp, i32, i32, vp, vp, vp, i64, i64]
+    lib.l2pd_attention_kv4_scratch_bytes.argtypes = [vp, i32, i32, i32, i32]
+    lib.l2pd_attention_kv4_scratch_bytes.restype = i64
+    lib.l2pd_attention_kv4.argtypes = [vp, vp, vp, vp, vp, i32, i32, vp, vp, vp, i32, i32, i64, i64, f32, vp, i64, i32]
+    lib.l2pd_kv4_weights.argtypes = [vp, vp, vp, vp, vp, vp, i32, i32, vp, vp, vp, i32, i32, i64, f32]
+    lib.l2pd_kv4_evict.argtypes = [vp, vp, vp, vp, vp, vp, vp, i32, vp, vp, i32, i32, i32, vp, vp, vp]
+    lib.l2pd_qk_norm_rope.argtypes = [vp, i32, vp, vp, vp, vp, vp, vp, vp, i32, i32, i32, i32, i64, i64, i64, i64, f32, f32]
     return lib
 
 
@@ -464,6 +480,211 @@ def attention_bf16(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, H: int, dh
     _check(lib.l2pd_attention_bf16(_stream(), q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(),
                                    Tq, Tk, H, dh, q.stride(0), k.stride(0), out.stride(0), impl, 1))
     return out
+
+
+# ---- operators around a key/value cache in 4 bits --------------------------------------------------------------------
+
+def _rows(x: torch.Tensor, heads: int, dh: int, what: str, dtype=torch.bfloat16):
+    """A packed batch [N, heads, dh] or [B, rows, heads, dh]: its row stride, after the checks the library cannot make."""
+    if x.dtype != dtype or not x.is_cuda:
+        raise ValueError("%s must be a %s tensor on a GPU" % (what, dtype))
+    if x.dim() not in (3, 4) or x.shape[-2] != heads or x.shape[-1] != dh:
+        raise ValueError("%s must be [rows, %d, %d] or [sequences, rows, %d, %d]" % (what, heads, dh, heads, dh))
+    st = x.stride()
+    if st[-1] != 1 or (heads > 1 and st[-2] != dh) or (x.dim() == 4 and x.shape[0] > 1 and st[0] != x.shape[1] * st[1]):
+        raise ValueError("%s: heads and their numbers must be contiguous, sequences one row stride apart" % what)
+    return st[-3] if x.shape[-3] > 1 else (st[0] if x.dim() == 4 and x.shape[0] > 1 else max(st[-3], heads * dh))
+
+
+def _ints(x: Optional[torch.Tensor], n: int, what: str, device):
+    """Address of an int32 array of at least n entries, or None."""
+    if x is None:
+        return None
+    if x.dtype != torch.int32 or x.device != device or not x.is_contiguous() or x.numel() < n:
+        raise ValueError("%s must be a contiguous int32 tensor of at least %d entries on %s" % (what, n, device))
+    return x.data_ptr()
+
+
+def _batch(x: torch.Tensor, row_start: Optional[torch.Tensor], max_rows: Optional[int]):
+    """(sequences, most rows of one, address of row_start) of a packed batch."""
+    if x.dim() == 4:
+        if row_start is not None:
+            raise ValueError("row_start goes with packed rows [N, heads, head_dim]")
+        return int(x.shape[0]), int(x.shape[1]), None
+    if row_start is None:
+        return 1, int(x.shape[0]), None
+    if max_rows is None:
+        raise ValueError("row_start needs max_rows, the most rows of a sequence")
+    b = row_start.numel() - 1
+    return b, int(max_rows), _ints(row_start, 1, "row_start", x.device)
+
+
+class _on:
+    """The tensor's device as the current one during a call; enter gives its current stream."""
+
+    def __init__(self, device):
+        self.device, self.back = device, None
+
+    def __enter__(self) -> int:
+        now = torch.cuda.current_device()
+        if now != self.device.index:
+            self.back = now
+            torch.cuda.set_device(self.device)
+        return torch.cuda.current_stream().cuda_stream
+
+    def __exit__(self, *exc):
+        if self.back is not None:
+            torch.cuda.set_device(self.back)
+
+
+class KvCache4:
+    """A key/value cache in 4 bits: `slots` sequences of up to `capacity` keys, `heads` key heads of 64 or 128 numbers.
+    Zeroed at start.  All calls run on the cache's device and its current stream; arrays of the batch (slots, lengths, starts) are
+    int32 device tensors.  Row tensors are [sequences, rows, heads, head_dim], or packed [N, heads, head_dim] with row_start
+    [sequences + 1] and max_rows."""
+
+    def __init__(self, slots: int, heads: int, head_dim: int, capacity: int, device: int = 0):
+        n = lib.l2pd_kv4_bytes(slots, heads, head_dim, capacity)
+        if n <= 0:
+            raise L2pdError(-2, "cache of %d slots, %d heads of %d, %d keys" % (slots, heads, head_dim, capacity))
+        self.slots, self.heads, self.head_dim, self.capacity = slots, heads, head_dim, capacity
+        self.data = torch.zeros(n, dtype=torch.uint8, device="cuda:%d" % device)
+        self.device = self.data.device
+        self._c = Kv4(self.data.data_ptr(), slots, heads, head_dim, capacity)
+        self._ref = C.addressof(self._c)
+
+    def _same_device(self, *tensors):
+        for x in tensors:
+            if x is not None and x.device != self.device:
+                raise ValueError("a tensor is not on the cache's device %s" % self.device)
+
+    def store(self, k: torch.Tensor, v: torch.Tensor, key_start=None, slots=None, row_start=None, max_rows=None):
+        """Row r of sequence i becomes key key_start[i] + r (key_start None: r) of slot slots[i] (None: i)."""
+        ks, vs = _rows(k, self.heads, self.head_dim, "k"), _rows(v, self.heads, self.head_dim, "v")
+        if k.shape != v.shape:
+            raise ValueError("k and v differ in shape")
+        self._same_device(k, v)
+        b, rows, rs = _batch(k, row_start, max_rows)
+        with _on(self.device) as stream:
+            _check(lib.l2pd_kv4_store(stream, self._ref, k.data_ptr(), v.data_ptr(), b, rows, rs, _ints(slots, b, "slots", self.device),
+                                      _ints(key_start, b, "key_start", self.device), ks, vs))
+
+    def load(self, rows: int, key_start=None, slots=None, row_start=None, total_rows=None, dtype=torch.bfloat16):
+        """The values of `rows` keys of each sequence, from key_start[i] on: (k, v), [sequences, rows, heads, head_dim].  With
+        row_start: packed [total_rows, heads, head_dim], at most `rows` of a sequence."""
+        if dtype not in (torch.bfloat16, torch.float32):
+            raise ValueError("dtype is torch.bfloat16 or torch.float32")
+        if row_start is not None:
+            if total_rows is None:
+                raise ValueError("row_start needs total_rows, the rows of the packed result")
+            b, shape = row_start.numel() - 1, (total_rows, self.heads, self.head_dim)
+        else:
+            given = slots if slots is not None else key_start
+            b = self.slots if given is None else given.numel()
+            shape = (b, rows, self.heads, self.head_dim)
+        k = torch.empty(shape, dtype=dtype, device=self.device)
+        v = torch.empty_like(k)
+        st = self.heads * self.head_dim
+        with _on(self.device) as stream:
+            _check(lib.l2pd_kv4_load(stream, self._ref, L2PD_BF16 if dtype == torch.bfloat16 else L2PD_F32, k.data_ptr(), v.data_ptr(), b, rows,
+                                     _ints(row_start, b + 1, "row_start", self.device), _ints(slots, b, "slots", self.device),
+                                     _ints(key_start, b, "key_start", self.device), st, st))
+        return k, v
+
+    def attention(self, q: torch.Tensor, lens: torch.Tensor, max_len: int, row_start=None, max_rows=None, slots=None,
+                  scale: Optional[float] = None, out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None, check: bool = False):
+        """Softmax attention of q [.., Hq, head_dim] over the first lens[i] keys of each sequence, lens[i] <= max_len; scale None:
+        1 / sqrt(head_dim).  Returns (out, lse), q's shape in bf16 and [.., Hq] in fp32."""
+        hq = q.shape[-2]
+        qs = _rows(q, hq, self.head_dim, "q")
+        b, rows, rs = _batch(q, row_start, max_rows)
+        if out is None:
+            out = torch.empty(q.shape, dtype=torch.bfloat16, device=self.device)
+        if lse is None:
+            lse = torch.empty(q.shape[:-1], dtype=torch.float32, device=self.device)
+        self._same_device(q, out, lse)
+        if out.shape != q.shape or lse.shape != q.shape[:-1] or lse.dtype != torch.float32 or not lse.is_contiguous():
+            raise ValueError("out has q's shape, lse [.., Hq] in contiguous fp32")
+        with _on(self.device) as stream:
+            n = lib.l2pd_attention_kv4_scratch_bytes(self._ref, b, rows, hq, max_len)
+            scratch = torch.empty(max(n, 16), dtype=torch.uint8, device=self.device)
+            _check(lib.l2pd_attention_kv4(stream, self._ref, q.data_ptr(), out.data_ptr(), lse.data_ptr(), b, rows, rs,
+                                          _ints(slots, b, "slots", self.device), _ints(lens, b, "lens", self.device), max_len, hq, qs,
+                                          _rows(out, hq, self.head_dim, "out"), 1.0 / self.head_dim ** 0.5 if scale is None else scale,
+                                          scratch.data_ptr(), n, int(check)))
+        return out, lse
+
+    def _per_key(self, x: torch.Tensor, dtype, what: str):
+        if x.shape != (self.slots, self.heads, self.capacity) or x.dtype != dtype or not x.is_contiguous():
+            raise ValueError("%s must be a contiguous %s tensor [slots, heads, capacity] of its cache" % (what, dtype))
+        self._same_device(x)
+        return x.data_ptr()
+
+    def attention_weights(self, q: torch.Tensor, lse: torch.Tensor, lens: torch.Tensor, max_len: int, weights: torch.Tensor,
+                          out: Optional[torch.Tensor] = None, row_start=None, max_rows=None, slots=None, scale: Optional[float] = None):
+        """out = weights + what every key receives from these rows, weights [slots, heads, capacity] in fp32 (out None: in place).
+        lse is attention()'s.  Returns out; keys at and behind a sequence's length are not written."""
+        hq = q.shape[-2]
+        qs = _rows(q, hq, self.head_dim, "q")
+        b, rows, rs = _batch(q, row_start, max_rows)
+        out = weights if out is None else out
+        self._same_device(q, lse)
+        if lse.shape != q.shape[:-1] or lse.dtype != torch.float32 or not lse.is_contiguous():
+            raise ValueError("lse must be [.., Hq] in contiguous fp32")
+        with _on(self.device) as stream:
+            _check(lib.l2pd_kv4_weights(stream, self._ref, q.data_ptr(), lse.data_ptr(), self._per_key(weights, torch.float32, "weights"),
+                                        self._per_key(out, torch.float32, "out"), b, rows, rs, _ints(slots, b, "slots", self.device),
+                                        _ints(lens, b, "lens", self.device), max_len, hq, qs,
+                                        1.0 / self.head_dim ** 0.5 if scale is None else scale))
+        return out
+
+    def evict(self, weights: torch.Tensor, lens: torch.Tensor, max_len: int, keep: int, positions=None, first: int = 0, protect_from=None,
+              slots=None, into: Optional["KvCache4"] = None, weights_into=None, positions_into=None):
+        """Keeps the `keep` heaviest keys of every head (see l2pd_kv4_evict) in `into`, or in place, where weights and positions
+        follow in place too unless arrays for them are given.  Returns (kept [sequences, heads, keep], the new lengths)."""
+        dst = self if into is None else into
+        if dst is self:
+            weights_into = weights if weights_into is None else weights_into
+            positions_into = positions if positions_into is None else positions_into
+        b = lens.numel()
+        self._same_device(dst.data)
+        kept = torch.empty(b, self.heads, max(keep, 0), dtype=torch.int32, device=self.device)
+        lens_out = torch.empty(b, dtype=torch.int32, device=self.device)
+        with _on(self.device) as stream:
+            _check(lib.l2pd_kv4_evict(stream, self._ref, dst._ref, self._per_key(weights, torch.float32, "weights"),
+                                      None if weights_into is None else dst._per_key(weights_into, torch.float32, "weights_into"),
+                                      None if positions is None else self._per_key(positions, torch.int32, "positions"),
+                                      None if positions_into is None else dst._per_key(positions_into, torch.int32, "positions_into"),
+                                      b, _ints(slots, b, "slots", self.device), _ints(lens, b, "lens", self.device), max_len, keep, first,
+                                      _ints(protect_from, b, "protect_from", self.device), kept.data_ptr(), lens_out.data_ptr()))
+        return kept, lens_out
+
+
+def qk_norm_rope(q: torch.Tensor, k: torch.Tensor, q_gain=None, k_gain=None, positions=None, theta: float = 10000.0, eps: float = 1e-5,
+                 q_out=None, k_out=None):
+    """Head norms (gains fp32 [dh], None: none) and rotation of q [rows, Hq, dh] and k [rows, Hk, dh] (bf16 or fp32) by their
+    positions (int32 [rows], None: the row's number).  Returns (q_out, k_out); the inputs themselves may be given for them."""
+    if q.dim() != 3 or k.dim() != 3 or q.shape[0] != k.shape[0] or q.shape[2] != k.shape[2] or q.dtype != k.dtype or q.dtype not in (torch.bfloat16, torch.float32):
+        raise ValueError("q [rows, Hq, dh] and k [rows, Hk, dh], both bf16 or both fp32")
+    t, hq, dh = q.shape
+    hk = k.shape[1]
+    if q_out is None:
+        q_out = torch.empty((t, hq, dh), dtype=q.dtype, device=q.device)
+    if k_out is None:
+        k_out = torch.empty((t, hk, dh), dtype=q.dtype, device=q.device)
+    if q_out.shape != q.shape or k_out.shape != k.shape:
+        raise ValueError("the outputs have their inputs' shapes")
+    strides = [_rows(x, x.shape[1], dh, n, q.dtype) for x, n in ((q, "q"), (k, "k"), (q_out, "q_out"), (k_out, "k_out"))]
+    for g, n in ((q_gain, "q_gain"), (k_gain, "k_gain")):
+        if g is not None and (g.dtype != torch.float32 or g.numel() != dh or not g.is_contiguous() or g.device != q.device):
+            raise ValueError("%s must be a contiguous fp32 tensor [dh] on %s" % (n, q.device))
+    if any(x.device != q.device for x in (k, q_out, k_out)):
+        raise ValueError("the tensors lie on different devices")
+    with _on(q.device) as stream:
+        _check(lib.l2pd_qk_norm_rope(stream, L2PD_BF16 if q.dtype == torch.bfloat16 else L2PD_F32, q.data_ptr(), k.data_ptr(), q_out.data_ptr(),
+                                     k_out.data_ptr(), None if q_gain is None else q_gain.data_ptr(), None if k_gain is None else k_gain.data_ptr(),
+                                     _ints(positions, t, "positions", q.device), t, hq, hk, dh, *strides, eps, theta))
+    return q_out, k_out
 
 
 def _flat_params(arrays, dev):

@@ -14,6 +14,7 @@
 #include <vector>
 
 #include "common.cuh"
+#include "kv4.cuh"
 
 using namespace l2pd;
 
@@ -1492,6 +1493,198 @@ l2pd_status l2pd_attention_bf16(void *stream, const void *q, const void *k, cons
   if (e != cudaSuccess) return L2PD_ERR_CUDA;
   if (check && cudaStreamSynchronize((cudaStream_t)stream) != cudaSuccess) return L2PD_ERR_CUDA;
   return L2PD_OK;
+}
+
+// ---- operators around a key/value cache in 4 bits ---------------------------------------------------------------------------
+
+static l2pd_status refuse(l2pd_status st, const char *call, const char *why) {
+  set_standalone_error("%s: %s", call, why);
+  return st;
+}
+static bool aligned16(const void *p) { return ((uintptr_t)p & 15u) == 0; }
+
+static bool kv4_sizes_ok(int32_t slots, int32_t heads, int32_t head_dim, int32_t capacity) {
+  return slots >= 1 && heads >= 1 && heads <= 65535 && (head_dim == 64 || head_dim == 128) && capacity >= 1 && capacity <= 0x7fffffc0;
+}
+
+int64_t l2pd_kv4_bytes(int32_t slots, int32_t heads, int32_t head_dim, int32_t capacity) {
+  if (!kv4_sizes_ok(slots, heads, head_dim, capacity)) return 0;
+  const int64_t head = ceil_div64(capacity, KV4_TILE) * kv4_tile_bytes(head_dim);
+  if (head > INT64_MAX / heads / slots) return 0;
+  return head * heads * slots;
+}
+
+// The device's view of a cache, after the checks that every call makes.
+static l2pd_status kv4_view(const char *call, const l2pd_kv4 *c, Kv4View *v) {
+  if (!c || !c->data) return refuse(L2PD_ERR_ARG, call, "null cache");
+  if (!l2pd_kv4_bytes(c->slots, c->heads, c->head_dim, c->capacity))
+    return refuse(L2PD_ERR_SHAPE, call, "cache of slots >= 1, 1 to 65535 heads of 64 or 128, capacity >= 1");
+  if (!aligned16(c->data)) return refuse(L2PD_ERR_ARG, call, "the cache is not 16-byte aligned");
+  v->data = (uint8_t *)c->data; v->slots = c->slots; v->heads = c->heads; v->dh = c->head_dim; v->cap = c->capacity;
+  v->head_bytes = ceil_div64(c->capacity, KV4_TILE) * kv4_tile_bytes(c->head_dim);
+  v->slot_bytes = v->head_bytes * c->heads;
+  return L2PD_OK;
+}
+
+static l2pd_status kv4_batch(const char *call, int32_t B, int32_t rows, const int32_t *row_start, const int32_t *slots, const int32_t *keys,
+                             Kv4Batch *b) {
+  if (B < 0 || B > 65535 || rows < 0 || (int64_t)B * rows > 0x7fffffff)
+    return refuse(L2PD_ERR_SHAPE, call, "0 to 65535 sequences, rows >= 0, fewer than 2^31 rows in all");
+  b->B = B; b->rows = rows; b->row_start = row_start; b->slots = slots; b->keys = keys;
+  return L2PD_OK;
+}
+
+static l2pd_status kv4_launched(const char *call, cudaError_t e) {
+  return e == cudaSuccess ? L2PD_OK : standalone_cuda_error(call, e);
+}
+
+l2pd_status l2pd_kv4_store(void *stream, const l2pd_kv4 *cache, const void *k, const void *v, int32_t B, int32_t rows,
+                           const int32_t *d_row_start, const int32_t *d_slots, const int32_t *d_key_start, int64_t k_stride, int64_t v_stride) {
+  const char *call = "l2pd_kv4_store";
+  Kv4View c; Kv4Batch b;
+  l2pd_status r = kv4_view(call, cache, &c);
+  if (r == L2PD_OK) r = kv4_batch(call, B, rows, d_row_start, d_slots, d_key_start, &b);
+  if (r != L2PD_OK) return r;
+  if (B == 0 || rows == 0) return L2PD_OK;
+  if (!k || !v) return refuse(L2PD_ERR_ARG, call, "null pointer");
+  const int64_t w = (int64_t)c.heads * c.dh;
+  if (k_stride < w || v_stride < w || k_stride % 8 || v_stride % 8 || !aligned16(k) || !aligned16(v))
+    return refuse(L2PD_ERR_SHAPE, call, "row strides of at least heads * head_dim, rows on 16 bytes");
+  return kv4_launched(call, launch_kv4_store((cudaStream_t)stream, c, (const bf16 *)k, (const bf16 *)v, b, k_stride, v_stride));
+}
+
+l2pd_status l2pd_kv4_load(void *stream, const l2pd_kv4 *cache, int32_t dtype, void *k, void *v, int32_t B, int32_t rows,
+                          const int32_t *d_row_start, const int32_t *d_slots, const int32_t *d_key_start, int64_t k_stride, int64_t v_stride) {
+  const char *call = "l2pd_kv4_load";
+  Kv4View c; Kv4Batch b;
+  l2pd_status r = kv4_view(call, cache, &c);
+  if (r == L2PD_OK) r = kv4_batch(call, B, rows, d_row_start, d_slots, d_key_start, &b);
+  if (r != L2PD_OK) return r;
+  if (dtype != L2PD_F32 && dtype != L2PD_BF16) return refuse(L2PD_ERR_ARG, call, "dtype is L2PD_F32 or L2PD_BF16");
+  if (B == 0 || rows == 0) return L2PD_OK;
+  if (!k || !v) return refuse(L2PD_ERR_ARG, call, "null pointer");
+  const int64_t w = (int64_t)c.heads * c.dh;
+  if (k_stride < w || v_stride < w || k_stride % 8 || v_stride % 8 || !aligned16(k) || !aligned16(v))
+    return refuse(L2PD_ERR_SHAPE, call, "row strides of at least heads * head_dim, rows on 16 bytes");
+  return kv4_launched(call, launch_kv4_load((cudaStream_t)stream, c, dtype, k, v, b, k_stride, v_stride));
+}
+
+// What attention and the weights have in common
+static l2pd_status kv4_query_checks(const char *call, const Kv4View &c, const void *q, const int32_t *d_lens, int32_t rows, int32_t max_len,
+                                    int32_t Hq, int64_t q_stride) {
+  if ((rows && !q) || !d_lens) return refuse(L2PD_ERR_ARG, call, "null pointer");
+  if (Hq < 1 || Hq % c.heads || max_len < 0 || (int64_t)rows * (Hq / c.heads) > 0x7fffffff)
+    return refuse(L2PD_ERR_SHAPE, call, "query heads a multiple of the cache's heads, max_len >= 0");
+  if (q_stride < (int64_t)Hq * c.dh || q_stride % 8 || !aligned16(q))
+    return refuse(L2PD_ERR_SHAPE, call, "row stride of at least Hq * head_dim, rows on 16 bytes");
+  return L2PD_OK;
+}
+
+int64_t l2pd_attention_kv4_scratch_bytes(const l2pd_kv4 *cache, int32_t B, int32_t rows, int32_t Hq, int32_t max_len) {
+  if (!cache || !kv4_sizes_ok(cache->slots, cache->heads, cache->head_dim, cache->capacity) || B < 0 || rows < 0 || Hq < 1 ||
+      Hq % cache->heads || max_len < 0)
+    return 0;
+  Kv4View c{};
+  c.heads = cache->heads; c.dh = cache->head_dim; c.cap = cache->capacity;
+  return 4 * attention_kv4_scratch_floats(c, B, rows, Hq, max_len, device_sms());
+}
+
+l2pd_status l2pd_attention_kv4(void *stream, const l2pd_kv4 *cache, const void *q, void *out, float *d_lse, int32_t B, int32_t rows,
+                               const int32_t *d_row_start, const int32_t *d_slots, const int32_t *d_lens, int32_t max_len, int32_t Hq,
+                               int64_t q_stride, int64_t out_stride, float scale, void *scratch, int64_t scratch_bytes, int32_t check) {
+  const char *call = "l2pd_attention_kv4";
+  Kv4AttnArgs a;
+  l2pd_status r = kv4_view(call, cache, &a.c);
+  if (r == L2PD_OK) r = kv4_batch(call, B, rows, d_row_start, d_slots, d_lens, &a.b);
+  if (r != L2PD_OK) return r;
+  if (B == 0 || rows == 0) return L2PD_OK;
+  r = kv4_query_checks(call, a.c, q, d_lens, rows, max_len, Hq, q_stride);
+  if (r != L2PD_OK) return r;
+  if (!out || !scratch) return refuse(L2PD_ERR_ARG, call, "null pointer");
+  if (out_stride < (int64_t)Hq * a.c.dh || out_stride % 8 || !aligned16(out) || !aligned16(scratch))
+    return refuse(L2PD_ERR_SHAPE, call, "row stride of at least Hq * head_dim, rows and scratch on 16 bytes");
+  const int sms = device_sms();
+  if (scratch_bytes < 4 * attention_kv4_scratch_floats(a.c, B, rows, Hq, max_len, sms))
+    return refuse(L2PD_ERR_SHAPE, call, "scratch smaller than l2pd_attention_kv4_scratch_bytes");
+  a.max_len = max_len; a.Hq = Hq; a.q = (const bf16 *)q; a.out = (bf16 *)out; a.lse = d_lse; a.q_stride = q_stride; a.out_stride = out_stride;
+  a.scale = scale; a.scratch = (float *)scratch;
+  a.status = standalone_status();
+  if (!a.status) return refuse(L2PD_ERR_CUDA, call, "no status word");
+  r = kv4_launched(call, launch_attention_kv4((cudaStream_t)stream, a, sms));
+  return r == L2PD_OK ? finish_standalone((cudaStream_t)stream, a.status, check) : r;
+}
+
+l2pd_status l2pd_kv4_weights(void *stream, const l2pd_kv4 *cache, const void *q, const float *d_lse, const float *d_in, float *d_out, int32_t B,
+                             int32_t rows, const int32_t *d_row_start, const int32_t *d_slots, const int32_t *d_lens, int32_t max_len,
+                             int32_t Hq, int64_t q_stride, float scale) {
+  const char *call = "l2pd_kv4_weights";
+  Kv4WeighArgs a;
+  l2pd_status r = kv4_view(call, cache, &a.c);
+  if (r == L2PD_OK) r = kv4_batch(call, B, rows, d_row_start, d_slots, d_lens, &a.b);
+  if (r != L2PD_OK) return r;
+  if (B == 0 || max_len == 0) return L2PD_OK;
+  r = kv4_query_checks(call, a.c, q, d_lens, rows, max_len, Hq, q_stride);
+  if (r != L2PD_OK) return r;
+  if ((rows && !d_lse) || !d_in || !d_out) return refuse(L2PD_ERR_ARG, call, "null pointer");
+  a.max_len = max_len; a.Hq = Hq; a.q = (const bf16 *)q; a.lse = d_lse; a.q_stride = q_stride; a.scale = scale; a.w_in = d_in; a.w_out = d_out;
+  return kv4_launched(call, launch_kv4_weights((cudaStream_t)stream, a, device_sms()));
+}
+
+l2pd_status l2pd_kv4_evict(void *stream, const l2pd_kv4 *cache, const l2pd_kv4 *into, const float *d_weights, float *d_weights_into,
+                           const int32_t *d_positions, int32_t *d_positions_into, int32_t B, const int32_t *d_slots, const int32_t *d_lens,
+                           int32_t max_len, int32_t keep, int32_t first, const int32_t *d_protect_from, int32_t *d_kept,
+                           int32_t *d_lens_out) {
+  const char *call = "l2pd_kv4_evict";
+  Kv4EvictArgs a;
+  l2pd_status r = kv4_view(call, cache, &a.src);
+  if (r == L2PD_OK) r = kv4_view(call, into ? into : cache, &a.dst);
+  if (r == L2PD_OK) r = kv4_batch(call, B, 0, nullptr, d_slots, d_lens, &a.b);
+  if (r != L2PD_OK) return r;
+  if (B == 0) return L2PD_OK;
+  if (!d_weights || !d_lens || !d_kept || !d_lens_out) return refuse(L2PD_ERR_ARG, call, "null pointer");
+  if (d_lens_out == d_lens) return refuse(L2PD_ERR_ARG, call, "the new lengths need an array of their own");
+  const int32_t longest = max_len < a.src.cap ? max_len : a.src.cap;
+  if (keep < 1 || max_len < 0 || longest > KV4_MAX_EVICT) return refuse(L2PD_ERR_SHAPE, call, "keep >= 1, at most 524288 keys");
+  if (a.dst.heads != a.src.heads || a.dst.dh != a.src.dh || a.dst.cap < (keep < longest ? keep : longest))
+    return refuse(L2PD_ERR_SHAPE, call, "the destination has the cache's heads and head_dim, and room for the kept keys");
+  const bool same = a.src.data == a.dst.data;
+  const int64_t sb = a.src.slot_bytes * a.src.slots, db = a.dst.slot_bytes * a.dst.slots;
+  if (same ? a.src.cap != a.dst.cap : (a.src.data < a.dst.data + db && a.dst.data < a.src.data + sb))
+    return refuse(L2PD_ERR_ARG, call, "the destination is the cache itself or a buffer apart from it");
+  if (a.src.cap != a.dst.cap && (d_weights == d_weights_into || (d_positions && d_positions == d_positions_into)))
+    return refuse(L2PD_ERR_ARG, call, "weights and positions of a destination of another capacity need arrays of their own");
+  a.max_len = longest; a.keep = keep; a.first = first; a.weights = d_weights; a.weights_dst = d_weights_into; a.positions = d_positions;
+  a.positions_dst = d_positions_into; a.protect_from = d_protect_from; a.kept = d_kept; a.lens_out = d_lens_out;
+  return kv4_launched(call, launch_kv4_evict((cudaStream_t)stream, a));
+}
+
+l2pd_status l2pd_qk_norm_rope(void *stream, int32_t dtype, const void *q, const void *k, void *q_out, void *k_out, const float *q_gain,
+                              const float *k_gain, const int32_t *d_positions, int32_t rows, int32_t Hq, int32_t Hk, int32_t head_dim,
+                              int64_t q_stride, int64_t k_stride, int64_t q_out_stride, int64_t k_out_stride, float eps, float theta) {
+  const char *call = "l2pd_qk_norm_rope";
+  if (dtype != L2PD_F32 && dtype != L2PD_BF16) return refuse(L2PD_ERR_ARG, call, "dtype is L2PD_F32 or L2PD_BF16");
+  if (rows < 0 || Hq < 0 || Hk < 0 || Hq > 65535 || Hk > 65535 || head_dim < 2 || head_dim > 256 || head_dim % 2)
+    return refuse(L2PD_ERR_SHAPE, call, "rows >= 0, heads in [0, 65535], an even head_dim of at most 256");
+  if (!(theta > 0.f) || !(theta < INFINITY) || !(eps >= 0.f)) return refuse(L2PD_ERR_ARG, call, "theta > 0 and eps >= 0");
+  if (rows == 0 || Hq + Hk == 0) return L2PD_OK;
+  if ((Hq && (!q || !q_out)) || (Hk && (!k || !k_out))) return refuse(L2PD_ERR_ARG, call, "null pointer");
+  const int64_t wq = (int64_t)Hq * head_dim, wk = (int64_t)Hk * head_dim;
+  if (q_stride < wq || q_out_stride < wq || k_stride < wk || k_out_stride < wk)
+    return refuse(L2PD_ERR_SHAPE, call, "row strides of at least heads * head_dim");
+  if ((Hq && q == q_out && q_stride != q_out_stride) || (Hk && k == k_out && k_stride != k_out_stride))
+    return refuse(L2PD_ERR_ARG, call, "in place, the strides are the same");
+  const int e = dtype == L2PD_BF16 ? 2 : 4, per = 16 / e;
+  NormRopeArgs a;
+  a.q = q; a.k = k; a.q_out = q_out; a.k_out = k_out; a.q_gain = q_gain; a.k_gain = k_gain; a.positions = d_positions;
+  a.rows = rows; a.Hq = Hq; a.Hk = Hk; a.dh = head_dim; a.q_stride = q_stride; a.k_stride = k_stride; a.qo_stride = q_out_stride;
+  a.ko_stride = k_out_stride; a.eps = eps; a.theta = theta;
+  a.vec = head_dim % (2 * per) == 0 &&
+          (!Hq || (aligned16(q) && aligned16(q_out) && q_stride % per == 0 && q_out_stride % per == 0)) &&
+          (!Hk || (aligned16(k) && aligned16(k_out) && k_stride % per == 0 && k_out_stride % per == 0)) &&
+          (!q_gain || aligned16(q_gain)) && (!k_gain || aligned16(k_gain));
+  const int sms = device_sms();
+  return kv4_launched(call, dtype == L2PD_BF16 ? launch_qk_norm_rope<bf16>((cudaStream_t)stream, a, sms)
+                                               : launch_qk_norm_rope<float>((cudaStream_t)stream, a, sms));
 }
 
 }  // extern "C"

@@ -1,0 +1,297 @@
+// A key/value cache in 4 bits: rows written into it, read back as values, and evicted from it.
+#include "kv4.cuh"
+
+namespace l2pd {
+
+namespace {
+
+// ---- store -------------------------------------------------------------------------------------------------------------
+// dh / 8 threads hold a row, eight values each.  The codes are those of the exact quotient (x - m) / s: the fp32 quotient is
+// within 5e-6 of it, so where it comes within 1e-4 of a border the thread decides its eight codes in 64 bits.
+__device__ __forceinline__ uint32_t kv4_codes(const float *x, float m, float s) {
+  uint32_t w = 0;
+  if (!(s > 0.f)) return w;
+  const float inv = 1.f / s;
+  bool sure = true;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const float t = (x[i] - m) * inv, c = rintf(t);
+    sure = sure && fabsf(t - c) < 0.4999f;           // false for the NaN of an overflown 1 / s too
+    w |= (uint32_t)fminf(c, 15.f) << (4 * i);
+  }
+  if (sure) return w;
+  w = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const double c = rint(((double)x[i] - (double)m) / (double)s);
+    w |= (uint32_t)(c < 15.0 ? c : 15.0) << (4 * i);
+  }
+  return w;
+}
+
+constexpr int STORE_ROWS = 64;   // rows of a block
+
+template <int DH>
+__global__ void __launch_bounds__(256) kv4_store_kernel(const Kv4View c, const bf16 *k, const bf16 *v, const Kv4Batch b, int64_t k_stride,
+                                                        int64_t v_stride) {
+  constexpr int G = DH / 8;
+  grid_dep_launch();
+  grid_dep_wait();
+  const int seq = blockIdx.y, h = blockIdx.x % c.heads, r0 = blockIdx.x / c.heads * STORE_ROWS;
+  const int n = b.n_rows(seq), slot = b.slot(seq, c.slots);
+  if (slot < 0 || r0 >= n) return;
+  const bool is_v = blockIdx.z;
+  const int64_t stride = is_v ? v_stride : k_stride;
+  const int li = threadIdx.x % G, start = b.keys ? b.keys[seq] : 0;
+  const unsigned lanes = (G == 16 ? 0xffffu : 0xffu) << ((threadIdx.x & 31) / G * G);   // the threads of this row
+  const bf16 *src = (is_v ? v : k) + b.row0(seq) * stride + (int64_t)h * DH + 8 * li;
+  for (int r = r0 + threadIdx.x / G; r < min(n, r0 + STORE_ROWS); r += 256 / G) {
+    const uint4 raw = *reinterpret_cast<const uint4 *>(src + r * stride);
+    const uint32_t wv[4] = {raw.x, raw.y, raw.z, raw.w};
+    float x[8], mn = INFINITY, mx = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      x[i] = __uint_as_float(i & 1 ? wv[i >> 1] & 0xffff0000u : wv[i >> 1] << 16);
+      mn = fminf(mn, x[i]);
+      mx = fabsf(x[i]) < INFINITY ? fmaxf(mx, x[i]) : INFINITY;
+    }
+#pragma unroll
+    for (int o = G / 2; o; o >>= 1) {
+      mn = fminf(mn, __shfl_xor_sync(lanes, mn, o));
+      mx = fmaxf(mx, __shfl_xor_sync(lanes, mx, o));
+    }
+    const float range = mx - mn;
+    const bool fine = range < INFINITY;               // no infinity, no NaN, no range beyond fp32
+    const float s = fine ? __bfloat162float(__float2bfloat16_rn(__fdiv_rn(range, 15.f))) : __uint_as_float(0x7fc00000u);
+    const uint32_t codes = fine ? kv4_codes(x, mn, s) : 0u;
+    const int64_t key = (int64_t)start + r;
+    if (key < 0 || key >= c.cap) continue;
+    uint8_t *t = c.tile(slot, h, (int)(key / KV4_TILE));
+    const int kr = (int)(key % KV4_TILE);
+    const int off = is_v ? kv4_off_v(DH) + kr * (DH / 2) + ((4 * li) ^ kv4_v_swizzle(kr, DH)) : kr * (DH / 2) + 4 * li;
+    *reinterpret_cast<uint32_t *>(t + off) = codes;
+    if (li == 0) {
+      const uint32_t meta = (__float_as_uint(s) >> 16) | (fine ? __float_as_uint(mn) & 0xffff0000u : 0x7fc00000u);
+      *reinterpret_cast<uint32_t *>(t + (is_v ? kv4_off_vmeta(DH) : kv4_off_kmeta(DH)) + 4 * kr) = meta;
+    }
+  }
+}
+
+// ---- load --------------------------------------------------------------------------------------------------------------
+// As store, backwards.  Rows whose key or slot does not exist read as 0.
+template <int DH, typename T>
+__global__ void __launch_bounds__(256) kv4_load_kernel(const Kv4View c, T *k, T *v, const Kv4Batch b, int64_t k_stride, int64_t v_stride) {
+  constexpr int G = DH / 8;
+  grid_dep_launch();
+  grid_dep_wait();
+  const int seq = blockIdx.y, h = blockIdx.x % c.heads, r0 = blockIdx.x / c.heads * STORE_ROWS;
+  const int n = b.n_rows(seq), slot = b.slot(seq, c.slots);
+  if (r0 >= n) return;
+  const bool is_v = blockIdx.z;
+  const int64_t stride = is_v ? v_stride : k_stride;
+  const int li = threadIdx.x % G, start = b.keys ? b.keys[seq] : 0;
+  T *dst = (is_v ? v : k) + b.row0(seq) * stride + (int64_t)h * DH + 8 * li;
+  for (int r = r0 + threadIdx.x / G; r < min(n, r0 + STORE_ROWS); r += 256 / G) {
+    const int64_t key = (int64_t)start + r;
+    uint32_t codes = 0, meta = 0;
+    if (slot >= 0 && key >= 0 && key < c.cap) {
+      const uint8_t *t = c.tile(slot, h, (int)(key / KV4_TILE));
+      const int kr = (int)(key % KV4_TILE);
+      const int off = is_v ? kv4_off_v(DH) + kr * (DH / 2) + ((4 * li) ^ kv4_v_swizzle(kr, DH)) : kr * (DH / 2) + 4 * li;
+      codes = *reinterpret_cast<const uint32_t *>(t + off);
+      meta = *reinterpret_cast<const uint32_t *>(t + (is_v ? kv4_off_vmeta(DH) : kv4_off_kmeta(DH)) + 4 * kr);
+    }
+    const float s = kv4_scale(meta), m = kv4_min(meta);
+    T *y = dst + r * stride;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) y[i] = from_f32<T>(fmaf((float)((codes >> (4 * i)) & 15u), s, m));   // c s is exact
+  }
+}
+
+// ---- eviction ----------------------------------------------------------------------------------------------------------
+// Rank of a weight as an unsigned number: the order of the floats, both zeros alike, NaN below all, protected keys above all.
+__device__ __forceinline__ uint32_t weight_rank(float w, bool is_protected) {
+  if (is_protected) return 0xffffffffu;
+  if (!(w == w)) return 0u;
+  const uint32_t u = w == 0.f ? 0u : __float_as_uint(w);
+  return u >> 31 ? ~u : u | 0x80000000u;
+}
+
+constexpr int SELECT_THREADS = 1024;
+
+// Exclusive sum over the block of one value a thread; *total receives the sum.
+__device__ __forceinline__ int block_scan(int x, int *warp_sums, int *total) {
+  const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
+  int s = x;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int y = __shfl_up_sync(0xffffffffu, s, o);
+    if (lane >= o) s += y;
+  }
+  __syncthreads();
+  if (lane == 31) warp_sums[w] = s;
+  __syncthreads();
+  if (w == 0) {
+    int y = lane < (int)(blockDim.x >> 5) ? warp_sums[lane] : 0;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int z = __shfl_up_sync(0xffffffffu, y, o);
+      if (lane >= o) y += z;
+    }
+    warp_sums[lane] = y;
+  }
+  __syncthreads();
+  *total = warp_sums[(blockDim.x >> 5) - 1];
+  return s - x + (w ? warp_sums[w - 1] : 0);
+}
+
+// One block per (head, sequence).  The rank of the last kept key is found digit by digit (four histograms of 256); a bitmap of
+// the kept keys with the running count before each word then answers both "how many free places before j" and "which is the
+// i-th kept key", so that no list is built.
+__global__ void __launch_bounds__(SELECT_THREADS) kv4_select_kernel(const Kv4EvictArgs a) {
+  extern __shared__ uint32_t sm[];
+  __shared__ int hist[256], warp_sums[32], pick[2];
+  grid_dep_launch();
+  grid_dep_wait();
+  const int h = blockIdx.x, seq = blockIdx.y, H = a.src.heads, tid = threadIdx.x;
+  const int slot = a.b.slot(seq, min(a.src.slots, a.dst.slots));
+  const int n = slot < 0 ? 0 : max(0, min(min(a.b.keys[seq], a.max_len), a.src.cap)), m = min(n, a.keep);
+  int32_t *kept = a.kept + ((int64_t)seq * H + h) * a.keep;
+  if (h == 0 && tid == 0) a.lens_out[seq] = m;
+  for (int j = m + tid; j < a.keep; j += SELECT_THREADS) kept[j] = -1;
+  if (n <= a.keep) {
+    for (int j = tid; j < n; j += SELECT_THREADS) kept[j] = j;
+    return;
+  }
+  const int64_t base = ((int64_t)slot * H + h) * a.src.cap;
+  const int from = a.protect_from ? a.protect_from[seq] : 0x7fffffff;
+  auto rank = [&](int j) {
+    const int pos = a.positions ? a.positions[base + j] : j;
+    return weight_rank(a.weights[base + j], pos < a.first || pos >= from);
+  };
+  uint32_t prefix = 0, mask = 0;
+  int need = m;                                   // of the keys whose leading digits equal the prefix, this many are kept
+  for (int shift = 24; shift >= 0; shift -= 8) {
+    if (tid < 256) hist[tid] = 0;
+    __syncthreads();
+    for (int j = tid; j < n; j += SELECT_THREADS) {
+      const uint32_t r = rank(j);
+      if ((r & mask) == prefix) atomicAdd(&hist[(r >> shift) & 255u], 1);
+    }
+    __syncthreads();
+    // keys in higher digits, counted from the top
+    int total;
+    const int x = tid < 256 ? hist[255 - tid] : 0;
+    const int above = block_scan(x, warp_sums, &total);
+    if (tid < 256 && above < need && above + x >= need) { pick[0] = 255 - tid; pick[1] = above; }
+    __syncthreads();
+    prefix |= (uint32_t)pick[0] << shift;
+    mask |= 255u << shift;
+    need -= pick[1];
+    __syncthreads();
+  }
+  // bitmap: all above the last kept rank, and of the equal ones the first `need`
+  const int words = (n + 31) >> 5, lane = tid & 31;
+  uint32_t *bits = sm;
+  int *before = reinterpret_cast<int *>(sm) + words;
+  for (int w = tid >> 5; w < words; w += SELECT_THREADS / 32) {
+    const int j = w * 32 + lane;
+    const uint32_t r = j < n ? rank(j) : 0u;
+    const uint32_t up = __ballot_sync(0xffffffffu, j < n && r > prefix), eq = __ballot_sync(0xffffffffu, j < n && r == prefix);
+    if (lane == 0) { bits[w] = up; before[w] = (int)eq; }
+  }
+  __syncthreads();
+  int ties = 0, count = 0;
+  for (int w0 = 0; w0 < words; w0 += SELECT_THREADS) {
+    const int w = w0 + tid;
+    uint32_t eq = w < words ? (uint32_t)before[w] : 0u;
+    uint32_t up = w < words ? bits[w] : 0u;
+    int total;
+    int room = need - ties - block_scan(__popc(eq), warp_sums, &total);
+    ties += total;
+    for (; eq && room > 0; --room) { up |= eq & (0u - eq); eq &= eq - 1; }
+    const int e = block_scan(__popc(up), warp_sums, &total);
+    if (w < words) { bits[w] = up; before[w] = count + e; }
+    count += total;
+  }
+  __syncthreads();
+  auto kept_before = [&](int j) { return before[j >> 5] + __popc(bits[j >> 5] & ((1u << (j & 31)) - 1u)); };
+  const int front = kept_before(m);               // kept keys that stay where they are (m < n)
+  for (int j = tid; j < m; j += SELECT_THREADS) {
+    int src = j;
+    if (!((bits[j >> 5] >> (j & 31)) & 1u)) {
+      int want = front + j - kept_before(j);      // the kept key with this many before it
+      int lo = m >> 5, hi = words - 1;            // its word: the last whose count does not pass `want`
+      while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (before[mid] <= want) lo = mid; else hi = mid - 1;
+      }
+      uint32_t u = bits[lo];
+      for (want -= before[lo]; want > 0; --want) u &= u - 1;
+      src = lo * 32 + __ffs(u) - 1;
+    }
+    kept[j] = src;
+  }
+}
+
+// Moves the records: a block takes 64 places, four threads a place.  In place only the filled holes move; their sources lie at or
+// behind the new end, all destinations before it.
+__global__ void __launch_bounds__(256) kv4_move_kernel(const Kv4EvictArgs a) {
+  grid_dep_launch();
+  grid_dep_wait();
+  const int seq = blockIdx.y, H = a.src.heads, h = blockIdx.x % H, part = threadIdx.x & 3;
+  const int j = blockIdx.x / H * 64 + (threadIdx.x >> 2);
+  if (j >= a.keep) return;
+  const int slot = a.b.slot(seq, min(a.src.slots, a.dst.slots));
+  const int s = a.kept[((int64_t)seq * H + h) * a.keep + j];
+  if (slot < 0 || s < 0) return;
+  const int64_t from = ((int64_t)slot * H + h) * a.src.cap + s, to = ((int64_t)slot * H + h) * a.dst.cap + j;
+  if (part == 2 && a.weights_dst && a.weights + from != a.weights_dst + to) a.weights_dst[to] = a.weights[from];
+  if (part == 3 && a.positions_dst && !(a.positions && a.positions + from == a.positions_dst + to))
+    a.positions_dst[to] = a.positions ? a.positions[from] : s;
+  if (a.src.data == a.dst.data && s == j) return;
+  const int dh = a.src.dh, rs = s % KV4_TILE, rd = j % KV4_TILE, row = dh / 2;
+  const uint8_t *ts = a.src.tile(slot, h, s / KV4_TILE);
+  uint8_t *td = a.dst.tile(slot, h, j / KV4_TILE);
+  if (part * 16 < row) {
+    *reinterpret_cast<uint4 *>(td + rd * row + part * 16) = *reinterpret_cast<const uint4 *>(ts + rs * row + part * 16);
+    *reinterpret_cast<uint4 *>(td + kv4_off_v(dh) + rd * row + ((part * 16) ^ kv4_v_swizzle(rd, dh))) =
+        *reinterpret_cast<const uint4 *>(ts + kv4_off_v(dh) + rs * row + ((part * 16) ^ kv4_v_swizzle(rs, dh)));
+  }
+  if (part < 2) {
+    const int o = part ? kv4_off_vmeta(dh) : kv4_off_kmeta(dh);
+    *reinterpret_cast<uint32_t *>(td + o + 4 * rd) = *reinterpret_cast<const uint32_t *>(ts + o + 4 * rs);
+  }
+}
+
+}  // namespace
+
+cudaError_t launch_kv4_store(cudaStream_t st, const Kv4View &c, const bf16 *k, const bf16 *v, const Kv4Batch &b, int64_t k_stride,
+                             int64_t v_stride) {
+  const dim3 grid((unsigned)(ceil_div(b.rows, STORE_ROWS) * c.heads), b.B, 2);
+  if (c.dh == 128) return launch_kernel(kv4_store_kernel<128>, grid, dim3(256), 0, st, c, k, v, b, k_stride, v_stride);
+  return launch_kernel(kv4_store_kernel<64>, grid, dim3(256), 0, st, c, k, v, b, k_stride, v_stride);
+}
+
+cudaError_t launch_kv4_load(cudaStream_t st, const Kv4View &c, int dtype, void *k, void *v, const Kv4Batch &b, int64_t k_stride,
+                            int64_t v_stride) {
+  const dim3 grid((unsigned)(ceil_div(b.rows, STORE_ROWS) * c.heads), b.B, 2);
+  if (dtype == L2PD_BF16) {
+    auto fn = c.dh == 128 ? kv4_load_kernel<128, bf16> : kv4_load_kernel<64, bf16>;
+    return launch_kernel(fn, grid, dim3(256), 0, st, c, (bf16 *)k, (bf16 *)v, b, k_stride, v_stride);
+  }
+  auto fn = c.dh == 128 ? kv4_load_kernel<128, float> : kv4_load_kernel<64, float>;
+  return launch_kernel(fn, grid, dim3(256), 0, st, c, (float *)k, (float *)v, b, k_stride, v_stride);
+}
+
+cudaError_t launch_kv4_evict(cudaStream_t st, const Kv4EvictArgs &a) {
+  const size_t smem = (size_t)ceil_div(a.max_len, 32) * 8;
+  cudaError_t e = cudaSuccess;
+  if (smem > 32 * 1024) e = cudaFuncSetAttribute(kv4_select_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, KV4_MAX_EVICT / 32 * 8);
+  if (e != cudaSuccess) return e;
+  e = launch_kernel(kv4_select_kernel, dim3(a.src.heads, a.b.B), dim3(SELECT_THREADS), smem, st, a);
+  if (e != cudaSuccess) return e;
+  return launch_kernel(kv4_move_kernel, dim3((unsigned)(ceil_div(a.keep, 64) * a.src.heads), a.b.B), dim3(256), 0, st, a);
+}
+
+}  // namespace l2pd

@@ -1,0 +1,538 @@
+"""The operators around the 4-bit cache against their plain forms in 64 bits.
+
+Codes, s and m are defined exactly, so what is stored reads back equal, bit for bit.  Attention: with A the largest sum of
+magnitudes |scale| sum_d |q_d| (c s + |m|) of a score, a score is off by at most D = A (dh / 16 + 8) 2^-23 (a product of 16 terms adds
+at most 2^-23 of the running magnitude, plus eight roundings around it), so a weight by 2 D relative (numerator and sum), plus 2^-20
+for the exponentials and sums.  Probabilities times s are rounded to fp16 (2^-11 relative, or 2^-25 of a number that is at least
+2^-1 for some key: 2^-24 a key), the output to bf16 (2^-8).  With R the largest |value| of the head: |out - want| <= 2^-8 |want| +
+(2^-11 + 2 D + 2^-20 + keys 2^-24) 2 R, |lse - want| <= D + 2^-20 + 2^-22 |want|.
+"""
+from __future__ import annotations
+
+import numpy as np
+import pytest
+import torch
+
+from tests import kv4_plain as plain
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+def _b():
+    from paper_2509_25188_b200 import binding
+    return binding
+
+
+def _i32(x):
+    return torch.tensor(x, dtype=torch.int32, device=DEV)
+
+
+def _rand(seed, *shape, scale=1.0, dtype=torch.bfloat16):
+    g = torch.Generator().manual_seed(seed)
+    return (torch.randn(*shape, generator=g) * scale).to(dtype).to(DEV)
+
+
+def _np(x):
+    return x.double().cpu().numpy()
+
+
+def _same(got, want):
+    got, want = got.float().cpu().numpy(), np.asarray(want, np.float32)
+    assert np.array_equal(got, want, equal_nan=True), np.argwhere(~((got == want) | (np.isnan(got) & np.isnan(want))))[:3]
+
+
+# ---- store and load ----------------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dh,heads,B,rows,start", [(128, 1, 1, 1, 0), (128, 3, 2, 65, 63), (64, 5, 3, 64, 0), (64, 1, 1, 200, 7), (128, 32, 2, 33, 64)])
+def test_store_then_load(dh, heads, B, rows, start):
+    b = _b()
+    c = b.KvCache4(B, heads, dh, start + rows)
+    k, v = _rand(1, B, rows, heads, dh), _rand(2, B, rows, heads, dh, scale=30)
+    c.store(k, v, key_start=_i32([start] * B))
+    for dt in (torch.float32, torch.bfloat16):
+        gk, gv = c.load(rows, key_start=_i32([start] * B), dtype=dt)
+        rnd = (lambda x: x) if dt == torch.float32 else plain.bf16_round
+        _same(gk, rnd(plain.values32(_np(k))))
+        _same(gv, rnd(plain.values32(_np(v))))
+    if start:
+        assert not c.load(start, dtype=torch.float32)[0].any()          # keys before them: still zero
+
+
+def _odd_rows(dh):
+    rows = np.zeros((12, dh), np.float32)
+    rows[0] = 3.25                                                      # no range
+    rows[1, :5] = [-7.5, 7.5, 1e-9, -1e-9, 0]                           # beside a border of step 1
+    rows[2, 0] = np.inf
+    rows[3, 7] = np.nan
+    rows[4, :2] = [-3e38, 3e38]                                         # range beyond fp32
+    rows[5, :2] = [-1e-40, 1e-40]                                       # subnormal step
+    rows[6, :3] = [9.2e-41, 0, 1.8e-40]                                 # step rounds to the smallest subnormal or 0
+    rows[7] = np.arange(dh) % 16 * 0.5                                  # all sixteen codes
+    rows[8] = (np.arange(dh) % 31) * 0.5                                # many values on borders
+    rows[8, -1] = 15.0
+    rows[9] = -np.linspace(1, 2, dh)
+    rows[10] = 3e38
+    rows[11, -1] = -np.inf
+    return torch.from_numpy(rows).to(torch.bfloat16)
+
+
+@pytest.mark.parametrize("dh", [64, 128])
+def test_rows_at_the_ends_of_the_range(dh):
+    b = _b()
+    x = _odd_rows(dh).to(DEV)[:, None]
+    c = b.KvCache4(1, 1, dh, 12)
+    c.store(x, x)
+    gk, gv = c.load(12, dtype=torch.float32)
+    _same(gk[0], plain.values32(_np(x)))
+    _same(gv[0], plain.values32(_np(x)))
+
+
+def test_ragged_batch_into_chosen_slots_and_places():
+    b = _b()
+    c = b.KvCache4(5, 2, 128, 90)
+    starts, slots, at = [0, 3, 3, 40, 41], [4, 0, 2, 1], [0, 5, 60, 89]
+    k, v = _rand(3, 50, 2, 128), _rand(4, 50, 2, 128)                   # rows 41.. belong to nobody
+    c.store(k, v, key_start=_i32(at), slots=_i32(slots), row_start=_i32(starts), max_rows=37)
+    gk, gv = c.load(90, dtype=torch.float32)
+    want = np.zeros((2, 5, 90, 2, 128), np.float32)
+    for i, s in enumerate(slots):
+        for r in range(starts[i], starts[i + 1]):
+            key = at[i] + r - starts[i]
+            if key < 90:                                                # the third sequence runs past the end
+                want[0, s, key], want[1, s, key] = plain.values32(_np(k[r])), plain.values32(_np(v[r]))
+    _same(gk, want[0])
+    _same(gv, want[1])
+    pk, _ = c.load(37, key_start=_i32(at), slots=_i32(slots), row_start=_i32(starts), total_rows=41, dtype=torch.float32)
+    for i, s in enumerate(slots):
+        for r in range(starts[i], starts[i + 1]):
+            key = at[i] + r - starts[i]
+            _same(pk[r], want[0, s, key] if key < 90 else np.zeros((2, 128)))
+
+
+def test_strided_rows_and_slots_that_do_not_exist():
+    b = _b()
+    c = b.KvCache4(2, 2, 64, 64)
+    qkv = _rand(5, 2, 10, 3, 2, 64)                                     # fused rows: q, k, v
+    k, v = qkv[:, :, 1], qkv[:, :, 2]
+    c.store(k, v, slots=_i32([7, -1]))
+    assert not c.data.any()
+    c.store(k, v, key_start=_i32([-3, 60]), slots=_i32([1, 0]))
+    gk, _ = c.load(64, dtype=torch.float32)
+    _same(gk[1, :7], plain.values32(_np(k[0, 3:])))
+    _same(gk[0, 60:], plain.values32(_np(k[1, :4])))
+    assert not gk[1, 7:].any() and not gk[0, :60].any()
+    zk, zv = c.load(3, slots=_i32([9]))
+    assert not zk.any() and not zv.any()
+
+
+# ---- attention ---------------------------------------------------------------------------------------------------------------
+
+def _check_attention(q, k, v, out, lse, scale):
+    """One sequence: q [rows, Hq, dh], k, v [keys, heads, dh] as stored (bf16)."""
+    kk, vv = plain.values(_np(k)), plain.values(_np(v))
+    want, wl, _ = plain.attention(_np(q), kk, vv, scale)
+    got, gl = _np(out), _np(lse)
+    if k.shape[0] == 0:
+        assert (got == 0).all() and (gl == -np.inf).all()
+        return
+    dh, heads = q.shape[2], k.shape[1]
+    group = q.shape[1] // heads
+    code, s, m = plain.quantise(_np(k))
+    size = code * s + np.abs(m)
+    for h in range(q.shape[1]):
+        a = abs(scale) * (np.abs(_np(q)[:, h]) @ size[:, h // group].T).max(-1)
+        d = a * (dh / 16 + 8) * 2.0 ** -23
+        r = np.abs(vv[:, h // group]).max()
+        tol = 2.0 ** -8 * np.abs(want[:, h]) + ((2.0 ** -11 + 2 * d + 2.0 ** -20 + k.shape[0] * 2.0 ** -24) * 2 * r)[:, None]
+        err = np.abs(got[:, h] - want[:, h])
+        assert (err <= tol).all(), (h, float((err / tol).max()))
+        el = np.abs(gl[:, h] - wl[:, h])
+        assert (el <= d + 2.0 ** -20 + 2.0 ** -22 * np.abs(wl[:, h])).all(), (h, float(el.max()))
+
+
+# (heads, group, dh, rows of each sequence, keys of each sequence)
+ATTENTION = [
+    (1, 1, 128, [1], [1]),
+    (1, 1, 64, [1], [2]),
+    (2, 4, 128, [1, 1, 1], [63, 64, 65]),
+    (8, 4, 128, [1], [1000]),
+    (3, 1, 64, [5, 1, 0, 2], [129, 0, 17, 4097]),
+    (2, 3, 128, [3, 2], [500, 77]),                    # nine columns: two groups of eight
+    (4, 1, 128, [32, 32], [512, 300]),
+    (1, 8, 64, [4, 1], [700, 3]),
+    (2, 2, 128, [17, 33, 5], [640, 1, 100]),           # more columns than a chunk of 32
+    (1, 5, 64, [64], [900]),
+    (2, 4, 128, [32, 31], [257, 2000]),                # a block with grouped heads
+    (1, 16, 128, [9], [130]),
+    (1, 1, 128, [1], [70000]),                         # one long sequence over every SM
+    (1, 4, 64, [32], [9000]),
+    (2, 8, 128, [40], [1500]),
+]
+
+
+@pytest.mark.parametrize("heads,group,dh,rows,keys", ATTENTION)
+def test_attention(heads, group, dh, rows, keys):
+    b = _b()
+    B, cap = len(rows), max(keys) + 70
+    c = b.KvCache4(B + 1, heads, dh, cap)
+    n = sum(rows)
+    starts = np.concatenate(([0], np.cumsum(rows))).tolist()
+    slots = [(i + 1) % (B + 1) for i in range(B)]
+    k, v = _rand(6, B, cap, heads, dh, scale=2), _rand(7, B, cap, heads, dh)
+    for i, x in enumerate(keys):
+        k[i, x:], v[i, x:] = float("nan"), float("inf")                 # behind the end: never read
+    c.store(k, v, slots=_i32(slots))
+    q = _rand(8, n + 3, heads * group, dh)
+    out, lse = torch.full_like(q, 7.0), torch.full(q.shape[:2], 7.0, device=DEV)
+    c.attention(q, _i32(keys), max(keys), row_start=_i32(starts), max_rows=max(rows), slots=_i32(slots), out=out, lse=lse, check=True)
+    assert (out[n:] == 7).all() and (lse[n:] == 7).all()
+    for i in range(B):
+        lo, hi = starts[i], starts[i + 1]
+        _check_attention(q[lo:hi], k[i, :keys[i]], v[i, :keys[i]], out[lo:hi], lse[lo:hi], dh ** -0.5)
+    o2, l2 = c.attention(q[:n], _i32(keys), cap, row_start=_i32(starts), max_rows=max(rows), slots=_i32(slots))
+    for i in range(B):                                                  # another max_len may split otherwise
+        lo, hi = starts[i], starts[i + 1]
+        _check_attention(q[lo:hi], k[i, :keys[i]], v[i, :keys[i]], o2[lo:hi], l2[lo:hi], dh ** -0.5)
+    o3, l3 = c.attention(q[:n], _i32(keys), cap, row_start=_i32(starts), max_rows=max(rows), slots=_i32(slots))
+    assert torch.equal(o2, o3) and torch.equal(l2, l3)
+
+
+@pytest.mark.parametrize("vscale", [1e-30, 1e-6, 1e6, 1e25])
+@pytest.mark.parametrize("qscale,rows", [(1e-20, 3), (30.0, 3), (1.0, 40)])
+def test_attention_whatever_the_magnitudes(vscale, qscale, rows):
+    b = _b()
+    c = b.KvCache4(1, 2, 128, 400)
+    k, v = _rand(9, 400, 2, 128), _rand(10, 400, 2, 128, scale=vscale)
+    v[::7] *= 1e-3                                                      # scales that differ from key to key
+    v[5] = float(v[6, 0, 0])                                            # a value row without a range
+    q = _rand(11, rows, 2, 128, scale=qscale)
+    c.store(k, v)
+    out, lse = c.attention(q, _i32([400]), 400)
+    _check_attention(q, k, v, out, lse, 128 ** -0.5)
+
+
+@pytest.mark.parametrize("rows", [2, 20, 40])
+def test_rising_scores_move_the_reference(rows):
+    b = _b()
+    c = b.KvCache4(1, 1, 128, 1000)
+    k, v = _rand(12, 1000, 1, 128, scale=0.1), _rand(13, 1000, 1, 128)
+    k[:, 0, :4] += torch.linspace(-20, 20, 1000, device=DEV)[:, None].to(torch.bfloat16)
+    q = _rand(14, rows, 1, 128)
+    q[:, 0, :4] = 3 * (1 - 2 * (torch.arange(rows, device=DEV) % 2)[:, None]).to(torch.bfloat16)     # rising in even rows, falling in odd ones
+    c.store(k, v)
+    out, lse = c.attention(q, _i32([1000]), 1000, scale=0.7)
+    _check_attention(q, k, v, out, lse, 0.7)
+
+
+@pytest.mark.parametrize("rows", [2, 40])
+def test_nan_stays_where_it_belongs(rows):
+    b = _b()
+    c = b.KvCache4(1, 3, 64, 200)
+    k, v, q = _rand(15, 200, 3, 64), _rand(16, 200, 3, 64), _rand(17, rows, 3, 64)
+    k[150, 0, 3] = float("nan")
+    v[20, 1, 60] = float("inf")
+    q[1, 2, 5] = float("inf")
+    c.store(k, v)
+    out, lse = c.attention(q, _i32([200]), 200)
+    assert out[:, 0].isnan().all() and lse[:, 0].isnan().all()
+    assert out[:, 1].isnan().all() and lse[:, 1].isfinite().all()
+    assert out[1, 2].isnan().all() and out[0, 2].isfinite().all()
+    w = c.attention_weights(q, lse, _i32([200]), 200, torch.zeros(1, 3, 200, device=DEV))
+    assert w[0, 1].isfinite().all() and w[0, 0].isnan().all()
+    out, lse = c.attention(q, _i32([150]), 200)                         # the bad key behind the end
+    assert out[:, 0].isfinite().all()
+
+
+def test_cache_past_32_bits():
+    b = _b()
+    slots, heads, cap = 9, 32, 131072                                   # 5.1 GB
+    c = b.KvCache4(slots, heads, 128, cap)
+    assert c.data.numel() > 2 ** 32
+    k, v, q = _rand(18, 1, 100, heads, 128), _rand(19, 1, 100, heads, 128), _rand(20, 1, 1, heads, 128)
+    at, slot = _i32([cap - 100]), _i32([slots - 1])
+    c.store(k, v, key_start=at, slots=slot)
+    gk, gv = c.load(100, key_start=at, slots=slot, dtype=torch.float32)
+    _same(gk, plain.values32(_np(k)))
+    _same(gv, plain.values32(_np(v)))
+    out, lse = c.attention(q, _i32([cap]), cap, slots=slot)
+    kk, vv = np.zeros((cap, 1, 128)), np.zeros((cap, 1, 128))
+    kk[-100:], vv[-100:] = plain.values(_np(k[0, :, -1:])), plain.values(_np(v[0, :, -1:]))
+    want, wl, ww = plain.attention(_np(q[0, :, -1:]), kk, vv, 128 ** -0.5)
+    assert np.abs(_np(out[0, :, -1]) - want[:, 0]).max() <= 2.0 ** -8 * np.abs(want).max() + 2.0 ** -11 * np.abs(vv).max() * 100 / cap * 8
+    assert np.abs(_np(lse[0, :, -1]) - wl[:, 0]).max() <= 2.0 ** -17
+    w = c.attention_weights(q, lse, _i32([cap]), cap, torch.zeros(slots, heads, cap, device=DEV), slots=slot)
+    assert not w[:-1].any() and np.abs(_np(w[-1, -1]) - ww[0]).max() <= 2.0 ** -15 * ww.max()
+
+
+def test_other_streams_captures_and_strides():
+    b = _b()
+    c = b.KvCache4(2, 2, 128, 300)
+    k, v = _rand(21, 2, 300, 2, 128), _rand(22, 2, 300, 2, 128)
+    wide = _rand(23, 2, 9, 3, 4, 128)
+    q = wide[:, :, 1]                                                   # rows 12 heads apart
+    store = torch.zeros(2, 9, 3, 4, 128, dtype=torch.bfloat16, device=DEV)
+    out = store[:, :, 2]
+    lens = _i32([300, 41])
+    c.store(k, v)
+    want, wl = c.attention(q.contiguous(), lens, 300)
+    lse = torch.empty(2, 9, 4, device=DEV)
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        c.attention(q, lens, 300, out=out, lse=lse)
+    s.synchronize()
+    assert torch.equal(out, want) and torch.equal(lse, wl) and not store[:, :, :2].any()
+    # two graphs over the same cache, replayed in turn and with changed lengths
+    outs, graphs = [torch.zeros_like(want) for _ in range(2)], []
+    weights = torch.zeros(2, 2, 300, device=DEV)
+    for i in range(2):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            _, l = c.attention(q, lens, 300, out=outs[i])
+            c.attention_weights(q, l, lens, 300, weights)
+        graphs.append(g)
+    lens.copy_(_i32([7, 300]))
+    for g in (0, 1, 0, 1):
+        graphs[g].replay()
+    torch.cuda.synchronize()
+    again, al = c.attention(q, lens, 300)
+    assert torch.equal(outs[0], again) and torch.equal(outs[1], again)
+    once = c.attention_weights(q, al, lens, 300, torch.zeros(2, 2, 300, device=DEV))
+    assert torch.allclose(weights, 4 * once, rtol=2.0 ** -21, atol=0)   # four additions, a half-ulp each
+
+
+def test_binding_refuses_wrong_tensors():
+    b = _b()
+    c = b.KvCache4(1, 2, 128, 10)
+    x, n = _rand(24, 5, 2, 128), _i32([5])
+    for bad in (x.float(), x[:, :1], x.cpu(), x.transpose(0, 1), x.view(5, 4, 64)):
+        with pytest.raises(ValueError):
+            c.store(bad, bad)
+    with pytest.raises(ValueError):
+        c.attention(x, n.long(), 5)
+    with pytest.raises(ValueError):
+        c.attention(x, n.cpu(), 5)
+    with pytest.raises(ValueError):
+        c.store(x, x, row_start=_i32([0, 5]))
+    with pytest.raises(ValueError):
+        c.attention_weights(x, torch.zeros(5, 2, device=DEV), n, 5, torch.zeros(1, 2, 9, device=DEV))
+    with pytest.raises(b.L2pdError):
+        c.attention(_rand(24, 5, 3, 128), n, 5)                         # three query heads on two key heads
+    with pytest.raises(b.L2pdError):
+        b.KvCache4(1, 2, 96, 10)
+
+
+# ---- weights -----------------------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("heads,group,dh,rows,keys", [a for a in ATTENTION if max(a[4]) < 10000])
+def test_weights(heads, group, dh, rows, keys):
+    b = _b()
+    B, cap = len(rows), max(keys) + 5
+    c = b.KvCache4(B, heads, dh, cap)
+    n = sum(rows)
+    starts = np.concatenate(([0], np.cumsum(rows))).tolist()
+    k, v, q = _rand(25, B, cap, heads, dh), _rand(26, B, cap, heads, dh), _rand(27, n, heads * group, dh)
+    c.store(k, v)
+    lens, rs = _i32(keys), _i32(starts)
+    _, lse = c.attention(q, lens, cap, row_start=rs, max_rows=max(rows))
+    base = torch.rand(B, heads, cap, device=DEV)
+    out = torch.full_like(base, -1.0)
+    c.attention_weights(q, lse, lens, cap, base, out=out, row_start=rs, max_rows=max(rows))
+    inplace = base.clone()
+    c.attention_weights(q, lse, lens, cap, inplace, row_start=rs, max_rows=max(rows))
+    for i in range(B):
+        kk = plain.values(_np(k[i, :keys[i]]))
+        qi = _np(q[starts[i]:starts[i + 1]])
+        _, _, w = plain.attention(qi, kk, kk, dh ** -0.5)
+        assert (out[i, :, keys[i]:] == -1).all() and torch.equal(inplace[i, :, keys[i]:], base[i, :, keys[i]:])
+        got, was = _np(out[i, :, :keys[i]]), _np(base[i, :, :keys[i]])
+        # a weight is off by twice the score's error, relative, plus the exponential's; the sums of rows * group terms by 2^-24 each
+        code, s, m = plain.quantise(_np(k[i, :keys[i]]))
+        a = max((np.abs(qi[:, h]) @ (code * s + np.abs(m))[:, h // group].T).max() for h in range(heads * group)) if w.size and len(qi) else 0.0
+        d = a * dh ** -0.5 * (dh / 16 + 8) * 2.0 ** -23
+        tol = (2 * d + 2.0 ** -19 + rows[i] * group * 2.0 ** -24) * w + 2.0 ** -23 * (was + w)
+        assert (np.abs(got - was - w) <= tol).all()
+        assert torch.equal(inplace[i, :, :keys[i]], out[i, :, :keys[i]])
+
+
+# ---- eviction ----------------------------------------------------------------------------------------------------------------
+
+def _weights(kind, B, heads, cap):
+    g = torch.Generator().manual_seed(31)
+    w = torch.rand(B, heads, cap, generator=g)
+    if kind == "ties":
+        w = torch.round(w * 4) / 4
+    elif kind == "equal":
+        w = torch.zeros_like(w)
+        w[:, :, ::2] = -0.0
+    elif kind == "wild":
+        w = (w - 0.5) * 10.0 ** torch.randint(-38, 38, w.shape, generator=g)
+        w[:, :, 3::11] = float("nan")
+        w[:, :, 5::13] = float("inf")
+        w[:, :, 7::17] = -float("inf")
+    return w.to(DEV)
+
+
+@pytest.mark.parametrize("into", [False, True])
+@pytest.mark.parametrize("kind", ["plain", "ties", "equal", "wild"])
+@pytest.mark.parametrize("heads,dh,lens,keep,first,guard", [(1, 128, [1], 1, 0, 0), (2, 64, [5, 0, 100, 64], 33, 0, 0), (3, 128, [130, 131], 64, 4, 20),
+                                                            (2, 128, [2050, 1500], 1024, 4, 32), (1, 64, [40], 30, 35, 0), (1, 128, [9000], 8999, 0, 1),
+                                                            (2, 64, [70000], 1, 0, 0), (1, 128, [70000], 20000, 4, 100)])
+def test_evict(into, kind, heads, dh, lens, keep, first, guard):
+    b = _b()
+    B, cap = len(lens), max(lens) + 3
+    slots = list(range(B))[::-1]
+    c = b.KvCache4(B, heads, dh, cap)
+    k, v = _rand(28, B, cap, heads, dh), _rand(29, B, cap, heads, dh)
+    c.store(k, v)
+    w = _weights(kind, B, heads, cap)
+    pos = torch.arange(cap, dtype=torch.int32, device=DEV).expand(B, heads, cap).contiguous() * 2
+    from_ = [2 * max(n - guard, 0) if guard else 2 ** 31 - 1 for n in lens]
+    dcap = keep if into else cap
+    dst = b.KvCache4(B, heads, dh, dcap) if into else c
+    w0, p0, wn = w.clone(), pos.clone(), w.double().cpu().numpy()
+    wi = torch.full((B, heads, dcap), -5.0, device=DEV) if into else None
+    pi = torch.full((B, heads, dcap), -5, dtype=torch.int32, device=DEV) if into else None
+    kept, new = c.evict(w, _i32(lens), max(lens), keep, positions=pos, first=2 * first, protect_from=_i32(from_), slots=_i32(slots),
+                        into=dst if into else None, weights_into=wi, positions_into=pi)
+    gk, gv = dst.load(dcap, dtype=torch.float32)
+    wo, po = (wi, pi) if into else (w, pos)
+    assert new.tolist() == [min(n, keep) for n in lens]
+    ak, av = plain.values32(_np(k)), plain.values32(_np(v))
+    for i, n in enumerate(lens):
+        s, m = slots[i], min(lens[i], keep)
+        for h in range(heads):
+            want = plain.keep(wn[s, h], (2 * np.arange(cap)).tolist(), n, keep, 2 * first, from_[i])
+            assert kept[i, h, :m].tolist() == want and (kept[i, h, m:] == -1).all()
+            _same(gk[s, :m, h], ak[s, want, h])
+            _same(gv[s, :m, h], av[s, want, h])
+            assert torch.equal(wo[s, h, :m].view(torch.int32), w0[s, h, want].view(torch.int32)) and torch.equal(po[s, h, :m], p0[s, h, want])
+            if into:
+                assert (wo[s, h, m:] == -5).all() and (po[s, h, m:] == -5).all() and not gk[s, m:, h].any()
+            else:
+                assert torch.equal(po[s, h, m:], p0[s, h, m:])
+                _same(gk[s, m:, h], ak[s, m:, h])
+
+
+def test_evict_without_positions_and_twice():
+    b = _b()
+    c = b.KvCache4(1, 2, 128, 600)
+    k = _rand(32, 1, 600, 2, 128)
+    c.store(k, k)
+    w = torch.rand(1, 2, 600, device=DEV)
+    wn = _np(w)
+    pos = torch.full((1, 2, 600), -1, dtype=torch.int32, device=DEV)
+    kept, n1 = c.evict(w, _i32([600]), 600, 300, positions_into=pos)   # no positions yet: an index is its key's position
+    first = kept.cpu().numpy()
+    assert np.array_equal(pos[0, :, :300].cpu().numpy(), first[0])
+    kept, n2 = c.evict(w, n1, 600, 100, positions=pos, protect_from=_i32([590]))
+    for h in range(2):
+        p1 = first[0, h]
+        want = plain.keep(wn[0, h][p1], p1.tolist(), 300, 100, 0, 590)
+        assert kept[0, h].tolist() == want and pos[0, h, :100].tolist() == p1[want].tolist()
+        _same(c.load(100, dtype=torch.float32)[0][0, :, h], plain.values32(_np(k))[0, p1[want], h])
+
+
+# ---- norms and rotation ------------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("norm", [True, False])
+@pytest.mark.parametrize("dtype,rows,hq,hk,dh,start", [("bf16", 1, 1, 1, 128, 0), ("bf16", 37, 8, 2, 128, 1000000), ("bf16", 300, 32, 32, 64, 5),
+                                                       ("fp32", 96, 4, 4, 64, 0), ("fp32", 5, 3, 1, 80, 2 ** 31 - 6), ("fp32", 2, 2, 2, 256, 77),
+                                                       ("bf16", 3, 5, 3, 6, 9), ("fp32", 4, 1, 0, 2, 1), ("bf16", 2, 0, 2, 128, 4), ("bf16", 2000, 7, 1, 128, 3)])
+def test_norm_rope(norm, dtype, rows, hq, hk, dh, start):
+    b = _b()
+    dt = torch.bfloat16 if dtype == "bf16" else torch.float32
+    q, k = _rand(33, rows, hq, dh, scale=3, dtype=dt), _rand(34, rows, hk, dh, scale=0.01, dtype=dt)
+    if rows > 2 and hq:
+        q[1] = 0
+    pos = torch.arange(start, start + rows, dtype=torch.int64).clamp(max=2 ** 31 - 1).int()
+    gq, gk = (_rand(35, dh, dtype=torch.float32) + 1, _rand(36, dh, dtype=torch.float32) + 1) if norm else (None, None)
+    for inplace in (False, True):
+        qi, ki = q.clone(), k.clone()
+        qo, ko = b.qk_norm_rope(qi, ki, gq, gk, pos.to(DEV), theta=500000.0, eps=1e-5, q_out=qi if inplace else None, k_out=ki if inplace else None)
+        for x, got, g in ((q, qo, gq), (k, ko, gk)):
+            if not x.numel():
+                continue
+            want = plain.norm_rope(_np(x), None if g is None else _np(g), pos.numpy(), 500000.0, float(np.float32(1e-5)))
+            # fp32 steps: the mean of dh squares (dh + 4 roundings, halved by the root), norm, gain, angle (2^-24 of a half turn, sine and cosine within 2 ulp), two
+            # products and a sum: (dh / 2 + 16) 2^-24 of the pair's magnitude; then the store's half step
+            pair = np.hypot(want[..., :dh // 2], want[..., dh // 2:])
+            pair = np.concatenate((pair, pair), -1)
+            tol = (2.0 ** -8 if dtype == "bf16" else 2.0 ** -24) * np.abs(want) + (dh / 2 + 16) * 2.0 ** -24 * pair
+            assert (np.abs(_np(got) - want) <= tol).all(), float((np.abs(_np(got) - want) - tol).max())
+
+
+def test_norm_rope_strides_alignment_and_default_positions():
+    b = _b()
+    wide = _rand(37, 11, 3, 4, 64)
+    q, k = wide[:, 0], wide[:, 1]
+    flat = _rand(38, 11 * 4 * 64 + 1)
+    odd = flat[1:].view(11, 4, 64)                                      # rows not on 16 bytes
+    odd.copy_(q)
+    want, wk = b.qk_norm_rope(q.contiguous(), k.contiguous(), theta=100.0)
+    got, gk = b.qk_norm_rope(q, k, theta=100.0)
+    go, _ = b.qk_norm_rope(odd, k, theta=100.0)
+    assert torch.equal(want, got) and torch.equal(wk, gk) and torch.equal(go, want)
+    assert torch.equal(want, b.qk_norm_rope(q, k, positions=torch.arange(11, dtype=torch.int32, device=DEV), theta=100.0)[0])
+    vcopy = wide[:, 2].clone()
+    b.qk_norm_rope(q, k, theta=100.0, q_out=q, k_out=k)                 # in place inside the wide rows
+    assert torch.equal(q, want) and torch.equal(k, wk) and torch.equal(wide[:, 2], vcopy)
+    with pytest.raises(ValueError):
+        b.qk_norm_rope(q, k.float())
+
+
+# ---- together ----------------------------------------------------------------------------------------------------------------
+
+def test_a_cached_decode_with_eviction():
+    """Two sequences through norm + rotation, the cache, attention, weights and eviction, block after block, against the same in
+    64 bits on what the cache holds."""
+    b = _b()
+    heads, group, dh, s, prompt, keep = 2, 2, 128, 16, 150, 120
+    B, scale = 2, 128 ** -0.5
+    cap = prompt + 3 * s
+    c = b.KvCache4(B, heads, dh, cap)
+    gain = _rand(40, dh, scale=0.1, dtype=torch.float32) + 1
+    weights = torch.zeros(B, heads, cap, device=DEV)
+    positions = torch.full((B, heads, cap), -1, dtype=torch.int32, device=DEV)
+    lens = _i32([0, 0])
+    mirror = [[([], [], []) for _ in range(heads)] for _ in range(B)]   # per head: keys, values, positions the cache holds
+    seen = 0
+    for step, rows in enumerate([prompt, s, s]):
+        q, k, v = (_rand(50 + 3 * step + i, B, rows, h, dh) for i, h in enumerate((heads * group, heads, heads)))
+        pos = torch.arange(seen, seen + rows, dtype=torch.int32, device=DEV).repeat(B)
+        qr, kr = b.qk_norm_rope(q.view(B * rows, -1, dh), k.view(B * rows, heads, dh), gain, gain, pos, theta=10000.0)
+        qr, kr = qr.view(q.shape), kr.view(k.shape)
+        c.store(kr, v, key_start=lens)
+        n0 = int(lens[0])
+        positions[:, :, n0:n0 + rows] = torch.arange(seen, seen + rows, dtype=torch.int32, device=DEV)
+        lens = lens + rows
+        for i in range(B):
+            for h in range(heads):
+                mk, mv, mp = mirror[i][h]
+                mk += list(plain.values(_np(kr[i, :, h]))); mv += list(plain.values(_np(v[i, :, h]))); mp += range(seen, seen + rows)
+        seen += rows
+        out, lse = c.attention(qr, lens, cap)
+        before = weights.clone()
+        c.attention_weights(qr, lse, lens, cap, weights)
+        n = n0 + rows
+        for i in range(B):
+            for h in range(heads):
+                mk, mv, mp = mirror[i][h]
+                assert positions[i, h, :n].tolist() == list(mp)
+                qh = _np(qr[i, :, h * group:(h + 1) * group])
+                want, wl, ww = plain.attention(qh, np.array(mk)[:, None], np.array(mv)[:, None], scale)
+                r = np.abs(mv).max()
+                d = scale * (np.abs(qh).sum(-1).max() * 2 * np.abs(mk).max()) * 16 * 2.0 ** -23
+                assert (np.abs(_np(out[i, :, h * group:(h + 1) * group]) - want) <= 2.0 ** -8 * np.abs(want) + (2.0 ** -11 + 2 * d + 2.0 ** -18) * 2 * r).all()
+                got = _np(weights[i, h, :n] - before[i, h, :n])
+                assert np.abs(got - ww[0]).max() <= (2 * d + 2.0 ** -17) * max(1.0, ww.max(), float(weights[i, h, :n].max()))
+        old = weights.double().cpu().numpy()
+        kept, lens = c.evict(weights, lens, cap, keep, positions=positions, first=4, protect_from=_i32([seen - s] * B))
+        for i in range(B):
+            for h in range(heads):
+                mk, mv, mp = mirror[i][h]
+                want = plain.keep(old[i, h], list(mp), n, keep, 4, seen - s)
+                assert kept[i, h, :len(want)].tolist() == want
+                mirror[i][h] = ([mk[j] for j in want], [mv[j] for j in want], [mp[j] for j in want])
+    assert lens.tolist() == [keep, keep]
