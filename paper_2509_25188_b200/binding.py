@@ -7,6 +7,7 @@ module without it raises, there is no fallback.
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import os
 from typing import Dict, Optional
 
@@ -490,6 +491,8 @@ def _rows(x: torch.Tensor, heads: int, dh: int, what: str, dtype=torch.bfloat16)
         raise ValueError("%s must be a %s tensor on a GPU" % (what, dtype))
     if x.dim() not in (3, 4) or x.shape[-2] != heads or x.shape[-1] != dh:
         raise ValueError("%s must be [rows, %d, %d] or [sequences, rows, %d, %d]" % (what, heads, dh, heads, dh))
+    if x.is_contiguous():
+        return heads * dh
     st = x.stride()
     if st[-1] != 1 or (heads > 1 and st[-2] != dh) or (x.dim() == 4 and x.shape[0] > 1 and st[0] != x.shape[1] * st[1]):
         raise ValueError("%s: heads and their numbers must be contiguous, sequences one row stride apart" % what)
@@ -519,22 +522,19 @@ def _batch(x: torch.Tensor, row_start: Optional[torch.Tensor], max_rows: Optiona
     return b, int(max_rows), _ints(row_start, 1, "row_start", x.device)
 
 
-class _on:
-    """The tensor's device as the current one during a call; enter gives its current stream."""
+_device_now, _raw_stream = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
 
-    def __init__(self, device):
-        self.device, self.back = device, None
 
-    def __enter__(self) -> int:
-        now = torch.cuda.current_device()
-        if now != self.device.index:
-            self.back = now
-            torch.cuda.set_device(self.device)
-        return torch.cuda.current_stream().cuda_stream
-
-    def __exit__(self, *exc):
-        if self.back is not None:
-            torch.cuda.set_device(self.back)
+def _on_device(fn):
+    """Runs a call on the device of its cache, or of its first tensor."""
+    @functools.wraps(fn)
+    def call(subject, /, *args, **kw):
+        index = subject.device.index
+        if index is None or _device_now() == index:
+            return fn(subject, *args, **kw)
+        with torch.cuda.device(index):
+            return fn(subject, *args, **kw)
+    return call
 
 
 class KvCache4:
@@ -558,6 +558,7 @@ class KvCache4:
             if x is not None and x.device != self.device:
                 raise ValueError("a tensor is not on the cache's device %s" % self.device)
 
+    @_on_device
     def store(self, k: torch.Tensor, v: torch.Tensor, key_start=None, slots=None, row_start=None, max_rows=None):
         """Row r of sequence i becomes key key_start[i] + r (key_start None: r) of slot slots[i] (None: i)."""
         ks, vs = _rows(k, self.heads, self.head_dim, "k"), _rows(v, self.heads, self.head_dim, "v")
@@ -565,10 +566,11 @@ class KvCache4:
             raise ValueError("k and v differ in shape")
         self._same_device(k, v)
         b, rows, rs = _batch(k, row_start, max_rows)
-        with _on(self.device) as stream:
-            _check(lib.l2pd_kv4_store(stream, self._ref, k.data_ptr(), v.data_ptr(), b, rows, rs, _ints(slots, b, "slots", self.device),
-                                      _ints(key_start, b, "key_start", self.device), ks, vs))
+        stream = _raw_stream(self.device.index)
+        _check(lib.l2pd_kv4_store(stream, self._ref, k.data_ptr(), v.data_ptr(), b, rows, rs, _ints(slots, b, "slots", self.device),
+                                  _ints(key_start, b, "key_start", self.device), ks, vs))
 
+    @_on_device
     def load(self, rows: int, key_start=None, slots=None, row_start=None, total_rows=None, dtype=torch.bfloat16):
         """The values of `rows` keys of each sequence, from key_start[i] on: (k, v), [sequences, rows, heads, head_dim].  With
         row_start: packed [total_rows, heads, head_dim], at most `rows` of a sequence."""
@@ -585,12 +587,13 @@ class KvCache4:
         k = torch.empty(shape, dtype=dtype, device=self.device)
         v = torch.empty_like(k)
         st = self.heads * self.head_dim
-        with _on(self.device) as stream:
-            _check(lib.l2pd_kv4_load(stream, self._ref, L2PD_BF16 if dtype == torch.bfloat16 else L2PD_F32, k.data_ptr(), v.data_ptr(), b, rows,
-                                     _ints(row_start, b + 1, "row_start", self.device), _ints(slots, b, "slots", self.device),
-                                     _ints(key_start, b, "key_start", self.device), st, st))
+        stream = _raw_stream(self.device.index)
+        _check(lib.l2pd_kv4_load(stream, self._ref, L2PD_BF16 if dtype == torch.bfloat16 else L2PD_F32, k.data_ptr(), v.data_ptr(), b, rows,
+                                 _ints(row_start, b + 1, "row_start", self.device), _ints(slots, b, "slots", self.device),
+                                 _ints(key_start, b, "key_start", self.device), st, st))
         return k, v
 
+    @_on_device
     def attention(self, q: torch.Tensor, lens: torch.Tensor, max_len: int, row_start=None, max_rows=None, slots=None,
                   scale: Optional[float] = None, out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None, check: bool = False):
         """Softmax attention of q [.., Hq, head_dim] over the first lens[i] keys of each sequence, lens[i] <= max_len; scale None:
@@ -599,19 +602,19 @@ class KvCache4:
         qs = _rows(q, hq, self.head_dim, "q")
         b, rows, rs = _batch(q, row_start, max_rows)
         if out is None:
-            out = torch.empty(q.shape, dtype=torch.bfloat16, device=self.device)
+            out = torch.empty_like(q, memory_format=torch.contiguous_format)
         if lse is None:
             lse = torch.empty(q.shape[:-1], dtype=torch.float32, device=self.device)
         self._same_device(q, out, lse)
         if out.shape != q.shape or lse.shape != q.shape[:-1] or lse.dtype != torch.float32 or not lse.is_contiguous():
             raise ValueError("out has q's shape, lse [.., Hq] in contiguous fp32")
-        with _on(self.device) as stream:
-            n = lib.l2pd_attention_kv4_scratch_bytes(self._ref, b, rows, hq, max_len)
-            scratch = torch.empty(max(n, 16), dtype=torch.uint8, device=self.device)
-            _check(lib.l2pd_attention_kv4(stream, self._ref, q.data_ptr(), out.data_ptr(), lse.data_ptr(), b, rows, rs,
-                                          _ints(slots, b, "slots", self.device), _ints(lens, b, "lens", self.device), max_len, hq, qs,
-                                          _rows(out, hq, self.head_dim, "out"), 1.0 / self.head_dim ** 0.5 if scale is None else scale,
-                                          scratch.data_ptr(), n, int(check)))
+        stream = _raw_stream(self.device.index)
+        n = lib.l2pd_attention_kv4_scratch_bytes(self._ref, b, rows, hq, max_len)
+        scratch = torch.empty(max(n, 16), dtype=torch.uint8, device=self.device)
+        _check(lib.l2pd_attention_kv4(stream, self._ref, q.data_ptr(), out.data_ptr(), lse.data_ptr(), b, rows, rs,
+                                      _ints(slots, b, "slots", self.device), _ints(lens, b, "lens", self.device), max_len, hq, qs,
+                                      _rows(out, hq, self.head_dim, "out"), 1.0 / self.head_dim ** 0.5 if scale is None else scale,
+                                      scratch.data_ptr(), n, int(check)))
         return out, lse
 
     def _per_key(self, x: torch.Tensor, dtype, what: str):
@@ -620,6 +623,7 @@ class KvCache4:
         self._same_device(x)
         return x.data_ptr()
 
+    @_on_device
     def attention_weights(self, q: torch.Tensor, lse: torch.Tensor, lens: torch.Tensor, max_len: int, weights: torch.Tensor,
                           out: Optional[torch.Tensor] = None, row_start=None, max_rows=None, slots=None, scale: Optional[float] = None):
         """out = weights + what every key receives from these rows, weights [slots, heads, capacity] in fp32 (out None: in place).
@@ -631,13 +635,14 @@ class KvCache4:
         self._same_device(q, lse)
         if lse.shape != q.shape[:-1] or lse.dtype != torch.float32 or not lse.is_contiguous():
             raise ValueError("lse must be [.., Hq] in contiguous fp32")
-        with _on(self.device) as stream:
-            _check(lib.l2pd_kv4_weights(stream, self._ref, q.data_ptr(), lse.data_ptr(), self._per_key(weights, torch.float32, "weights"),
-                                        self._per_key(out, torch.float32, "out"), b, rows, rs, _ints(slots, b, "slots", self.device),
-                                        _ints(lens, b, "lens", self.device), max_len, hq, qs,
-                                        1.0 / self.head_dim ** 0.5 if scale is None else scale))
+        stream = _raw_stream(self.device.index)
+        _check(lib.l2pd_kv4_weights(stream, self._ref, q.data_ptr(), lse.data_ptr(), self._per_key(weights, torch.float32, "weights"),
+                                    self._per_key(out, torch.float32, "out"), b, rows, rs, _ints(slots, b, "slots", self.device),
+                                    _ints(lens, b, "lens", self.device), max_len, hq, qs,
+                                    1.0 / self.head_dim ** 0.5 if scale is None else scale))
         return out
 
+    @_on_device
     def evict(self, weights: torch.Tensor, lens: torch.Tensor, max_len: int, keep: int, positions=None, first: int = 0, protect_from=None,
               slots=None, into: Optional["KvCache4"] = None, weights_into=None, positions_into=None):
         """Keeps the `keep` heaviest keys of every head (see l2pd_kv4_evict) in `into`, or in place, where weights and positions
@@ -650,16 +655,17 @@ class KvCache4:
         self._same_device(dst.data)
         kept = torch.empty(b, self.heads, max(keep, 0), dtype=torch.int32, device=self.device)
         lens_out = torch.empty(b, dtype=torch.int32, device=self.device)
-        with _on(self.device) as stream:
-            _check(lib.l2pd_kv4_evict(stream, self._ref, dst._ref, self._per_key(weights, torch.float32, "weights"),
-                                      None if weights_into is None else dst._per_key(weights_into, torch.float32, "weights_into"),
-                                      None if positions is None else self._per_key(positions, torch.int32, "positions"),
-                                      None if positions_into is None else dst._per_key(positions_into, torch.int32, "positions_into"),
-                                      b, _ints(slots, b, "slots", self.device), _ints(lens, b, "lens", self.device), max_len, keep, first,
-                                      _ints(protect_from, b, "protect_from", self.device), kept.data_ptr(), lens_out.data_ptr()))
+        stream = _raw_stream(self.device.index)
+        _check(lib.l2pd_kv4_evict(stream, self._ref, dst._ref, self._per_key(weights, torch.float32, "weights"),
+                                  None if weights_into is None else dst._per_key(weights_into, torch.float32, "weights_into"),
+                                  None if positions is None else self._per_key(positions, torch.int32, "positions"),
+                                  None if positions_into is None else dst._per_key(positions_into, torch.int32, "positions_into"),
+                                  b, _ints(slots, b, "slots", self.device), _ints(lens, b, "lens", self.device), max_len, keep, first,
+                                  _ints(protect_from, b, "protect_from", self.device), kept.data_ptr(), lens_out.data_ptr()))
         return kept, lens_out
 
 
+@_on_device
 def qk_norm_rope(q: torch.Tensor, k: torch.Tensor, q_gain=None, k_gain=None, positions=None, theta: float = 10000.0, eps: float = 1e-5,
                  q_out=None, k_out=None):
     """Head norms (gains fp32 [dh], None: none) and rotation of q [rows, Hq, dh] and k [rows, Hk, dh] (bf16 or fp32) by their
@@ -669,9 +675,9 @@ def qk_norm_rope(q: torch.Tensor, k: torch.Tensor, q_gain=None, k_gain=None, pos
     t, hq, dh = q.shape
     hk = k.shape[1]
     if q_out is None:
-        q_out = torch.empty((t, hq, dh), dtype=q.dtype, device=q.device)
+        q_out = torch.empty_like(q, memory_format=torch.contiguous_format)
     if k_out is None:
-        k_out = torch.empty((t, hk, dh), dtype=q.dtype, device=q.device)
+        k_out = torch.empty_like(k, memory_format=torch.contiguous_format)
     if q_out.shape != q.shape or k_out.shape != k.shape:
         raise ValueError("the outputs have their inputs' shapes")
     strides = [_rows(x, x.shape[1], dh, n, q.dtype) for x, n in ((q, "q"), (k, "k"), (q_out, "q_out"), (k_out, "k_out"))]
@@ -680,10 +686,10 @@ def qk_norm_rope(q: torch.Tensor, k: torch.Tensor, q_gain=None, k_gain=None, pos
             raise ValueError("%s must be a contiguous fp32 tensor [dh] on %s" % (n, q.device))
     if any(x.device != q.device for x in (k, q_out, k_out)):
         raise ValueError("the tensors lie on different devices")
-    with _on(q.device) as stream:
-        _check(lib.l2pd_qk_norm_rope(stream, L2PD_BF16 if q.dtype == torch.bfloat16 else L2PD_F32, q.data_ptr(), k.data_ptr(), q_out.data_ptr(),
-                                     k_out.data_ptr(), None if q_gain is None else q_gain.data_ptr(), None if k_gain is None else k_gain.data_ptr(),
-                                     _ints(positions, t, "positions", q.device), t, hq, hk, dh, *strides, eps, theta))
+    stream = _raw_stream(q.device.index)
+    _check(lib.l2pd_qk_norm_rope(stream, L2PD_BF16 if q.dtype == torch.bfloat16 else L2PD_F32, q.data_ptr(), k.data_ptr(), q_out.data_ptr(),
+                                 k_out.data_ptr(), None if q_gain is None else q_gain.data_ptr(), None if k_gain is None else k_gain.data_ptr(),
+                                 _ints(positions, t, "positions", q.device), t, hq, hk, dh, *strides, eps, theta))
     return q_out, k_out
 
 

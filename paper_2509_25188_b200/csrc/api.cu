@@ -1678,7 +1678,7 @@ l2pd_status l2pd_qk_norm_rope(void *stream, int32_t dtype, const void *q, const 
   a.q = q; a.k = k; a.q_out = q_out; a.k_out = k_out; a.q_gain = q_gain; a.k_gain = k_gain; a.positions = d_positions;
   a.rows = rows; a.Hq = Hq; a.Hk = Hk; a.dh = head_dim; a.q_stride = q_stride; a.k_stride = k_stride; a.qo_stride = q_out_stride;
   a.ko_stride = k_out_stride; a.eps = eps; a.theta = theta;
-  a.vec = head_dim % (2 * per) == 0 &&
+  a.vec = head_dim % 16 == 0 &&
           (!Hq || (aligned16(q) && aligned16(q_out) && q_stride % per == 0 && q_out_stride % per == 0)) &&
           (!Hk || (aligned16(k) && aligned16(k_out) && k_stride % per == 0 && k_out_stride % per == 0)) &&
           (!q_gain || aligned16(q_gain)) && (!k_gain || aligned16(k_gain));

@@ -18,34 +18,6 @@ __device__ __forceinline__ float block_sum(float v, float *red) {
   return t;
 }
 
-template <typename T> struct Vec8;
-template <> struct Vec8<bf16> {
-  uint4 raw;
-  __device__ __forceinline__ void load(const bf16 *p) { raw = *reinterpret_cast<const uint4 *>(p); }
-  __device__ __forceinline__ void store(bf16 *p) const { *reinterpret_cast<uint4 *>(p) = raw; }
-  __device__ __forceinline__ float get(int i) const {
-    const __nv_bfloat16 *h = reinterpret_cast<const __nv_bfloat16 *>(&raw);
-    return __bfloat162float(h[i]);
-  }
-  __device__ __forceinline__ void set(int i, float f) {
-    __nv_bfloat16 *h = reinterpret_cast<__nv_bfloat16 *>(&raw);
-    h[i] = __float2bfloat16_rn(f);
-  }
-};
-template <> struct Vec8<float> {
-  float4 a, b;
-  __device__ __forceinline__ void load(const float *p) {
-    a = *reinterpret_cast<const float4 *>(p);
-    b = *reinterpret_cast<const float4 *>(p + 4);
-  }
-  __device__ __forceinline__ void store(float *p) const {
-    *reinterpret_cast<float4 *>(p) = a;
-    *reinterpret_cast<float4 *>(p + 4) = b;
-  }
-  __device__ __forceinline__ float get(int i) const { return reinterpret_cast<const float *>(&a)[i]; }
-  __device__ __forceinline__ void set(int i, float f) { reinterpret_cast<float *>(&a)[i] = f; }
-};
-
 constexpr int META_BATCH = STEP_META_BATCH;
 struct MetaBatch { SeqMeta m[META_BATCH]; };
 

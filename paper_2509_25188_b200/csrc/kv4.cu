@@ -29,25 +29,29 @@ __device__ __forceinline__ uint32_t kv4_codes(const float *x, float m, float s) 
   return w;
 }
 
-constexpr int STORE_ROWS = 64;   // rows of a block
+// A block takes rows of one head; a thread has four of them in flight.
+template <int DH> constexpr int STORE_ROWS = 4 * 256 / (DH / 8);
 
 template <int DH>
 __global__ void __launch_bounds__(256) kv4_store_kernel(const Kv4View c, const bf16 *k, const bf16 *v, const Kv4Batch b, int64_t k_stride,
                                                         int64_t v_stride) {
-  constexpr int G = DH / 8;
+  constexpr int G = DH / 8, STEP = 256 / G;
   grid_dep_launch();
   grid_dep_wait();
-  const int seq = blockIdx.y, h = blockIdx.x % c.heads, r0 = blockIdx.x / c.heads * STORE_ROWS;
+  const int seq = blockIdx.y, h = blockIdx.x % c.heads, r0 = blockIdx.x / c.heads * STORE_ROWS<DH> + threadIdx.x / G;
   const int n = b.n_rows(seq), slot = b.slot(seq, c.slots);
-  if (slot < 0 || r0 >= n) return;
+  if (slot < 0 || blockIdx.x / c.heads * STORE_ROWS<DH> >= n) return;
   const bool is_v = blockIdx.z;
   const int64_t stride = is_v ? v_stride : k_stride;
   const int li = threadIdx.x % G, start = b.keys ? b.keys[seq] : 0;
-  const unsigned lanes = (G == 16 ? 0xffffu : 0xffu) << ((threadIdx.x & 31) / G * G);   // the threads of this row
   const bf16 *src = (is_v ? v : k) + b.row0(seq) * stride + (int64_t)h * DH + 8 * li;
-  for (int r = r0 + threadIdx.x / G; r < min(n, r0 + STORE_ROWS); r += 256 / G) {
-    const uint4 raw = *reinterpret_cast<const uint4 *>(src + r * stride);
-    const uint32_t wv[4] = {raw.x, raw.y, raw.z, raw.w};
+  uint4 raw[4];
+#pragma unroll
+  for (int u = 0; u < 4; ++u)
+    raw[u] = r0 + u * STEP < n ? *reinterpret_cast<const uint4 *>(src + (r0 + u * STEP) * stride) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+  for (int u = 0; u < 4; ++u) {
+    const uint32_t wv[4] = {raw[u].x, raw[u].y, raw[u].z, raw[u].w};
     float x[8], mn = INFINITY, mx = -INFINITY;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
@@ -57,15 +61,15 @@ __global__ void __launch_bounds__(256) kv4_store_kernel(const Kv4View c, const b
     }
 #pragma unroll
     for (int o = G / 2; o; o >>= 1) {
-      mn = fminf(mn, __shfl_xor_sync(lanes, mn, o));
-      mx = fmaxf(mx, __shfl_xor_sync(lanes, mx, o));
+      mn = fminf(mn, __shfl_xor_sync(0xffffffffu, mn, o));
+      mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
     }
     const float range = mx - mn;
     const bool fine = range < INFINITY;               // no infinity, no NaN, no range beyond fp32
     const float s = fine ? __bfloat162float(__float2bfloat16_rn(__fdiv_rn(range, 15.f))) : __uint_as_float(0x7fc00000u);
     const uint32_t codes = fine ? kv4_codes(x, mn, s) : 0u;
-    const int64_t key = (int64_t)start + r;
-    if (key < 0 || key >= c.cap) continue;
+    const int64_t key = (int64_t)start + r0 + u * STEP;
+    if (r0 + u * STEP >= n || key < 0 || key >= c.cap) continue;
     uint8_t *t = c.tile(slot, h, (int)(key / KV4_TILE));
     const int kr = (int)(key % KV4_TILE);
     const int off = is_v ? kv4_off_v(DH) + kr * (DH / 2) + ((4 * li) ^ kv4_v_swizzle(kr, DH)) : kr * (DH / 2) + 4 * li;
@@ -81,30 +85,37 @@ __global__ void __launch_bounds__(256) kv4_store_kernel(const Kv4View c, const b
 // As store, backwards.  Rows whose key or slot does not exist read as 0.
 template <int DH, typename T>
 __global__ void __launch_bounds__(256) kv4_load_kernel(const Kv4View c, T *k, T *v, const Kv4Batch b, int64_t k_stride, int64_t v_stride) {
-  constexpr int G = DH / 8;
+  constexpr int G = DH / 8, STEP = 256 / G;
   grid_dep_launch();
   grid_dep_wait();
-  const int seq = blockIdx.y, h = blockIdx.x % c.heads, r0 = blockIdx.x / c.heads * STORE_ROWS;
+  const int seq = blockIdx.y, h = blockIdx.x % c.heads, r0 = blockIdx.x / c.heads * STORE_ROWS<DH> + threadIdx.x / G;
   const int n = b.n_rows(seq), slot = b.slot(seq, c.slots);
   if (r0 >= n) return;
   const bool is_v = blockIdx.z;
   const int64_t stride = is_v ? v_stride : k_stride;
   const int li = threadIdx.x % G, start = b.keys ? b.keys[seq] : 0;
   T *dst = (is_v ? v : k) + b.row0(seq) * stride + (int64_t)h * DH + 8 * li;
-  for (int r = r0 + threadIdx.x / G; r < min(n, r0 + STORE_ROWS); r += 256 / G) {
-    const int64_t key = (int64_t)start + r;
-    uint32_t codes = 0, meta = 0;
-    if (slot >= 0 && key >= 0 && key < c.cap) {
+  uint32_t codes[4], meta[4];
+#pragma unroll
+  for (int u = 0; u < 4; ++u) {
+    const int64_t key = (int64_t)start + r0 + u * STEP;
+    codes[u] = meta[u] = 0;
+    if (slot >= 0 && r0 + u * STEP < n && key >= 0 && key < c.cap) {
       const uint8_t *t = c.tile(slot, h, (int)(key / KV4_TILE));
       const int kr = (int)(key % KV4_TILE);
       const int off = is_v ? kv4_off_v(DH) + kr * (DH / 2) + ((4 * li) ^ kv4_v_swizzle(kr, DH)) : kr * (DH / 2) + 4 * li;
-      codes = *reinterpret_cast<const uint32_t *>(t + off);
-      meta = *reinterpret_cast<const uint32_t *>(t + (is_v ? kv4_off_vmeta(DH) : kv4_off_kmeta(DH)) + 4 * kr);
+      codes[u] = *reinterpret_cast<const uint32_t *>(t + off);
+      meta[u] = *reinterpret_cast<const uint32_t *>(t + (is_v ? kv4_off_vmeta(DH) : kv4_off_kmeta(DH)) + 4 * kr);
     }
-    const float s = kv4_scale(meta), m = kv4_min(meta);
-    T *y = dst + r * stride;
+  }
 #pragma unroll
-    for (int i = 0; i < 8; ++i) y[i] = from_f32<T>(fmaf((float)((codes >> (4 * i)) & 15u), s, m));   // c s is exact
+  for (int u = 0; u < 4; ++u) {
+    if (r0 + u * STEP >= n) break;
+    const float s = kv4_scale(meta[u]), m = kv4_min(meta[u]);
+    Vec8<T> y;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) y.set(i, fmaf((float)((codes[u] >> (4 * i)) & 15u), s, m));   // c s is exact
+    y.store(dst + (r0 + u * STEP) * stride);
   }
 }
 
@@ -268,14 +279,14 @@ __global__ void __launch_bounds__(256) kv4_move_kernel(const Kv4EvictArgs a) {
 
 cudaError_t launch_kv4_store(cudaStream_t st, const Kv4View &c, const bf16 *k, const bf16 *v, const Kv4Batch &b, int64_t k_stride,
                              int64_t v_stride) {
-  const dim3 grid((unsigned)(ceil_div(b.rows, STORE_ROWS) * c.heads), b.B, 2);
+  const dim3 grid((unsigned)(ceil_div(b.rows, c.dh == 128 ? STORE_ROWS<128> : STORE_ROWS<64>) * c.heads), b.B, 2);
   if (c.dh == 128) return launch_kernel(kv4_store_kernel<128>, grid, dim3(256), 0, st, c, k, v, b, k_stride, v_stride);
   return launch_kernel(kv4_store_kernel<64>, grid, dim3(256), 0, st, c, k, v, b, k_stride, v_stride);
 }
 
 cudaError_t launch_kv4_load(cudaStream_t st, const Kv4View &c, int dtype, void *k, void *v, const Kv4Batch &b, int64_t k_stride,
                             int64_t v_stride) {
-  const dim3 grid((unsigned)(ceil_div(b.rows, STORE_ROWS) * c.heads), b.B, 2);
+  const dim3 grid((unsigned)(ceil_div(b.rows, c.dh == 128 ? STORE_ROWS<128> : STORE_ROWS<64>) * c.heads), b.B, 2);
   if (dtype == L2PD_BF16) {
     auto fn = c.dh == 128 ? kv4_load_kernel<128, bf16> : kv4_load_kernel<64, bf16>;
     return launch_kernel(fn, grid, dim3(256), 0, st, c, (bf16 *)k, (bf16 *)v, b, k_stride, v_stride);

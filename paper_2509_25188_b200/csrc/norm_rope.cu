@@ -1,7 +1,12 @@
 // Norms of queries and keys for each head, with the rotation by position in the same pass:
 //     y = x g / sqrt(mean(x^2) + eps)        over the dh values of a (row, head)
 //     (y_i, y_{i + dh/2}) turned by the angle position * theta^(-2i/dh)
-// in fp32 between the load and the one rounding at the store.
+// in fp32 between the load and the one rounding at the store; the angle is reduced in 64 bits, so that far positions keep their phase.
+//
+// Bound by memory: every value is read and written once.  A block takes R rows: their sines and cosines (R dh/2 of them, for all
+// heads) go to shared memory while the first rows are on their way.  A thread holds eight values of a head's first half and the
+// eight they are paired with, dh / 16 threads a head, so that the sum of squares needs log2(dh / 16) shuffles; four such items are
+// loaded before the first is worked on.
 #include "kv4.cuh"
 
 namespace l2pd {
@@ -12,7 +17,90 @@ constexpr int MAX_HALF = 128;   // dh <= 256
 
 struct Freq { double f[MAX_HALF]; };   // turns (angle / 2 pi) of pair i per position
 
-// One warp per (row, head); a lane holds the pairs lane, lane + 32, ...
+constexpr int ITEMS = 4, TABLE = 1024;   // items in flight of a thread; (cos, sin) pairs in shared memory
+
+__device__ __forceinline__ float2 turn(double pos, double turns_per_position) {
+  double t = pos * turns_per_position;
+  t -= rint(t);
+  float2 cs;
+  sincospif(2.f * (float)t, &cs.y, &cs.x);
+  return cs;
+}
+
+// L = dh / 16 threads a head, a power of two
+template <typename T>
+__global__ void __launch_bounds__(256) qk_norm_rope_vec_kernel(const NormRopeArgs p, const __grid_constant__ Freq freq, int R, int L) {
+  __shared__ float4 table[TABLE / 2];        // row r, pairs 8 c + 2 q, + 1 at [(r * 4 + q) * L + c]: no bank conflicts over c
+  const int heads = p.Hq + p.Hk, half = p.dh >> 1, row0 = blockIdx.x * R, rows = min(R, p.rows - row0), per_row = heads * L;
+  const int n = rows * per_row, c = threadIdx.x & (L - 1);
+  grid_dep_launch();
+  grid_dep_wait();
+  for (int base = 0; base < n; base += 256 * ITEMS) {
+    Vec8<T> lo[ITEMS], hi[ITEMS];
+    int r[ITEMS], h[ITEMS];
+#pragma unroll
+    for (int u = 0; u < ITEMS; ++u) {
+      const int it = base + u * 256 + threadIdx.x;
+      r[u] = it / per_row;
+      h[u] = (it - r[u] * per_row) / L;
+      if (it < n) {
+        const bool is_k = h[u] >= p.Hq;
+        const T *x = is_k ? (const T *)p.k + (row0 + r[u]) * p.k_stride + (int64_t)(h[u] - p.Hq) * p.dh
+                          : (const T *)p.q + (row0 + r[u]) * p.q_stride + (int64_t)h[u] * p.dh;
+        lo[u].load(x + 8 * c);
+        hi[u].load(x + 8 * c + half);
+      } else {
+        r[u] = -1;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) { lo[u].set(i, 0.f); hi[u].set(i, 0.f); }
+      }
+    }
+    if (base == 0) {
+      for (int i = threadIdx.x; i < rows * half; i += 256) {
+        const int tr = i / half, k = i - tr * half;
+        const int64_t pos = p.positions ? p.positions[row0 + tr] : row0 + tr;
+        reinterpret_cast<float2 *>(table)[2 * ((tr * 4 + ((k >> 1) & 3)) * L + (k >> 3)) + (k & 1)] = turn((double)pos, freq.f[k]);
+      }
+      __syncthreads();
+    }
+#pragma unroll
+    for (int u = 0; u < ITEMS; ++u) {
+      float ss = 0.f;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) ss = fmaf(lo[u].get(i), lo[u].get(i), fmaf(hi[u].get(i), hi[u].get(i), ss));
+      for (int o = L >> 1; o; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
+      if (r[u] < 0) continue;
+      const bool is_k = h[u] >= p.Hq;
+      const float *g = is_k ? p.k_gain : p.q_gain;
+      const float norm = g ? rsqrtf(ss / p.dh + p.eps) : 1.f;
+      float ga[8], gb[8];
+#pragma unroll
+      for (int i = 0; i < 8; i += 4) {
+        const float4 one = make_float4(1.f, 1.f, 1.f, 1.f);
+        *reinterpret_cast<float4 *>(ga + i) = g ? *reinterpret_cast<const float4 *>(g + 8 * c + i) : one;
+        *reinterpret_cast<float4 *>(gb + i) = g ? *reinterpret_cast<const float4 *>(g + 8 * c + half + i) : one;
+      }
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const float4 cs = table[(r[u] * 4 + q) * L + c];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const int i = 2 * q + e;
+          const float co = e ? cs.z : cs.x, si = e ? cs.w : cs.y;
+          const float a = lo[u].get(i) * norm * ga[i], b = hi[u].get(i) * norm * gb[i];
+          lo[u].set(i, a * co - b * si);
+          hi[u].set(i, b * co + a * si);
+        }
+      }
+      T *y = is_k ? (T *)p.k_out + (row0 + r[u]) * p.ko_stride + (int64_t)(h[u] - p.Hq) * p.dh
+                  : (T *)p.q_out + (row0 + r[u]) * p.qo_stride + (int64_t)h[u] * p.dh;
+      lo[u].store(y + 8 * c);
+      hi[u].store(y + 8 * c + half);
+    }
+  }
+}
+
+// Any even head size and alignment.  One warp per (row, head); a lane holds the pairs lane, lane + 32, ...
 template <typename T>
 __global__ void __launch_bounds__(256) qk_norm_rope_kernel(const NormRopeArgs p, const __grid_constant__ Freq freq) {
   grid_dep_launch();
@@ -44,12 +132,9 @@ __global__ void __launch_bounds__(256) qk_norm_rope_kernel(const NormRopeArgs p,
       const int i = lane + 32 * u;
       if (i < half) {
         const float ya = a[u] * r * (g ? g[i] : 1.f), yb = b[u] * r * (g ? g[i + half] : 1.f);
-        double turns = pos * freq.f[i];
-        turns -= rint(turns);
-        float s, c;
-        sincospif(2.f * (float)turns, &s, &c);
-        y[i] = from_f32<T>(ya * c - yb * s);
-        y[i + half] = from_f32<T>(yb * c + ya * s);
+        const float2 cs = turn(pos, freq.f[i]);
+        y[i] = from_f32<T>(ya * cs.x - yb * cs.y);
+        y[i + half] = from_f32<T>(yb * cs.x + ya * cs.y);
       }
     }
   }
@@ -61,8 +146,20 @@ template <typename T>
 cudaError_t launch_qk_norm_rope(cudaStream_t st, const NormRopeArgs &a, int sms) {
   Freq f;
   const int half = a.dh / 2;
-  for (int i = 0; i < half; ++i) f.f[i] = exp(-log((double)a.theta) * i / half) / 6.283185307179586476925286766559;
-  const int64_t blocks = ceil_div64((int64_t)a.rows * (a.Hq + a.Hk), 8);
+  // theta^(-i / half) by repeated products in long double: 128 of them are off by 2^-57
+  const long double step = expl(-logl((long double)a.theta) / half);
+  long double x = 1.0L / 6.283185307179586476925286766559L;
+  for (int i = 0; i < half; ++i, x *= step) f.f[i] = (double)x;
+  const int L = a.dh / 16, heads = a.Hq + a.Hk;
+  if (a.vec && (L & (L - 1)) == 0) {
+    // rows of a block: four items a thread, but no fewer than two blocks an SM
+    const int64_t fill = (int64_t)ITEMS * 256 / ((int64_t)heads * L), share = a.rows / (2 * sms);
+    int64_t R = fill < share ? fill : share;
+    if (R > TABLE / half) R = TABLE / half;
+    if (R < 1) R = 1;
+    return launch_kernel(qk_norm_rope_vec_kernel<T>, dim3((unsigned)ceil_div64(a.rows, R)), dim3(256), 0, st, a, f, (int)R, L);
+  }
+  const int64_t blocks = ceil_div64((int64_t)a.rows * heads, 8);
   const int grid = (int)(blocks < (int64_t)sms * 8 ? blocks : (int64_t)sms * 8);
   return launch_kernel(qk_norm_rope_kernel<T>, dim3(grid), dim3(256), 0, st, a, f);
 }
