@@ -13,7 +13,8 @@
 //
 // Work: the key tiles of all (sequence, head, chunk of columns) stand in one line and every CTA takes an equal run of it; a run
 // that starts or ends inside an item leaves a partial result, joined in the order of the tiles by a second kernel.  A warp takes
-// every eighth tile of its CTA's run, through a ring of its own.
+// every fourth tile of its CTA's run, through a ring of its own; the CTA's second half of an SM computes while the first one
+// fetches queries or brings its warps' sums together.
 #include <cuda_fp16.h>
 #include <math.h>
 
@@ -24,25 +25,60 @@ namespace l2pd {
 
 namespace {
 
-constexpr int WARPS = 8, STAGES = 3;
+using ptx::F2;
+
+constexpr int WARPS = 4, CTAS_PER_SM = 2;
 constexpr float LAZY = 6.0f;         // log2 units the running maximum may pass the reference
 
 // ---- the line of work --------------------------------------------------------------------------------------------------
-// Items: for sequence b, key heads times chunks of CH columns (those that have rows), tiles_b key tiles each.
+// Items: for sequence b, key heads times chunks of `chunk` columns (those that have rows), tiles_b key tiles each.
 struct Line {
   int B, H, chunk, group, slots, max_keys;
   Kv4Batch b;
   __device__ __forceinline__ int keys(int s) const { return b.slot(s, slots) < 0 ? 0 : max(0, min(b.keys[s], max_keys)); }
   __device__ __forceinline__ int chunks(int s) const { return (b.n_rows(s) * group + chunk - 1) / chunk; }
   __device__ __forceinline__ int tiles(int s) const { return (keys(s) + KV4_TILE - 1) / KV4_TILE; }
-  __device__ __forceinline__ int64_t all_tiles(int s) const { return (int64_t)H * chunks(s) * tiles(s); }
-  // tiles of the sequences [0, s), every lane of the warp receives it (whole warp)
+  __device__ __forceinline__ int64_t all_tiles(int s) const { return s < B ? (int64_t)H * chunks(s) * tiles(s) : 0; }
+  // tiles of the sequences [0, s), the same answer in every lane (whole warp)
   __device__ int64_t before(int s) const {
     int64_t x = 0;
     for (int i = threadIdx.x & 31; i < s; i += 32) x += all_tiles(i);
 #pragma unroll
     for (int o = 16; o; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
     return x;
+  }
+  // sequence that tile `pos` of the line belongs to, and the tiles before it (whole warp; pos below the line's end)
+  __device__ int find(int64_t pos, int64_t *start) const {
+    const int lane = threadIdx.x & 31;
+    int64_t run = 0;
+    for (int s0 = 0;; s0 += 32) {
+      const int64_t own = all_tiles(s0 + lane);
+      int64_t x = own;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int64_t y = __shfl_up_sync(0xffffffffu, x, o);
+        if (lane >= o) x += y;
+      }
+      const unsigned here = __ballot_sync(0xffffffffu, pos < run + x);
+      if (here || s0 + 32 >= B) {
+        const int l = here ? __ffs(here) - 1 : 31;
+        *start = run + __shfl_sync(0xffffffffu, x - own, l);
+        return min(s0 + l, B - 1);
+      }
+      run += __shfl_sync(0xffffffffu, x, 31);
+    }
+  }
+  // Tiles of a CTA's run.  Sequences of one length: whole items where that costs the longest run no more than a fifth, since a
+  // split item's halves go through memory (8 x 32 heads of 2048 keys on 296 CTAs: 32 tiles instead of 28).
+  __device__ int64_t share(int64_t total, int ctas) const {
+    const int64_t even = (total + ctas - 1) / ctas;
+    const int nt = tiles(0);
+    int64_t items = nt ? total / nt : 0;
+    bool same = true;
+    for (int i = threadIdx.x & 31; i < B; i += 32) same = same && (tiles(i) == nt || chunks(i) == 0);
+    if (!__all_sync(0xffffffffu, same)) return even;
+    const int64_t whole = (items + ctas - 1) / ctas * nt;
+    return whole * 5 <= even * 6 ? whole : even;
   }
 };
 
@@ -68,82 +104,101 @@ __device__ __forceinline__ void spread(uint32_t w, uint32_t *r) {
   r[2] = w & 0x000f000fu; r[3] = w & 0x00f000f0u;
 }
 
-// tile row of MMA row k (0..7): odd and even rows change places in every other pair, see kv4.cuh on banks
+// tile row of MMA row k (0..7): in every other pair the two change places, so that the four keys whose V rows a warp reads at
+// once lie in different banks
 __device__ __forceinline__ int tile_row(int k) { return k ^ ((k >> 1) & 1); }
 
-// Queries of eight columns as B fragments: lane (g, t) holds of column g the dimensions [t dh/4, (t + 1) dh/4).
-// csum: sum of the column's scaled queries in the scale of the codes' products, cf: what turns those into log2 scores.
-template <int DH>
-__device__ __forceinline__ void load_queries(const bf16 *q, bool there, float scale_log2, uint32_t (&f)[DH / 8], float &cf, float &csum) {
-  constexpr int W = DH / 32;                       // words of codes a lane holds: 8 dimensions each
+// ---- queries as B fragments --------------------------------------------------------------------------------------------
+// Eight columns: lane (g, t) holds of column g the dimensions [t dh/4, (t + 1) dh/4).
+template <int DH> struct Queries {
   uint32_t raw[DH / 8];
+  uint32_t top;                                    // the column's largest magnitude, as bits; non-finite ones above all
+  __device__ __forceinline__ void load(const bf16 *q, bool there) {
 #pragma unroll
-  for (int j = 0; j < W; ++j) {
-    const uint4 x = there ? *reinterpret_cast<const uint4 *>(q + 8 * j) : make_uint4(0, 0, 0, 0);
-    raw[4 * j] = x.x; raw[4 * j + 1] = x.y; raw[4 * j + 2] = x.z; raw[4 * j + 3] = x.w;
-  }
-  uint32_t top = 0;                                // largest magnitude, as bits: infinities and NaN above all
-  float x[DH / 4];
+    for (int j = 0; j < DH / 32; ++j) {
+      const uint4 x = there ? *reinterpret_cast<const uint4 *>(q + 8 * j) : make_uint4(0, 0, 0, 0);
+      raw[4 * j] = x.x; raw[4 * j + 1] = x.y; raw[4 * j + 2] = x.z; raw[4 * j + 3] = x.w;
+    }
+    top = 0;
 #pragma unroll
-  for (int i = 0; i < DH / 8; ++i) {
-    x[2 * i] = __uint_as_float(raw[i] << 16); x[2 * i + 1] = __uint_as_float(raw[i] & 0xffff0000u);
-    top = max(top, max(__float_as_uint(x[2 * i]) & 0x7fffffffu, __float_as_uint(x[2 * i + 1]) & 0x7fffffffu));
+    for (int i = 0; i < DH / 8; ++i) top = max(top, max(raw[i] << 16 & 0x7fffffffu, raw[i] & 0x7fff0000u));
+    top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+    top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
   }
-  top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
-  top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
-  // the largest becomes 2^14 .. 2^15
-  const int e = (int)(top >> 23) - 127;
-  const float up = __uint_as_float((uint32_t)(127 + min(14 - e, 126)) << 23);
-  cf = scale_log2 * 1024.f * __uint_as_float((uint32_t)(127 - min(14 - e, 126) + 14) << 23);   // 2^24 / up
-  if (e == 128) cf = __uint_as_float(0x7fc00000u);   // infinity or NaN among the queries: the column is NaN
-  csum = 0.f;
+  __device__ __forceinline__ bool finite() const { return top < 0x7f800000u; }
+  // Scaled by 2^u to fp16.  Returns the column's sum in the scale of the products with codes; NaN: a column that holds an
+  // infinity or NaN, whose scores are all NaN.
+  __device__ __forceinline__ float convert(int u, uint32_t (&f)[DH / 8]) const {
+    const float up = __uint_as_float((uint32_t)(127 + u) << 23);
+    float sum = 0.f;
 #pragma unroll
-  for (int i = 0; i < DH / 4; ++i) {
-    x[i] = e == 128 ? 0.f : x[i] * up;
-    csum += x[i];
-  }
-  csum += __shfl_xor_sync(0xffffffffu, csum, 1);
-  csum += __shfl_xor_sync(0xffffffffu, csum, 2);
-  csum *= __uint_as_float((127 - 24) << 23);
+    for (int j = 0; j < DH / 32; ++j) {
+      float y[8];
 #pragma unroll
-  for (int j = 0; j < W; ++j) {
-    const float *y = x + 8 * j;
-    auto pair = [](float a, float b) { __half2 h = __floats2half2_rn(a, b); return *reinterpret_cast<uint32_t *>(&h); };
-    f[4 * j] = pair(y[0], y[4]); f[4 * j + 1] = pair(y[1] * 0.0625f, y[5] * 0.0625f);
-    f[4 * j + 2] = pair(y[2], y[6]); f[4 * j + 3] = pair(y[3] * 0.0625f, y[7] * 0.0625f);
+      for (int i = 0; i < 4; ++i) {
+        const uint32_t w = finite() ? raw[4 * j + i] : 0u;
+        y[2 * i] = __uint_as_float(w << 16) * up; y[2 * i + 1] = __uint_as_float(w & 0xffff0000u) * up;
+        sum += y[2 * i] + y[2 * i + 1];
+      }
+      auto pair = [](float a, float b) { __half2 h = __floats2half2_rn(a, b); return *reinterpret_cast<uint32_t *>(&h); };
+      f[4 * j] = pair(y[0], y[4]); f[4 * j + 1] = pair(y[1] * 0.0625f, y[5] * 0.0625f);
+      f[4 * j + 2] = pair(y[2], y[6]); f[4 * j + 3] = pair(y[3] * 0.0625f, y[7] * 0.0625f);
+    }
+    sum += __shfl_xor_sync(0xffffffffu, sum, 1);
+    sum += __shfl_xor_sync(0xffffffffu, sum, 2);
+    return finite() ? sum * __uint_as_float((127 - 24) << 23) : __uint_as_float(0x7fc00000u);
   }
+};
+// Power of two that takes the largest of all columns to 2^14 .. 2^15.  (A column 2^20 below the largest still has 2^-19 of its own
+// magnitude, and scores a millionth of the other's.)  What then turns the products into log2 scores: scale 2^(24 - u).
+__device__ __forceinline__ int query_exponent(uint32_t top) { return min(14 - ((int)(top >> 23) - 127), 126); }
+__device__ __forceinline__ float query_factor(float scale_log2, int u) {
+  return scale_log2 * 1024.f * __uint_as_float((uint32_t)(127 + 14 - u) << 23);
 }
 
+template <int DH, int NT> struct AttnShape {
+  static constexpr int CH = 8 * NT, TILE = KV4_TILE * (DH + 8), STAGES = NT == 1 ? 3 : 2, RING = STAGES * TILE;
+  static constexpr int META = KV4_TILE * 24, QBYTES = NT * DH * 16;
+  static constexpr int OFF_META = WARPS * RING, OFF_Q = OFF_META + WARPS * META, SMEM = OFF_Q + QBYTES;
+};
+
 template <int DH, int NT>
-__global__ void __launch_bounds__(WARPS * 32, 1) attention_kv4_kernel(const AttnParams p) {
-  constexpr int W = DH / 32, MT = DH / 16, CH = 8 * NT, MS = 4 / NT;   // MS: groups of 16 keys taken together
-  constexpr int TILE = KV4_TILE * (DH + 8), RING = STAGES * TILE, LDO = DH + 4;
+__global__ void __launch_bounds__(WARPS * 32, CTAS_PER_SM) attention_kv4_kernel(const AttnParams p) {
+  using Sh = AttnShape<DH, NT>;
+  constexpr int W = DH / 32, MT = DH / 16, CH = Sh::CH, MS = 4 / NT;   // MS: groups of 16 keys taken together
+  constexpr int TILE = Sh::TILE, RING = Sh::RING, STAGES = Sh::STAGES, LDO = DH + 4;
   static_assert(CH * LDO * 4 <= RING, "a warp's output goes to its ring");
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ __align__(8) uint64_t bars[WARPS * STAGES];
-  __shared__ float fin[WARPS][3][CH];              // reference, sum of probabilities, sum of probability times m
+  __shared__ float fin[WARPS][2][CH];              // reference and sum of probabilities
+  __shared__ float qsum[CH];
+  __shared__ uint32_t qtop[WARPS];
   __shared__ int abort_flag;
   const int warp = ptx::warp_index(), lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   const uint32_t bar0 = ptx::smem_u32(&bars[warp * STAGES]);
   uint8_t *const ring = smem + warp * RING;
   const uint32_t ring_u = ptx::smem_u32(ring);
-  if (lane == 0)
+  float4 *const meta_a = reinterpret_cast<float4 *>(smem + Sh::OFF_META + warp * Sh::META);   // by key: cf s, cf m of K, e - E, 2^(E - e)
+  float2 *const meta_b = reinterpret_cast<float2 *>(meta_a + KV4_TILE);                        // s 2^-e, m 2^-e of V
+  uint4 *const qs = reinterpret_cast<uint4 *>(smem + Sh::OFF_Q);
+  if (lane == 0) {
     for (int i = 0; i < STAGES; ++i) ptx::mbar_init(bar0 + 8 * i, 1);
+    ptx::fence_barrier_init();
+    ptx::fence_proxy_async();
+  }
   if (threadIdx.x == 0) abort_flag = 0;
-  if (lane == 0) { ptx::fence_barrier_init(); ptx::fence_proxy_async(); }
   __syncthreads();
   grid_dep_launch();
   grid_dep_wait();
 
   const Line &ln = p.line;
-  const int64_t total = ln.before(ln.B), share = (total + gridDim.x - 1) / gridDim.x;
+  const int64_t total = ln.before(ln.B), share = ln.share(total, gridDim.x);
   int64_t pos = share * blockIdx.x;
   const int64_t end = min(total, pos + share);
   uint32_t used = 0;                               // tiles this warp has taken: stage and parity
-  int b = -1;
-  int64_t b_start = 0, b_tiles = 0;
   while (pos < end) {
-    while (b < 0 || pos >= b_start + b_tiles) { b_start += b_tiles; ++b; b_tiles = ln.all_tiles(b); }
+    int64_t b_start;
+    const int b = ln.find(pos, &b_start);
     const int n_keys = ln.keys(b), nt = ln.tiles(b), nc = ln.chunks(b), rows = ln.b.n_rows(b), row0 = ln.b.row0(b);
     const int64_t in_b = pos - b_start;
     const int item = (int)(in_b / nt), t0 = (int)(in_b - (int64_t)item * nt), t1 = (int)min((int64_t)nt, t0 + (end - pos));
@@ -162,41 +217,84 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attention_kv4_kernel(const Attn
     };
     for (int i = 0; i < STAGES; ++i) request(i);
 
-    uint32_t qf[NT][DH / 8];
-    float cfa[NT], cfb[NT], za[NT], zb[NT];        // of the columns 2t and 2t + 1 of each eight
-#pragma unroll
-    for (int n = 0; n < NT; ++n) {
-      const int col = c0 + 8 * n + g, r = col / ln.group;
-      const bool there = 8 * n + g < cols;
-      float cf, cs;
-      load_queries<DH>(p.q + (int64_t)(row0 + r) * p.q_stride + (int64_t)(h * ln.group + col - r * ln.group) * DH + t * (DH / 4), there,
-                       p.scale_log2, qf[n], cf, cs);
-      cs *= cf;
-      cfa[n] = __shfl_sync(0xffffffffu, cf, 8 * t); cfb[n] = __shfl_sync(0xffffffffu, cf, 8 * t + 4);
-      za[n] = __shfl_sync(0xffffffffu, cs, 8 * t); zb[n] = __shfl_sync(0xffffffffu, cs, 8 * t + 4);
+    // queries: warp n converts the columns 8 n .. 8 n + 7 for all
+    Queries<DH> qn;
+    qn.top = 0;
+    if (warp < NT) {
+      const int col = c0 + 8 * warp + g, r = col / ln.group;
+      qn.load(p.q + (int64_t)(row0 + r) * p.q_stride + (int64_t)(h * ln.group + col - r * ln.group) * DH + t * (DH / 4), 8 * warp + g < cols);
     }
-    float o[MT][NT][4], la[NT], lb[NT], wa[NT], wb[NT], ma[NT], mb[NT];
+    const uint32_t top = __reduce_max_sync(0xffffffffu, qn.finite() ? qn.top : 0u);
+    if (lane == 0) qtop[warp] = top;
+    __syncthreads();
+    const int u = query_exponent(max(max(qtop[0], qtop[1]), max(qtop[2], qtop[3])));
+    const float cf = query_factor(p.scale_log2, u);
+    if (warp < NT) {
+      uint32_t f[DH / 8];
+      const float cs = qn.convert(u, f);
+      if (t == 0) qsum[8 * warp + g] = cs;
+#pragma unroll
+      for (int j = 0; j < W; ++j) qs[(warp * W + j) * 32 + lane] = make_uint4(f[4 * j], f[4 * j + 1], f[4 * j + 2], f[4 * j + 3]);
+    }
+    __syncthreads();
+    uint32_t qf[NT][DH / 8];
+    F2 cs[NT];                                     // columns 2t and 2t + 1 of each eight
+    F2 neg_m[NT], l[NT], wm[NT];                   // minus the reference, sum of probabilities, sum of probability times m
+    float o[MT][NT][4];
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
-      la[n] = lb[n] = wa[n] = wb[n] = 0.f; ma[n] = mb[n] = -INFINITY;
+#pragma unroll
+      for (int j = 0; j < W; ++j) *reinterpret_cast<uint4 *>(&qf[n][4 * j]) = qs[(n * W + j) * 32 + lane];
+      cs[n] = ptx::f2(qsum[8 * n + 2 * t], qsum[8 * n + 2 * t + 1]);
+      neg_m[n] = l[n] = wm[n] = ptx::f2(0.f, 0.f);
 #pragma unroll
       for (int m = 0; m < MT; ++m) o[m][n][0] = o[m][n][1] = o[m][n][2] = o[m][n][3] = 0.f;
     }
     int e0 = -1000;                                // E
-    bool ok = true;
+    bool ok = true, first = true;
     for (int i = 0; i < mine; ++i) {
       const uint32_t s = (used + i) % STAGES;
       ok = ptx::mbar_wait_warp(bar0 + 8 * s, ((used + i) / STAGES) & 1u);
       if (!ok) break;
       const uint8_t *tile = ring + s * TILE;
       const int left = n_keys - (t0 + warp + i * WARPS) * KV4_TILE;    // keys of this tile, or more
+      // what belongs to a key, once for all columns; keys behind the end get weight 0
+      {
+        uint32_t km[2], vm[2];
+        int ex[2];
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          const int k = lane + 32 * x;
+          const bool real = k < left;
+          km[x] = real ? *reinterpret_cast<const uint32_t *>(tile + kv4_off_kmeta(DH) + 4 * k) : 0u;
+          vm[x] = real ? *reinterpret_cast<const uint32_t *>(tile + kv4_off_vmeta(DH) + 4 * k) : 0u;
+          ex[x] = min(max((int)((vm[x] >> 7) & 255u), (int)((vm[x] >> 23) & 255u) - 4) - 126, 100);
+        }
+        const int ex_top = __reduce_max_sync(0xffffffffu, max(ex[0], ex[1]));
+        if (ex_top > e0) {                         // rare: what came before is in units of 2^e0
+          const int was = e0;
+          e0 = max(ex_top, -100) + 2;
+          const float f = __uint_as_float((uint32_t)max(127 - (e0 - was), 0) << 23);
+#pragma unroll
+          for (int n = 0; n < NT; ++n) {
+            wm[n] = ptx::mul2(wm[n], ptx::f2(f, f));
+#pragma unroll
+            for (int m = 0; m < MT; ++m) { o[m][n][0] *= f; o[m][n][1] *= f; o[m][n][2] *= f; o[m][n][3] *= f; }
+          }
+        }
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          const int k = lane + 32 * x, e = max(ex[x], e0 - 60);
+          const float w = __uint_as_float((uint32_t)(127 - e) << 23);
+          meta_a[k] = make_float4(kv4_scale(km[x]) * cf, kv4_min(km[x]) * cf, k < left ? (float)(e - e0) : -INFINITY,
+                                  __uint_as_float((uint32_t)(127 - e + e0) << 23));
+          meta_b[k] = make_float2(kv4_scale(vm[x]) * w, kv4_min(vm[x]) * w);
+        }
+        __syncwarp();
+      }
 #pragma unroll 1
       for (int s0 = 0; s0 < 4; s0 += MS) {
         float acc[MS][NT][4];
-#pragma unroll
-        for (int u = 0; u < MS; ++u)
-#pragma unroll
-          for (int n = 0; n < NT; ++n) acc[u][n][0] = acc[u][n][1] = acc[u][n][2] = acc[u][n][3] = 0.f;
         const int kr = 16 * s0 + tile_row(g);
         uint32_t ka[MS][W], kb[MS][W];
 #pragma unroll
@@ -218,106 +316,78 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attention_kv4_kernel(const Attn
             spread(ka[u][j], x); spread(kb[u][j], y);
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
-              ptx::mma_f16_16x8x16(acc[u][n], x[0], y[0], x[1], y[1], qf[n][4 * j], qf[n][4 * j + 1]);
+              if (j == 0) ptx::mma_f16_16x8x16_first(acc[u][n], x[0], y[0], x[1], y[1], qf[n][0], qf[n][1]);
+              else ptx::mma_f16_16x8x16(acc[u][n], x[0], y[0], x[1], y[1], qf[n][4 * j], qf[n][4 * j + 1]);
               ptx::mma_f16_16x8x16(acc[u][n], x[2], y[2], x[3], y[3], qf[n][4 * j + 2], qf[n][4 * j + 3]);
             }
           }
-        // what belongs to a key: s and m of K; of V the exponent e, 2^-e, s 2^-e and m 2^-e
-        float vs[MS][2], vm[MS][2], vw[MS][2];
-        uint32_t vmeta[MS][2];
-        int ex[MS][2], ex_top = -126;
+        // scores against the reference
+        float top = -INFINITY;
 #pragma unroll
         for (int u = 0; u < MS; ++u)
 #pragma unroll
-          for (int e2 = 0; e2 < 2; ++e2) {
-            const int k = kr + 16 * u + 8 * e2;
-            vmeta[u][e2] = k < left ? *reinterpret_cast<const uint32_t *>(tile + kv4_off_vmeta(DH) + 4 * k) : 0u;
-            ex[u][e2] = min(max((int)((vmeta[u][e2] >> 7) & 255u), (int)((vmeta[u][e2] >> 23) & 255u) - 4) - 126, 100);
-            ex_top = max(ex_top, ex[u][e2]);
-          }
-        ex_top = __reduce_max_sync(0xffffffffu, ex_top);
-        if (ex_top > e0) {                         // rare: what came before is in units of 2^e0
-          const int up = e0;
-          e0 = max(ex_top, -100) + 2;
-          const float f = __uint_as_float((uint32_t)max(127 - (e0 - up), 0) << 23);
-#pragma unroll
-          for (int n = 0; n < NT; ++n) {
-            wa[n] *= f; wb[n] *= f;
-#pragma unroll
-            for (int m = 0; m < MT; ++m) { o[m][n][0] *= f; o[m][n][1] *= f; o[m][n][2] *= f; o[m][n][3] *= f; }
-          }
-        }
-#pragma unroll
-        for (int u = 0; u < MS; ++u)
-#pragma unroll
-          for (int e2 = 0; e2 < 2; ++e2) {
-            const int k = kr + 16 * u + 8 * e2;
-            const bool real = k < left;
-            const uint32_t km = real ? *reinterpret_cast<const uint32_t *>(tile + kv4_off_kmeta(DH) + 4 * k) : 0u;
-            const int e = max(ex[u][e2], e0 - 60);
-            const float w = __uint_as_float((uint32_t)(127 - e) << 23), bias = real ? (float)(e - e0) : -INFINITY;
-            vw[u][e2] = __uint_as_float((uint32_t)(127 - e + e0) << 23); vs[u][e2] = kv4_scale(vmeta[u][e2]) * w; vm[u][e2] = kv4_min(vmeta[u][e2]) * w;
-            const float ks = kv4_scale(km), kmin = kv4_min(km);
+          for (int e = 0; e < 2; ++e) {
+            const float4 k = meta_a[kr + 16 * u + 8 * e];
+            const F2 ks = ptx::f2(k.x, k.x), km = ptx::f2(k.y, k.y), bias = ptx::f2(k.z, k.z);
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
-              float &ta = acc[u][n][2 * e2], &tb = acc[u][n][2 * e2 + 1];
-              ta = fmaf(ta * cfa[n], ks, fmaf(kmin, za[n], bias)) - (ma[n] == -INFINITY ? 0.f : ma[n]);
-              tb = fmaf(tb * cfb[n], ks, fmaf(kmin, zb[n], bias)) - (mb[n] == -INFINITY ? 0.f : mb[n]);
+              float *x = &acc[u][n][2 * e];
+              const F2 y = ptx::fma2(ptx::f2(x[0], x[1]), ks, ptx::add2(ptx::fma2(km, cs[n], bias), neg_m[n]));
+              x[0] = ptx::f2_lo(y); x[1] = ptx::f2_hi(y);
+              top = fmaxf(top, fmaxf(x[0], x[1]));
             }
           }
-        // a new reference where the maximum has passed the old one by LAZY (or there was none)
-        bool grow = false;
-        float xa[NT], xb[NT];
-#pragma unroll
-        for (int n = 0; n < NT; ++n) {
-          xa[n] = xb[n] = -INFINITY;
-#pragma unroll
-          for (int u = 0; u < MS; ++u) {
-            xa[n] = fmaxf(xa[n], fmaxf(acc[u][n][0], acc[u][n][2]));
-            xb[n] = fmaxf(xb[n], fmaxf(acc[u][n][1], acc[u][n][3]));
-          }
-          grow = grow || xa[n] > LAZY || xb[n] > LAZY || (ma[n] == -INFINITY && xa[n] > -INFINITY) || (mb[n] == -INFINITY && xb[n] > -INFINITY);
-        }
-        if (__any_sync(0xffffffffu, grow)) {
+        // a new reference where the maximum has passed the old one by LAZY, and at the start
+        if (__any_sync(0xffffffffu, first || top > LAZY)) {
 #pragma unroll
           for (int n = 0; n < NT; ++n) {
+            float xa = -INFINITY, xb = -INFINITY;
+#pragma unroll
+            for (int u = 0; u < MS; ++u) {
+              xa = fmaxf(xa, fmaxf(acc[u][n][0], acc[u][n][2]));
+              xb = fmaxf(xb, fmaxf(acc[u][n][1], acc[u][n][3]));
+            }
 #pragma unroll
             for (int x = 4; x < 32; x <<= 1) {
-              xa[n] = fmaxf(xa[n], __shfl_xor_sync(0xffffffffu, xa[n], x));
-              xb[n] = fmaxf(xb[n], __shfl_xor_sync(0xffffffffu, xb[n], x));
+              xa = fmaxf(xa, __shfl_xor_sync(0xffffffffu, xa, x));
+              xb = fmaxf(xb, __shfl_xor_sync(0xffffffffu, xb, x));
             }
-            const bool fa = ma[n] == -INFINITY, fb = mb[n] == -INFINITY;   // no key yet
-            const float da = fa ? (xa[n] == -INFINITY ? 0.f : xa[n]) : fmaxf(xa[n], 0.f), db = fb ? (xb[n] == -INFINITY ? 0.f : xb[n]) : fmaxf(xb[n], 0.f);
-            const float sa = fa ? 0.f : ptx::ex2(-da), sb = fb ? 0.f : ptx::ex2(-db);
-            ma[n] = fa ? (xa[n] == -INFINITY ? -INFINITY : xa[n]) : ma[n] + da;
-            mb[n] = fb ? (xb[n] == -INFINITY ? -INFINITY : xb[n]) : mb[n] + db;
-            la[n] *= sa; lb[n] *= sb; wa[n] *= sa; wb[n] *= sb;
+            const float da = first ? (xa == -INFINITY ? 0.f : xa) : fmaxf(xa, 0.f), db = first ? (xb == -INFINITY ? 0.f : xb) : fmaxf(xb, 0.f);
+            const float sa = first ? 0.f : ptx::ex2(-da), sb = first ? 0.f : ptx::ex2(-db);
+            const F2 d = ptx::f2(-da, -db), sc = ptx::f2(sa, sb);
+            neg_m[n] = ptx::add2(neg_m[n], d);
+            l[n] = ptx::mul2(l[n], sc); wm[n] = ptx::mul2(wm[n], sc);
 #pragma unroll
             for (int m = 0; m < MT; ++m) { o[m][n][0] *= sa; o[m][n][2] *= sa; o[m][n][1] *= sb; o[m][n][3] *= sb; }
 #pragma unroll
             for (int u = 0; u < MS; ++u) { acc[u][n][0] -= da; acc[u][n][2] -= da; acc[u][n][1] -= db; acc[u][n][3] -= db; }
           }
+          first = false;
         }
 #pragma unroll
         for (int u = 0; u < MS; ++u) {
           uint32_t pf[NT][2];
 #pragma unroll
-          for (int n = 0; n < NT; ++n)
+          for (int e = 0; e < 2; ++e) {
+            const float w = meta_a[kr + 16 * u + 8 * e].w;
+            const float2 v = meta_b[kr + 16 * u + 8 * e];
+            const F2 vw = ptx::f2(w, w), vs = ptx::f2(v.x, v.x), vm = ptx::f2(v.y, v.y);
 #pragma unroll
-            for (int e2 = 0; e2 < 2; ++e2) {
-              const float pa = ptx::ex2(acc[u][n][2 * e2]), pb = ptx::ex2(acc[u][n][2 * e2 + 1]);
-              la[n] = fmaf(pa, vw[u][e2], la[n]); lb[n] = fmaf(pb, vw[u][e2], lb[n]);
-              wa[n] = fmaf(pa, vm[u][e2], wa[n]); wb[n] = fmaf(pb, vm[u][e2], wb[n]);
-              __half2 hp = __floats2half2_rn(pa * vs[u][e2], pb * vs[u][e2]);
-              pf[n][e2] = ptx::transpose_8x8(*reinterpret_cast<uint32_t *>(&hp));
+            for (int n = 0; n < NT; ++n) {
+              const F2 pr = ptx::f2(ptx::ex2(acc[u][n][2 * e]), ptx::ex2(acc[u][n][2 * e + 1]));
+              l[n] = ptx::fma2(pr, vw, l[n]);
+              wm[n] = ptx::fma2(pr, vm, wm[n]);
+              const F2 ps = ptx::mul2(pr, vs);
+              __half2 hp = __floats2half2_rn(ptx::f2_lo(ps), ptx::f2_hi(ps));
+              pf[n][e] = ptx::transpose_8x8(*reinterpret_cast<uint32_t *>(&hp));
             }
+          }
           // values: lane (g, t) holds dimensions [g dh/8, (g + 1) dh/8) of the keys of MMA columns 2t, 2t + 1, 2t + 8, 2t + 9
           constexpr int VW = DH / 64;
           uint32_t va[4][VW];
-          const int vr = 16 * (s0 + u) + tile_row(2 * t), vr1 = 16 * (s0 + u) + tile_row(2 * t + 1);
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            const int r = (e & 1 ? vr1 : vr) + 8 * (e >> 1);
+            const int r = 16 * (s0 + u) + tile_row(2 * t + (e & 1)) + 8 * (e >> 1);
             const uint8_t *a = tile + kv4_off_v(DH) + r * (DH / 2) + ((g * (DH / 16)) ^ kv4_v_swizzle(r, DH));
             if (DH == 128) *reinterpret_cast<uint2 *>(va[e]) = *reinterpret_cast<const uint2 *>(a);
             else va[e][0] = *reinterpret_cast<const uint32_t *>(a);
@@ -347,22 +417,26 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attention_kv4_kernel(const Attn
     // the warps meet: every warp's sums and outputs go to shared memory, each against its own reference
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
+      float la = ptx::f2_lo(l[n]), lb = ptx::f2_hi(l[n]), wa = ptx::f2_lo(wm[n]), wb = ptx::f2_hi(wm[n]);
 #pragma unroll
       for (int x = 4; x < 32; x <<= 1) {
-        la[n] += __shfl_xor_sync(0xffffffffu, la[n], x); lb[n] += __shfl_xor_sync(0xffffffffu, lb[n], x);
-        wa[n] += __shfl_xor_sync(0xffffffffu, wa[n], x); wb[n] += __shfl_xor_sync(0xffffffffu, wb[n], x);
+        la += __shfl_xor_sync(0xffffffffu, la, x); lb += __shfl_xor_sync(0xffffffffu, lb, x);
+        wa += __shfl_xor_sync(0xffffffffu, wa, x); wb += __shfl_xor_sync(0xffffffffu, wb, x);
       }
       if (g == 0) {
-        fin[warp][0][8 * n + 2 * t] = ma[n]; fin[warp][0][8 * n + 2 * t + 1] = mb[n];
-        fin[warp][1][8 * n + 2 * t] = la[n]; fin[warp][1][8 * n + 2 * t + 1] = lb[n];
+        fin[warp][0][8 * n + 2 * t] = mine > 0 ? -ptx::f2_lo(neg_m[n]) : -INFINITY;
+        fin[warp][0][8 * n + 2 * t + 1] = mine > 0 ? -ptx::f2_hi(neg_m[n]) : -INFINITY;
+        fin[warp][1][8 * n + 2 * t] = la; fin[warp][1][8 * n + 2 * t + 1] = lb;
       }
       float *oa = reinterpret_cast<float *>(ring) + (8 * n + 2 * t) * LDO + g * (DH / 8), *ob = oa + LDO;
       constexpr float EVEN = 16777216.f, ODD = 1048576.f;             // the codes' 2^24, and 2^20 where they came 16 times
       const float unit = __uint_as_float((uint32_t)(127 + max(e0, -126)) << 23);
 #pragma unroll
-      for (int m = 0; m < MT; ++m) {
-        *reinterpret_cast<float2 *>(oa + 2 * m) = make_float2(fmaf(o[m][n][0], EVEN, wa[n]) * unit, fmaf(o[m][n][2], ODD, wa[n]) * unit);
-        *reinterpret_cast<float2 *>(ob + 2 * m) = make_float2(fmaf(o[m][n][1], EVEN, wb[n]) * unit, fmaf(o[m][n][3], ODD, wb[n]) * unit);
+      for (int m = 0; m < MT; m += 2) {
+        *reinterpret_cast<float4 *>(oa + 2 * m) = make_float4(fmaf(o[m][n][0], EVEN, wa) * unit, fmaf(o[m][n][2], ODD, wa) * unit,
+                                                              fmaf(o[m + 1][n][0], EVEN, wa) * unit, fmaf(o[m + 1][n][2], ODD, wa) * unit);
+        *reinterpret_cast<float4 *>(ob + 2 * m) = make_float4(fmaf(o[m][n][1], EVEN, wb) * unit, fmaf(o[m][n][3], ODD, wb) * unit,
+                                                              fmaf(o[m + 1][n][1], EVEN, wb) * unit, fmaf(o[m + 1][n][3], ODD, wb) * unit);
       }
     }
     __syncthreads();
@@ -374,93 +448,96 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attention_kv4_kernel(const Attn
       float m = -INFINITY;
 #pragma unroll
       for (int w = 0; w < WARPS; ++w) m = fmaxf(m, fin[w][0][c]);
-      float l = 0.f;
+      float sum = 0.f;
       float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
       for (int w = 0; w < WARPS; ++w) {
         const float mw = fin[w][0][c], f = mw == -INFINITY ? 0.f : ptx::ex2(mw - m);
         const float4 z = *reinterpret_cast<const float4 *>(smem + w * RING + (c * LDO + d) * 4);
-        l = fmaf(fin[w][1][c], f, l);
+        sum = fmaf(fin[w][1][c], f, sum);
         y.x = fmaf(z.x, f, y.x); y.y = fmaf(z.y, f, y.y); y.z = fmaf(z.z, f, y.z); y.w = fmaf(z.w, f, y.w);
       }
       if (whole) {
         const int col = c0 + c, r = col / ln.group, hq = h * ln.group + col - r * ln.group;
-        const float inv = 1.f / l;
+        const float inv = 1.f / sum;
         __nv_bfloat162 y0 = __floats2bfloat162_rn(y.x * inv, y.y * inv), y1 = __floats2bfloat162_rn(y.z * inv, y.w * inv);
-        uint2 pk = make_uint2(*reinterpret_cast<uint32_t *>(&y0), *reinterpret_cast<uint32_t *>(&y1));
-        *reinterpret_cast<uint2 *>(p.out + (int64_t)(row0 + r) * p.out_stride + (int64_t)hq * DH + d) = pk;
-        if (d == 0 && p.lse) p.lse[(int64_t)(row0 + r) * p.Hq + hq] = (m + log2f(l)) * 0.6931471805599453f;
+        *reinterpret_cast<uint2 *>(p.out + (int64_t)(row0 + r) * p.out_stride + (int64_t)hq * DH + d) =
+            make_uint2(*reinterpret_cast<uint32_t *>(&y0), *reinterpret_cast<uint32_t *>(&y1));
+        if (d == 0 && p.lse) p.lse[(int64_t)(row0 + r) * p.Hq + hq] = (m + log2f(sum)) * 0.6931471805599453f;
       } else {
         *reinterpret_cast<float4 *>(part + c * LDO + d) = y;
-        if (d == 0) { part[c * LDO + DH] = m; part[c * LDO + DH + 1] = l; }
+        if (d == 0) { part[c * LDO + DH] = m; part[c * LDO + DH + 1] = sum; }
       }
     }
     ptx::fence_proxy_async();                      // the ring was written by the threads: the next copies come after
     __syncthreads();
   }
   if (abort_flag) {                                // a wait ran out: copies in flight land before shared memory goes away
-    const uint64_t t0 = ptx::globaltimer();
-    while (ptx::globaltimer() - t0 < 200000ull) __nanosleep(1000);
+    const uint64_t start = ptx::globaltimer();
+    while (ptx::globaltimer() - start < 200000ull) __nanosleep(1000);
   }
 }
 
-// Joins the partial results of an item, in the order of its tiles; a block has one column of it.  Sequences without keys: output
-// 0, log-sum -inf.
-template <int DH>
+// Joins the partial results of an item, in the order of its tiles.  WPC warps have a column (4: few columns of many pieces);
+// a block of four warps, 4 / WPC columns.  Sequences without keys: output 0, log-sum -inf.
+template <int DH, int WPC>
 __global__ void __launch_bounds__(128) kv4_join_kernel(const AttnParams p, int n_ctas) {
   constexpr int LDO = DH + 4;
   __shared__ float sm_m[4], sm_l[4];
   __shared__ float4 sm_o[4][32];
-  grid_dep_launch();
   const Line &ln = p.line;
-  const int b = blockIdx.y, h = blockIdx.z, col = blockIdx.x, lane = threadIdx.x & 31, w = threadIdx.x >> 5;
+  const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, b = blockIdx.y, h = blockIdx.z, col = blockIdx.x * (4 / WPC) + w / WPC;
+  grid_dep_launch();
   grid_dep_wait();
-  if (col >= ln.b.n_rows(b) * ln.group) return;
+  if (col >= ln.b.n_rows(b) * ln.group) return;    // WPC 4: the whole block
   const int nt = ln.tiles(b), nc = ln.chunks(b), r = col / ln.group, hq = h * ln.group + col - r * ln.group;
   const int64_t row = ln.b.row0(b) + r;
   bf16 *out = p.out + row * p.out_stride + (int64_t)hq * DH + 4 * lane;
   float *lse = p.lse ? p.lse + row * p.Hq + hq : nullptr;
-  const bool mine = 4 * lane < DH;
+  const bool mine = 4 * lane < DH, lead = w % WPC == 0;
   if (nt == 0) {
-    if (w == 0 && mine) *reinterpret_cast<uint2 *>(out) = make_uint2(0u, 0u);
-    if (threadIdx.x == 0 && lse) *lse = -INFINITY;
+    if (lead && mine) *reinterpret_cast<uint2 *>(out) = make_uint2(0u, 0u);
+    if (lead && lane == 0 && lse) *lse = -INFINITY;
     return;
   }
-  const int64_t total = ln.before(ln.B), share = (total + n_ctas - 1) / n_ctas;
+  const int64_t total = ln.before(ln.B), share = ln.share(total, n_ctas);
   const int64_t start = ln.before(b) + ((int64_t)h * nc + col / ln.chunk) * nt;
   const int i0 = (int)(start / share), i1 = (int)((start + nt - 1) / share);
   if (i0 == i1) return;                            // stored by its CTA
   const int c = col % ln.chunk;
   float m = -INFINITY, l = 0.f;
   float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
-  for (int i = i0 + w; i <= i1; i += 4) {
+#pragma unroll 4
+  for (int i = i0 + w % WPC; i <= i1; i += WPC) {
     const float *part = p.part + (int64_t)(2 * i + (i == i0 ? 1 : 0)) * part_floats(ln.chunk, DH) + c * LDO;
-    const float pm = part[DH], pl = part[DH + 1];
+    const float2 ml = *reinterpret_cast<const float2 *>(part + DH);
     const float4 z = mine ? *reinterpret_cast<const float4 *>(part + 4 * lane) : make_float4(0.f, 0.f, 0.f, 0.f);
-    const float mn = fmaxf(m, pm), f = m == -INFINITY ? 0.f : ptx::ex2(m - mn), fp = pm == -INFINITY ? 0.f : ptx::ex2(pm - mn);
-    l = l * f + pl * fp;
+    const float mn = fmaxf(m, ml.x), f = m == -INFINITY ? 0.f : ptx::ex2(m - mn), fp = ml.x == -INFINITY ? 0.f : ptx::ex2(ml.x - mn);
+    l = l * f + ml.y * fp;
     y.x = y.x * f + z.x * fp; y.y = y.y * f + z.y * fp; y.z = y.z * f + z.z * fp; y.w = y.w * f + z.w * fp;
     m = mn;
   }
-  if (lane == 0) { sm_m[w] = m; sm_l[w] = l; }
-  sm_o[w][lane] = y;
-  __syncthreads();
-  if (w) return;
-  float mx = fmaxf(fmaxf(sm_m[0], sm_m[1]), fmaxf(sm_m[2], sm_m[3]));
-  l = 0.f; y = make_float4(0.f, 0.f, 0.f, 0.f);
+  if (WPC == 4) {
+    if (lane == 0) { sm_m[w] = m; sm_l[w] = l; }
+    sm_o[w][lane] = y;
+    __syncthreads();
+    if (w) return;
+    m = fmaxf(fmaxf(sm_m[0], sm_m[1]), fmaxf(sm_m[2], sm_m[3]));
+    l = 0.f; y = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const float f = sm_m[i] == -INFINITY ? 0.f : ptx::ex2(sm_m[i] - mx);
-    const float4 z = sm_o[i][lane];
-    l = fmaf(sm_l[i], f, l);
-    y.x = fmaf(z.x, f, y.x); y.y = fmaf(z.y, f, y.y); y.z = fmaf(z.z, f, y.z); y.w = fmaf(z.w, f, y.w);
+    for (int i = 0; i < 4; ++i) {
+      const float f = sm_m[i] == -INFINITY ? 0.f : ptx::ex2(sm_m[i] - m);
+      const float4 z = sm_o[i][lane];
+      l = fmaf(sm_l[i], f, l);
+      y.x = fmaf(z.x, f, y.x); y.y = fmaf(z.y, f, y.y); y.z = fmaf(z.z, f, y.z); y.w = fmaf(z.w, f, y.w);
+    }
   }
   const float inv = 1.f / l;
   if (mine) {
     __nv_bfloat162 y0 = __floats2bfloat162_rn(y.x * inv, y.y * inv), y1 = __floats2bfloat162_rn(y.z * inv, y.w * inv);
     *reinterpret_cast<uint2 *>(out) = make_uint2(*reinterpret_cast<uint32_t *>(&y0), *reinterpret_cast<uint32_t *>(&y1));
   }
-  if (lane == 0 && lse) *lse = (mx + log2f(l)) * 0.6931471805599453f;
+  if (lane == 0 && lse) *lse = (m + log2f(l)) * 0.6931471805599453f;
 }
 
 struct AttnPlan { int chunk, ctas; };
@@ -471,7 +548,8 @@ AttnPlan plan_attention(int heads, int B, int rows, int Hq, int max_len, int sms
   pl.chunk = cols <= 8 ? 8 : cols <= 16 ? 16 : 32;
   // no more CTAs than give each warp of them a tile
   const int64_t tiles = (int64_t)B * heads * ceil_div(cols, pl.chunk) * ceil_div(max_len, KV4_TILE), want = ceil_div64(tiles, WARPS);
-  pl.ctas = (int)(want < 1 ? 1 : want < sms ? want : sms);
+  const int most = sms * CTAS_PER_SM;
+  pl.ctas = (int)(want < 1 ? 1 : want < most ? want : most);
   return pl;
 }
 
@@ -484,10 +562,17 @@ int64_t attention_kv4_scratch_floats(const Kv4View &c, int B, int rows, int Hq, 
 
 template <int DH, int NT>
 static cudaError_t launch_attn(cudaStream_t st, const AttnParams &p, int ctas) {
-  constexpr size_t smem = (size_t)WARPS * STAGES * KV4_TILE * (DH + 8);
-  cudaError_t e = cudaFuncSetAttribute(attention_kv4_kernel<DH, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+  constexpr int smem = AttnShape<DH, NT>::SMEM;
+  cudaError_t e = cudaFuncSetAttribute(attention_kv4_kernel<DH, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
   if (e != cudaSuccess) return e;
-  return launch_kernel(attention_kv4_kernel<DH, NT>, dim3(ctas), dim3(WARPS * 32), smem, st, p);
+  return launch_kernel(attention_kv4_kernel<DH, NT>, dim3(ctas), dim3(WARPS * 32), (size_t)smem, st, p);
+}
+
+template <int DH>
+static cudaError_t launch_join(cudaStream_t st, const AttnParams &p, int ctas, int cols) {
+  const int64_t all = (int64_t)cols * p.line.B * p.line.H;
+  if (all <= 2048) return launch_kernel(kv4_join_kernel<DH, 4>, dim3(cols, p.line.B, p.line.H), dim3(128), 0, st, p, ctas);
+  return launch_kernel(kv4_join_kernel<DH, 1>, dim3(ceil_div(cols, 4), p.line.B, p.line.H), dim3(128), 0, st, p, ctas);
 }
 
 cudaError_t launch_attention_kv4(cudaStream_t st, const Kv4AttnArgs &a, int sms) {
@@ -498,14 +583,12 @@ cudaError_t launch_attention_kv4(cudaStream_t st, const Kv4AttnArgs &a, int sms)
   Line &ln = p.line;
   ln.B = a.b.B; ln.H = a.c.heads; ln.chunk = pl.chunk; ln.group = a.Hq / a.c.heads; ln.slots = a.c.slots;
   ln.max_keys = a.max_len < a.c.cap ? a.max_len : a.c.cap; ln.b = a.b;
-  const int nt = pl.chunk / 8;
+  const int nt = pl.chunk / 8, cols = a.b.rows * ln.group;
   cudaError_t e;
   if (a.c.dh == 128) e = nt == 1 ? launch_attn<128, 1>(st, p, pl.ctas) : nt == 2 ? launch_attn<128, 2>(st, p, pl.ctas) : launch_attn<128, 4>(st, p, pl.ctas);
   else e = nt == 1 ? launch_attn<64, 1>(st, p, pl.ctas) : nt == 2 ? launch_attn<64, 2>(st, p, pl.ctas) : launch_attn<64, 4>(st, p, pl.ctas);
   if (e != cudaSuccess) return e;
-  const dim3 grid((unsigned)(a.b.rows * ln.group), a.b.B, a.c.heads);
-  if (a.c.dh == 128) return launch_kernel(kv4_join_kernel<128>, grid, dim3(128), 0, st, p, pl.ctas);
-  return launch_kernel(kv4_join_kernel<64>, grid, dim3(128), 0, st, p, pl.ctas);
+  return a.c.dh == 128 ? launch_join<128>(st, p, pl.ctas, cols) : launch_join<64>(st, p, pl.ctas, cols);
 }
 
 // ---- weights -----------------------------------------------------------------------------------------------------------
@@ -548,8 +631,11 @@ __global__ void __launch_bounds__(256) kv4_weights_kernel(const WeighParams p) {
     const int col = n + g, r = col / ln.group, hq = h * ln.group + col - r * ln.group;
     const bool there = col < cols;
     uint32_t qf[DH / 8];
-    float cf, cs;
-    load_queries<DH>(p.q + (int64_t)(row0 + r) * p.q_stride + (int64_t)hq * DH + t * (DH / 4), there, p.scale_log2, qf, cf, cs);
+    Queries<DH> qn;
+    qn.load(p.q + (int64_t)(row0 + r) * p.q_stride + (int64_t)hq * DH + t * (DH / 4), there);
+    const int qe = query_exponent(qn.finite() ? qn.top : 0u);
+    const float cf = query_factor(p.scale_log2, qe);
+    float cs = qn.convert(qe, qf);
     float lse = there ? p.lse[(int64_t)(row0 + r) * p.Hq + hq] * 1.4426950408889634f : INFINITY;
     if (lse == -INFINITY) lse = INFINITY;          // a row without keys gives no weight
     float acc[4] = {0.f, 0.f, 0.f, 0.f};
