@@ -1603,6 +1603,7 @@ l2pd_status l2pd_attention_kv4(void *stream, const l2pd_kv4 *cache, const void *
   if (!out || !scratch) return refuse(L2PD_ERR_ARG, call, "null pointer");
   if (out_stride < (int64_t)Hq * a.c.dh || out_stride % 8 || !aligned16(out) || !aligned16(scratch))
     return refuse(L2PD_ERR_SHAPE, call, "row stride of at least Hq * head_dim, rows and scratch on 16 bytes");
+  if (!attention_kv4_fits(a.c, B, rows, Hq, max_len)) return refuse(L2PD_ERR_SHAPE, call, "2^31 tiles of work or more");
   const int sms = device_sms();
   if (scratch_bytes < 4 * attention_kv4_scratch_floats(a.c, B, rows, Hq, max_len, sms))
     return refuse(L2PD_ERR_SHAPE, call, "scratch smaller than l2pd_attention_kv4_scratch_bytes");

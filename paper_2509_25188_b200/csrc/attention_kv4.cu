@@ -27,58 +27,78 @@ namespace {
 
 using ptx::F2;
 
-constexpr int WARPS = 4, CTAS_PER_SM = 2;
+constexpr int WARPS = 4;
 constexpr float LAZY = 6.0f;         // log2 units the running maximum may pass the reference
 
 // ---- the line of work --------------------------------------------------------------------------------------------------
-// Items: for sequence b, key heads times chunks of `chunk` columns (those that have rows), tiles_b key tiles each.
+// Items: for sequence b, key heads times chunks of `chunk` columns (those that have rows), tiles_b key tiles each.  Fewer than 2^31
+// tiles in all (the host sees to it).  Every warp surveys the line for itself, a lane a sequence: the lengths and rows of 32
+// sequences are one round of loads.
+struct Seq { int keys, rows, row0, slot, tiles, chunks; uint32_t count; };
 struct Line {
-  int B, H, chunk, group, slots, max_keys;
+  int B, H, chunk, group, slots, max_keys, tile_keys;
   Kv4Batch b;
-  __device__ __forceinline__ int keys(int s) const { return b.slot(s, slots) < 0 ? 0 : max(0, min(b.keys[s], max_keys)); }
-  __device__ __forceinline__ int chunks(int s) const { return (b.n_rows(s) * group + chunk - 1) / chunk; }
-  __device__ __forceinline__ int tiles(int s) const { return (keys(s) + KV4_TILE - 1) / KV4_TILE; }
-  __device__ __forceinline__ int64_t all_tiles(int s) const { return s < B ? (int64_t)H * chunks(s) * tiles(s) : 0; }
-  // tiles of the sequences [0, s), the same answer in every lane (whole warp)
-  __device__ int64_t before(int s) const {
-    int64_t x = 0;
-    for (int i = threadIdx.x & 31; i < s; i += 32) x += all_tiles(i);
-#pragma unroll
-    for (int o = 16; o; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
-    return x;
+  __device__ __forceinline__ Seq seq(int s) const {
+    Seq q = {0, 0, 0, -1, 0, 0, 0u};
+    if (s >= B) return q;
+    const int len = b.keys[s];
+    q.rows = b.n_rows(s); q.row0 = b.row0(s); q.slot = b.slot(s, slots);
+    q.keys = q.slot < 0 ? 0 : max(0, min(len, max_keys));
+    q.tiles = (q.keys + tile_keys - 1) / tile_keys;
+    q.chunks = (q.rows * group + chunk - 1) / chunk;
+    q.count = (uint32_t)H * q.chunks * q.tiles;
+    return q;
   }
-  // sequence that tile `pos` of the line belongs to, and the tiles before it (whole warp; pos below the line's end)
-  __device__ int find(int64_t pos, int64_t *start) const {
+  // Tiles of the line and of a CTA's run; *before: tiles of the sequences ahead of `upto`.  `own` is seq(lane).  (Whole warp.)
+  // Sequences of one length: whole items where that costs the longest run no more than a fifth, since a split item's halves go
+  // through memory.
+  __device__ uint32_t survey(const Seq &own, uint32_t ctas, int upto, uint32_t *share, uint32_t *before) const {
     const int lane = threadIdx.x & 31;
-    int64_t run = 0;
-    for (int s0 = 0;; s0 += 32) {
-      const int64_t own = all_tiles(s0 + lane);
-      int64_t x = own;
+    uint32_t total = 0, ahead = 0, lo = 0xffffffffu, hi = 0;
+    Seq q = own;
+    for (int s0 = 0;;) {
+      total += __reduce_add_sync(0xffffffffu, q.count);
+      ahead += __reduce_add_sync(0xffffffffu, s0 + lane < upto ? q.count : 0u);
+      lo = min(lo, __reduce_min_sync(0xffffffffu, q.chunks ? (uint32_t)q.tiles : 0xffffffffu));
+      hi = max(hi, __reduce_max_sync(0xffffffffu, q.chunks ? (uint32_t)q.tiles : 0u));
+      if ((s0 += 32) >= B) break;
+      q = seq(s0 + lane);
+    }
+    uint32_t even = (total + ctas - 1) / ctas;
+    if (lo == hi && hi) {
+      const uint32_t whole = (total / hi + ctas - 1) / ctas * hi;
+      if (whole <= even + even / 5) even = whole;
+    }
+    *share = even;
+    if (before) *before = ahead;
+    return total;
+  }
+  // The sequence that tile `pos` of the line belongs to, and the tiles before it.  (Whole warp, pos below the line's end.)
+  __device__ Seq find(const Seq &own, uint32_t pos, uint32_t *start) const {
+    const int lane = threadIdx.x & 31;
+    uint32_t run = 0;
+    Seq q = own;
+    for (int s0 = 0;;) {
+      uint32_t x = q.count;
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
-        const int64_t y = __shfl_up_sync(0xffffffffu, x, o);
+        const uint32_t y = __shfl_up_sync(0xffffffffu, x, o);
         if (lane >= o) x += y;
       }
       const unsigned here = __ballot_sync(0xffffffffu, pos < run + x);
       if (here || s0 + 32 >= B) {
         const int l = here ? __ffs(here) - 1 : 31;
-        *start = run + __shfl_sync(0xffffffffu, x - own, l);
-        return min(s0 + l, B - 1);
+        *start = run + __shfl_sync(0xffffffffu, x - q.count, l);
+        Seq r;
+        r.keys = __shfl_sync(0xffffffffu, q.keys, l); r.rows = __shfl_sync(0xffffffffu, q.rows, l);
+        r.row0 = __shfl_sync(0xffffffffu, q.row0, l); r.slot = __shfl_sync(0xffffffffu, q.slot, l);
+        r.tiles = __shfl_sync(0xffffffffu, q.tiles, l); r.chunks = __shfl_sync(0xffffffffu, q.chunks, l);
+        r.count = 0;
+        return r;
       }
       run += __shfl_sync(0xffffffffu, x, 31);
+      q = seq((s0 += 32) + lane);
     }
-  }
-  // Tiles of a CTA's run.  Sequences of one length: whole items where that costs the longest run no more than a fifth, since a
-  // split item's halves go through memory (8 x 32 heads of 2048 keys on 296 CTAs: 32 tiles instead of 28).
-  __device__ int64_t share(int64_t total, int ctas) const {
-    const int64_t even = (total + ctas - 1) / ctas;
-    const int nt = tiles(0);
-    int64_t items = nt ? total / nt : 0;
-    bool same = true;
-    for (int i = threadIdx.x & 31; i < B; i += 32) same = same && (tiles(i) == nt || chunks(i) == 0);
-    if (!__all_sync(0xffffffffu, same)) return even;
-    const int64_t whole = (items + ctas - 1) / ctas * nt;
-    return whole * 5 <= even * 6 ? whole : even;
   }
 };
 
@@ -157,17 +177,18 @@ __device__ __forceinline__ float query_factor(float scale_log2, int u) {
 }
 
 template <int DH, int NT> struct AttnShape {
-  static constexpr int CH = 8 * NT, TILE = KV4_TILE * (DH + 8), STAGES = NT == 1 ? 3 : 2, RING = STAGES * TILE;
+  static constexpr int CH = 8 * NT, TILE = KV4_TILE * (DH + 8), STAGES = 3, RING = STAGES * TILE;
+  static constexpr int CTAS = NT == 1 ? 4 : 3;     // an SM's, as registers allow
   static constexpr int META = KV4_TILE * 24, QBYTES = NT * DH * 16;
   static constexpr int OFF_META = WARPS * RING, OFF_Q = OFF_META + WARPS * META, SMEM = OFF_Q + QBYTES;
 };
 
 template <int DH, int NT>
-__global__ void __launch_bounds__(WARPS * 32, CTAS_PER_SM) attention_kv4_kernel(const AttnParams p) {
+__global__ void __launch_bounds__(WARPS * 32, AttnShape<DH, NT>::CTAS) attention_kv4_kernel(const AttnParams p) {
   using Sh = AttnShape<DH, NT>;
-  constexpr int W = DH / 32, MT = DH / 16, CH = Sh::CH, MS = 4 / NT;   // MS: groups of 16 keys taken together
+  constexpr int W = DH / 32, MT = DH / 16, CH = Sh::CH, MS = NT == 1 ? 2 : 1;   // MS: groups of 16 keys taken together
   constexpr int TILE = Sh::TILE, RING = Sh::RING, STAGES = Sh::STAGES, LDO = DH + 4;
-  static_assert(CH * LDO * 4 <= RING, "a warp's output goes to its ring");
+  static_assert(KV4_TILE == 32 && CH * LDO * 4 <= RING, "a warp's output goes to its ring");
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ __align__(8) uint64_t bars[WARPS * STAGES];
   __shared__ float fin[WARPS][2][CH];              // reference and sum of probabilities
@@ -192,18 +213,19 @@ __global__ void __launch_bounds__(WARPS * 32, CTAS_PER_SM) attention_kv4_kernel(
   grid_dep_wait();
 
   const Line &ln = p.line;
-  const int64_t total = ln.before(ln.B), share = ln.share(total, gridDim.x);
-  int64_t pos = share * blockIdx.x;
-  const int64_t end = min(total, pos + share);
+  const Seq own = ln.seq(lane);
+  uint32_t share;
+  const uint32_t total = ln.survey(own, gridDim.x, 0, &share, nullptr);
+  uint32_t pos = min((uint64_t)share * blockIdx.x, (uint64_t)total);
+  const uint32_t end = min(total, pos + share);
   uint32_t used = 0;                               // tiles this warp has taken: stage and parity
   while (pos < end) {
-    int64_t b_start;
-    const int b = ln.find(pos, &b_start);
-    const int n_keys = ln.keys(b), nt = ln.tiles(b), nc = ln.chunks(b), rows = ln.b.n_rows(b), row0 = ln.b.row0(b);
-    const int64_t in_b = pos - b_start;
-    const int item = (int)(in_b / nt), t0 = (int)(in_b - (int64_t)item * nt), t1 = (int)min((int64_t)nt, t0 + (end - pos));
-    const int h = item / nc, c0 = (item - h * nc) * CH, cols = min(CH, rows * ln.group - c0);
-    const uint8_t *src = p.c.tile(ln.b.slot(b, ln.slots), h, 0);
+    uint32_t before;
+    const Seq sq = ln.find(own, pos, &before);
+    const int nt = sq.tiles, item = (int)((pos - before) / nt), t0 = (int)(pos - before) - item * nt, t1 = (int)min((uint32_t)nt, t0 + (end - pos));
+    const int h = item / sq.chunks, c0 = (item - h * sq.chunks) * CH, cols = min(CH, sq.rows * ln.group - c0);
+    const int n_keys = sq.keys, row0 = sq.row0;
+    const uint8_t *src = p.c.tile(sq.slot, h, 0);
     pos += t1 - t0;
 
     // this warp's tiles: t0 + warp, + WARPS, ...
@@ -260,17 +282,11 @@ __global__ void __launch_bounds__(WARPS * 32, CTAS_PER_SM) attention_kv4_kernel(
       const int left = n_keys - (t0 + warp + i * WARPS) * KV4_TILE;    // keys of this tile, or more
       // what belongs to a key, once for all columns; keys behind the end get weight 0
       {
-        uint32_t km[2], vm[2];
-        int ex[2];
-#pragma unroll
-        for (int x = 0; x < 2; ++x) {
-          const int k = lane + 32 * x;
-          const bool real = k < left;
-          km[x] = real ? *reinterpret_cast<const uint32_t *>(tile + kv4_off_kmeta(DH) + 4 * k) : 0u;
-          vm[x] = real ? *reinterpret_cast<const uint32_t *>(tile + kv4_off_vmeta(DH) + 4 * k) : 0u;
-          ex[x] = min(max((int)((vm[x] >> 7) & 255u), (int)((vm[x] >> 23) & 255u) - 4) - 126, 100);
-        }
-        const int ex_top = __reduce_max_sync(0xffffffffu, max(ex[0], ex[1]));
+        const bool real = lane < left;
+        const uint32_t km = real ? *reinterpret_cast<const uint32_t *>(tile + kv4_off_kmeta(DH) + 4 * lane) : 0u;
+        const uint32_t vm = real ? *reinterpret_cast<const uint32_t *>(tile + kv4_off_vmeta(DH) + 4 * lane) : 0u;
+        const int ex = min(max((int)((vm >> 7) & 255u), (int)((vm >> 23) & 255u) - 4) - 126, 100);
+        const int ex_top = __reduce_max_sync(0xffffffffu, ex);
         if (ex_top > e0) {                         // rare: what came before is in units of 2^e0
           const int was = e0;
           e0 = max(ex_top, -100) + 2;
@@ -282,18 +298,15 @@ __global__ void __launch_bounds__(WARPS * 32, CTAS_PER_SM) attention_kv4_kernel(
             for (int m = 0; m < MT; ++m) { o[m][n][0] *= f; o[m][n][1] *= f; o[m][n][2] *= f; o[m][n][3] *= f; }
           }
         }
-#pragma unroll
-        for (int x = 0; x < 2; ++x) {
-          const int k = lane + 32 * x, e = max(ex[x], e0 - 60);
-          const float w = __uint_as_float((uint32_t)(127 - e) << 23);
-          meta_a[k] = make_float4(kv4_scale(km[x]) * cf, kv4_min(km[x]) * cf, k < left ? (float)(e - e0) : -INFINITY,
-                                  __uint_as_float((uint32_t)(127 - e + e0) << 23));
-          meta_b[k] = make_float2(kv4_scale(vm[x]) * w, kv4_min(vm[x]) * w);
-        }
+        const int e = max(ex, e0 - 60);
+        const float w = __uint_as_float((uint32_t)(127 - e) << 23);
+        meta_a[lane] = make_float4(kv4_scale(km) * cf, kv4_min(km) * cf, real ? (float)(e - e0) : -INFINITY,
+                                   __uint_as_float((uint32_t)(127 - e + e0) << 23));
+        meta_b[lane] = make_float2(kv4_scale(vm) * w, kv4_min(vm) * w);
         __syncwarp();
       }
 #pragma unroll 1
-      for (int s0 = 0; s0 < 4; s0 += MS) {
+      for (int s0 = 0; s0 < KV4_TILE / 16; s0 += MS) {
         float acc[MS][NT][4];
         const int kr = 16 * s0 + tile_row(g);
         uint32_t ka[MS][W], kb[MS][W];
@@ -309,18 +322,24 @@ __global__ void __launch_bounds__(WARPS * 32, CTAS_PER_SM) attention_kv4_kernel(
           }
         }
 #pragma unroll
-        for (int j = 0; j < W; ++j)
+        for (int j = 0; j < W; ++j) {
+          uint32_t x[MS][4], y[MS][4];
 #pragma unroll
-          for (int u = 0; u < MS; ++u) {
-            uint32_t x[4], y[4];
-            spread(ka[u][j], x); spread(kb[u][j], y);
+          for (int u = 0; u < MS; ++u) { spread(ka[u][j], x[u]); spread(kb[u][j], y[u]); }
+          // one step of all sums, then the next: a sum's steps depend on one another
+#pragma unroll
+          for (int u = 0; u < MS; ++u)
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
-              if (j == 0) ptx::mma_f16_16x8x16_first(acc[u][n], x[0], y[0], x[1], y[1], qf[n][0], qf[n][1]);
-              else ptx::mma_f16_16x8x16(acc[u][n], x[0], y[0], x[1], y[1], qf[n][4 * j], qf[n][4 * j + 1]);
-              ptx::mma_f16_16x8x16(acc[u][n], x[2], y[2], x[3], y[3], qf[n][4 * j + 2], qf[n][4 * j + 3]);
+              if (j == 0) ptx::mma_f16_16x8x16_first(acc[u][n], x[u][0], y[u][0], x[u][1], y[u][1], qf[n][0], qf[n][1]);
+              else ptx::mma_f16_16x8x16(acc[u][n], x[u][0], y[u][0], x[u][1], y[u][1], qf[n][4 * j], qf[n][4 * j + 1]);
             }
-          }
+#pragma unroll
+          for (int u = 0; u < MS; ++u)
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+              ptx::mma_f16_16x8x16(acc[u][n], x[u][2], y[u][2], x[u][3], y[u][3], qf[n][4 * j + 2], qf[n][4 * j + 3]);
+        }
         // scores against the reference
         float top = -INFINITY;
 #pragma unroll
@@ -489,9 +508,10 @@ __global__ void __launch_bounds__(128) kv4_join_kernel(const AttnParams p, int n
   const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, b = blockIdx.y, h = blockIdx.z, col = blockIdx.x * (4 / WPC) + w / WPC;
   grid_dep_launch();
   grid_dep_wait();
-  if (col >= ln.b.n_rows(b) * ln.group) return;    // WPC 4: the whole block
-  const int nt = ln.tiles(b), nc = ln.chunks(b), r = col / ln.group, hq = h * ln.group + col - r * ln.group;
-  const int64_t row = ln.b.row0(b) + r;
+  const Seq own = ln.seq(lane), sq = ln.seq(b);
+  if (col >= sq.rows * ln.group) return;           // WPC 4: the whole block
+  const int nt = sq.tiles, r = col / ln.group, hq = h * ln.group + col - r * ln.group;
+  const int64_t row = (int64_t)sq.row0 + r;
   bf16 *out = p.out + row * p.out_stride + (int64_t)hq * DH + 4 * lane;
   float *lse = p.lse ? p.lse + row * p.Hq + hq : nullptr;
   const bool mine = 4 * lane < DH, lead = w % WPC == 0;
@@ -500,8 +520,9 @@ __global__ void __launch_bounds__(128) kv4_join_kernel(const AttnParams p, int n
     if (lead && lane == 0 && lse) *lse = -INFINITY;
     return;
   }
-  const int64_t total = ln.before(ln.B), share = ln.share(total, n_ctas);
-  const int64_t start = ln.before(b) + ((int64_t)h * nc + col / ln.chunk) * nt;
+  uint32_t share, before;
+  ln.survey(own, n_ctas, b, &share, &before);
+  const uint32_t start = before + ((uint32_t)h * sq.chunks + col / ln.chunk) * nt;
   const int i0 = (int)(start / share), i1 = (int)((start + nt - 1) / share);
   if (i0 == i1) return;                            // stored by its CTA
   const int c = col % ln.chunk;
@@ -545,15 +566,20 @@ struct AttnPlan { int chunk, ctas; };
 AttnPlan plan_attention(int heads, int B, int rows, int Hq, int max_len, int sms) {
   AttnPlan pl;
   const int cols = rows * (Hq / heads);
-  pl.chunk = cols <= 8 ? 8 : cols <= 16 ? 16 : 32;
+  pl.chunk = cols <= 8 ? 8 : 16;
   // no more CTAs than give each warp of them a tile
   const int64_t tiles = (int64_t)B * heads * ceil_div(cols, pl.chunk) * ceil_div(max_len, KV4_TILE), want = ceil_div64(tiles, WARPS);
-  const int most = sms * CTAS_PER_SM;
+  const int most = sms * (pl.chunk == 8 ? 4 : 3);
   pl.ctas = (int)(want < 1 ? 1 : want < most ? want : most);
   return pl;
 }
 
 }  // namespace
+
+bool attention_kv4_fits(const Kv4View &c, int B, int rows, int Hq, int max_len) {
+  const double len = max_len < c.cap ? max_len : c.cap;
+  return (double)B * c.heads * ((double)rows * (Hq / c.heads) / 8 + 1) * (len / KV4_TILE + 1) < 2147483648.0;
+}
 
 int64_t attention_kv4_scratch_floats(const Kv4View &c, int B, int rows, int Hq, int max_len, int sms) {
   const AttnPlan pl = plan_attention(c.heads, B, rows, Hq, max_len, sms);
@@ -582,11 +608,11 @@ cudaError_t launch_attention_kv4(cudaStream_t st, const Kv4AttnArgs &a, int sms)
   p.scale_log2 = a.scale * 1.4426950408889634f; p.part = a.scratch; p.status = a.status;
   Line &ln = p.line;
   ln.B = a.b.B; ln.H = a.c.heads; ln.chunk = pl.chunk; ln.group = a.Hq / a.c.heads; ln.slots = a.c.slots;
-  ln.max_keys = a.max_len < a.c.cap ? a.max_len : a.c.cap; ln.b = a.b;
+  ln.max_keys = a.max_len < a.c.cap ? a.max_len : a.c.cap; ln.tile_keys = KV4_TILE; ln.b = a.b;
   const int nt = pl.chunk / 8, cols = a.b.rows * ln.group;
   cudaError_t e;
-  if (a.c.dh == 128) e = nt == 1 ? launch_attn<128, 1>(st, p, pl.ctas) : nt == 2 ? launch_attn<128, 2>(st, p, pl.ctas) : launch_attn<128, 4>(st, p, pl.ctas);
-  else e = nt == 1 ? launch_attn<64, 1>(st, p, pl.ctas) : nt == 2 ? launch_attn<64, 2>(st, p, pl.ctas) : launch_attn<64, 4>(st, p, pl.ctas);
+  if (a.c.dh == 128) e = nt == 1 ? launch_attn<128, 1>(st, p, pl.ctas) : launch_attn<128, 2>(st, p, pl.ctas);
+  else e = nt == 1 ? launch_attn<64, 1>(st, p, pl.ctas) : launch_attn<64, 2>(st, p, pl.ctas);
   if (e != cudaSuccess) return e;
   return a.c.dh == 128 ? launch_join<128>(st, p, pl.ctas, cols) : launch_join<64>(st, p, pl.ctas, cols);
 }
@@ -613,9 +639,9 @@ __global__ void __launch_bounds__(256) kv4_weights_kernel(const WeighParams p) {
   const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   const Line &ln = p.line;
   const int b = blockIdx.y, h = blockIdx.z, key0 = blockIdx.x * 128 + (threadIdx.x >> 5) * 16;
-  const int n_keys = ln.keys(b);
+  const Seq sq = ln.seq(b);
+  const int n_keys = sq.keys, slot = sq.slot, cols = sq.rows * ln.group, row0 = sq.row0;
   if (key0 >= n_keys) return;
-  const int slot = ln.b.slot(b, ln.slots), cols = ln.b.n_rows(b) * ln.group, row0 = ln.b.row0(b);
   const uint8_t *tile = p.c.tile(slot, h, key0 / KV4_TILE);
   const int kr = key0 % KV4_TILE + g;
   uint32_t ka[W], kb[W];
@@ -672,7 +698,7 @@ cudaError_t launch_kv4_weights(cudaStream_t st, const Kv4WeighArgs &a, int sms) 
   p.w_in = a.w_in; p.w_out = a.w_out;
   Line &ln = p.line;
   ln.B = a.b.B; ln.H = a.c.heads; ln.chunk = 8; ln.group = a.Hq / a.c.heads; ln.slots = a.c.slots;
-  ln.max_keys = a.max_len < a.c.cap ? a.max_len : a.c.cap; ln.b = a.b;
+  ln.max_keys = a.max_len < a.c.cap ? a.max_len : a.c.cap; ln.tile_keys = KV4_TILE; ln.b = a.b;
   const dim3 grid((unsigned)ceil_div(a.max_len, 128), a.b.B, a.c.heads);
   if (a.c.dh == 128) return launch_kernel(kv4_weights_kernel<128>, grid, dim3(256), 0, st, p);
   return launch_kernel(kv4_weights_kernel<64>, grid, dim3(256), 0, st, p);

@@ -5,8 +5,8 @@
 // Products with a row then need no values, only codes: q . x = s (q . c) + m sum(q), and sum_j p_j x_j = sum_j (p_j s_j) c_j +
 // sum_j p_j m_j: s and m meet the scores and the probabilities, one number a key instead of one a value.
 //
-// A (slot, head) is a run of tiles of 64 keys; a tile is one contiguous piece, which one bulk copy brings to shared memory:
-//     [64][dh/2] codes of K | [64] (s, m) of K | [64] (s, m) of V | [64][dh/2] codes of V        64 (dh + 8) bytes
+// A (slot, head) is a run of tiles of 32 keys; a tile is one contiguous piece, which one bulk copy brings to shared memory:
+//     [32][dh/2] codes of K | [32] (s, m) of K | [32] (s, m) of V | [32][dh/2] codes of V        32 (dh + 8) bytes
 // so that the scores alone read its first half.  A row's codes are in the order of the dimensions, the even one in a byte's low
 // half.  Head size 128: in V rows of keys 4..7 of every eight, the two halves of a row change places, so that the four keys whose
 // rows a warp reads at once (4 keys x 32 bytes) lie in different banks.
@@ -15,7 +15,7 @@
 
 namespace l2pd {
 
-constexpr int KV4_TILE = 64;
+constexpr int KV4_TILE = 32;
 constexpr int KV4_MAX_EVICT = 1 << 19;   // longest sequence an eviction takes: its bitmap lies in shared memory
 
 __host__ __device__ __forceinline__ int kv4_tile_bytes(int dh) { return KV4_TILE * (dh + 8); }
@@ -81,6 +81,7 @@ struct Kv4AttnArgs {
   float *scratch; int64_t scratch_floats;
   int32_t *status;
 };
+bool attention_kv4_fits(const Kv4View &c, int B, int rows, int Hq, int max_len);   // fewer than 2^31 tiles of work
 int64_t attention_kv4_scratch_floats(const Kv4View &c, int B, int rows, int Hq, int max_len, int sms);
 cudaError_t launch_attention_kv4(cudaStream_t st, const Kv4AttnArgs &a, int sms);
 struct Kv4WeighArgs {

@@ -49,7 +49,7 @@ def test_bytes_of_a_cache():
     b, _ = _cache()
     n = b.lib.l2pd_kv4_bytes
     assert n(1, 1, 128, 64) == 64 * 136 and n(1, 1, 64, 64) == 64 * 72
-    assert n(2, 4, 128, 65) == 2 * 4 * 128 * 136
+    assert n(2, 4, 128, 65) == 2 * 4 * 96 * 136
     assert n(100, 32, 128, 131072) == 100 * 32 * 131072 * 136          # past 32 bits
     for bad in ((0, 1, 128, 1), (1, 0, 128, 1), (1, 1, 96, 1), (1, 1, 128, 0), (-1, 1, 64, 4), (2 ** 31 - 1, 65535, 128, 2 ** 31 - 1)):
         assert n(*bad) == 0
