@@ -11,7 +11,7 @@ CSRC = os.path.join(HERE, "csrc")
 OUT = os.path.join(HERE, "libl2pd.so")
 OBJ = os.path.join(HERE, "_build")
 SOURCES = ["api.cu", "elementwise.cu", "simt.cu", "decide.cu", "gemm_tcgen05.cu", "attention.cu", "attention_tc.cu", "lm_head_static.cu", "filter_train.cu",
-           "kv4.cu", "attention_kv4.cu", "norm_rope.cu"]
+           "kv4.cu", "attention_kv4.cu", "attention_kv4_tc.cu", "norm_rope.cu"]
 NVCC = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
 FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
          "-Xcompiler", "-fPIC"]

@@ -18,104 +18,16 @@
 #include <cuda_fp16.h>
 #include <math.h>
 
-#include "kv4.cuh"
-#include "ptx.cuh"
+#include "attention_kv4.cuh"
 
 namespace l2pd {
 
 namespace {
 
+using namespace kv4;
 using ptx::F2;
 
 constexpr int WARPS = 4;
-constexpr float LAZY = 6.0f;         // log2 units the running maximum may pass the reference
-
-// ---- the line of work --------------------------------------------------------------------------------------------------
-// Items: for sequence b, key heads times chunks of `chunk` columns (those that have rows), tiles_b key tiles each.  Fewer than 2^31
-// tiles in all (the host sees to it).  Every warp surveys the line for itself, a lane a sequence: the lengths and rows of 32
-// sequences are one round of loads.
-struct Seq { int keys, rows, row0, slot, tiles, chunks; uint32_t count; };
-struct Line {
-  int B, H, chunk, group, slots, max_keys, tile_keys;
-  Kv4Batch b;
-  __device__ __forceinline__ Seq seq(int s) const {
-    Seq q = {0, 0, 0, -1, 0, 0, 0u};
-    if (s >= B) return q;
-    const int len = b.keys[s];
-    q.rows = b.n_rows(s); q.row0 = b.row0(s); q.slot = b.slot(s, slots);
-    q.keys = q.slot < 0 ? 0 : max(0, min(len, max_keys));
-    q.tiles = (q.keys + tile_keys - 1) / tile_keys;
-    q.chunks = (q.rows * group + chunk - 1) / chunk;
-    q.count = (uint32_t)H * q.chunks * q.tiles;
-    return q;
-  }
-  // Tiles of the line and of a CTA's run; *before: tiles of the sequences ahead of `upto`.  `own` is seq(lane).  (Whole warp.)
-  // Sequences of one length: whole items where that costs the longest run no more than a fifth, since a split item's halves go
-  // through memory.
-  __device__ uint32_t survey(const Seq &own, uint32_t ctas, int upto, uint32_t *share, uint32_t *before) const {
-    const int lane = threadIdx.x & 31;
-    uint32_t total = 0, ahead = 0, lo = 0xffffffffu, hi = 0;
-    Seq q = own;
-    for (int s0 = 0;;) {
-      total += __reduce_add_sync(0xffffffffu, q.count);
-      ahead += __reduce_add_sync(0xffffffffu, s0 + lane < upto ? q.count : 0u);
-      lo = min(lo, __reduce_min_sync(0xffffffffu, q.chunks ? (uint32_t)q.tiles : 0xffffffffu));
-      hi = max(hi, __reduce_max_sync(0xffffffffu, q.chunks ? (uint32_t)q.tiles : 0u));
-      if ((s0 += 32) >= B) break;
-      q = seq(s0 + lane);
-    }
-    uint32_t even = (total + ctas - 1) / ctas;
-    if (lo == hi && hi) {
-      const uint32_t whole = (total / hi + ctas - 1) / ctas * hi;
-      if (whole <= even + even / 5) even = whole;
-    }
-    *share = even;
-    if (before) *before = ahead;
-    return total;
-  }
-  // The sequence that tile `pos` of the line belongs to, and the tiles before it.  (Whole warp, pos below the line's end.)
-  __device__ Seq find(const Seq &own, uint32_t pos, uint32_t *start) const {
-    const int lane = threadIdx.x & 31;
-    uint32_t run = 0;
-    Seq q = own;
-    for (int s0 = 0;;) {
-      uint32_t x = q.count;
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const uint32_t y = __shfl_up_sync(0xffffffffu, x, o);
-        if (lane >= o) x += y;
-      }
-      const unsigned here = __ballot_sync(0xffffffffu, pos < run + x);
-      if (here || s0 + 32 >= B) {
-        const int l = here ? __ffs(here) - 1 : 31;
-        *start = run + __shfl_sync(0xffffffffu, x - q.count, l);
-        Seq r;
-        r.keys = __shfl_sync(0xffffffffu, q.keys, l); r.rows = __shfl_sync(0xffffffffu, q.rows, l);
-        r.row0 = __shfl_sync(0xffffffffu, q.row0, l); r.slot = __shfl_sync(0xffffffffu, q.slot, l);
-        r.tiles = __shfl_sync(0xffffffffu, q.tiles, l); r.chunks = __shfl_sync(0xffffffffu, q.chunks, l);
-        r.count = 0;
-        return r;
-      }
-      run += __shfl_sync(0xffffffffu, x, 31);
-      q = seq((s0 += 32) + lane);
-    }
-  }
-};
-
-struct AttnParams {
-  Kv4View c;
-  Line line;
-  int Hq;
-  const bf16 *q; bf16 *out; float *lse;
-  int64_t q_stride, out_stride;
-  float scale_log2;
-  float *part;             // [2 * CTAs][chunk][dh + 4]: O, M, L of a partial item
-  int32_t *status;
-};
-
-__host__ __device__ constexpr int part_floats(int chunk, int dh) { return chunk * (dh + 4); }
-
-__device__ __forceinline__ void fail(int32_t *status, int code) { if (status) atomicCAS(status, 0, code); }
 
 // The four registers of two MMA steps in a word of eight codes: codes 0 and 4, 1 and 5 (times 16), 2 and 6, 3 and 7 (times 16).
 __device__ __forceinline__ void spread(uint32_t w, uint32_t *r) {
@@ -561,15 +473,18 @@ __global__ void __launch_bounds__(128) kv4_join_kernel(const AttnParams p, int n
   if (lane == 0 && lse) *lse = (m + log2f(l)) * 0.6931471805599453f;
 }
 
-struct AttnPlan { int chunk, ctas; };
+// Up to 8 columns: the warp-level kernel, whose operands never leave registers.  More: tcgen05 with 32, 64 or 128 lanes.
+struct AttnPlan { int chunk, ctas, tc; };
 
 AttnPlan plan_attention(int heads, int B, int rows, int Hq, int max_len, int sms) {
   AttnPlan pl;
   const int cols = rows * (Hq / heads);
-  pl.chunk = cols <= 8 ? 8 : 16;
-  // no more CTAs than give each warp of them a tile
-  const int64_t tiles = (int64_t)B * heads * ceil_div(cols, pl.chunk) * ceil_div(max_len, KV4_TILE), want = ceil_div64(tiles, WARPS);
-  const int most = sms * (pl.chunk == 8 ? 4 : 3);
+  pl.tc = cols > 8;
+  pl.chunk = cols <= 8 ? 8 : cols <= 32 ? 32 : cols <= 64 ? 64 : 128;
+  // no more CTAs than there are tiles for each, or for each warp of them
+  const int64_t items = (int64_t)B * heads * ceil_div(cols, pl.chunk);
+  const int64_t want = pl.tc ? items * ceil_div(max_len, TC_TILE) : ceil_div64(items * ceil_div(max_len, KV4_TILE), WARPS);
+  const int most = pl.tc ? sms : sms * 4;
   pl.ctas = (int)(want < 1 ? 1 : want < most ? want : most);
   return pl;
 }
@@ -608,11 +523,11 @@ cudaError_t launch_attention_kv4(cudaStream_t st, const Kv4AttnArgs &a, int sms)
   p.scale_log2 = a.scale * 1.4426950408889634f; p.part = a.scratch; p.status = a.status;
   Line &ln = p.line;
   ln.B = a.b.B; ln.H = a.c.heads; ln.chunk = pl.chunk; ln.group = a.Hq / a.c.heads; ln.slots = a.c.slots;
-  ln.max_keys = a.max_len < a.c.cap ? a.max_len : a.c.cap; ln.tile_keys = KV4_TILE; ln.b = a.b;
-  const int nt = pl.chunk / 8, cols = a.b.rows * ln.group;
+  ln.max_keys = a.max_len < a.c.cap ? a.max_len : a.c.cap; ln.tile_keys = pl.tc ? TC_TILE : KV4_TILE; ln.b = a.b;
+  const int cols = a.b.rows * ln.group;
   cudaError_t e;
-  if (a.c.dh == 128) e = nt == 1 ? launch_attn<128, 1>(st, p, pl.ctas) : launch_attn<128, 2>(st, p, pl.ctas);
-  else e = nt == 1 ? launch_attn<64, 1>(st, p, pl.ctas) : launch_attn<64, 2>(st, p, pl.ctas);
+  if (pl.tc) e = launch_attention_kv4_tc(st, p, a.c.dh, pl.ctas);
+  else e = a.c.dh == 128 ? launch_attn<128, 1>(st, p, pl.ctas) : launch_attn<64, 1>(st, p, pl.ctas);
   if (e != cudaSuccess) return e;
   return a.c.dh == 128 ? launch_join<128>(st, p, pl.ctas, cols) : launch_join<64>(st, p, pl.ctas, cols);
 }

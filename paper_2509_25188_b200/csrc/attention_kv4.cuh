@@ -1,0 +1,103 @@
+// What the two attention kernels over the 4-bit cache share (internal): the line of work, parameters, partial results.
+#pragma once
+#include "kv4.cuh"
+#include "ptx.cuh"
+
+namespace l2pd {
+namespace kv4 {
+
+constexpr float LAZY = 6.0f;         // log2 units the running maximum may pass the reference
+
+// ---- the line of work --------------------------------------------------------------------------------------------------
+// Items: for sequence b, key heads times chunks of `chunk` columns (those that have rows), tiles_b key tiles each.  Fewer than 2^31
+// tiles in all (the host sees to it).  Every warp surveys the line for itself, a lane a sequence: the lengths and rows of 32
+// sequences are one round of loads.
+struct Seq { int keys, rows, row0, slot, tiles, chunks; uint32_t count; };
+struct Line {
+  int B, H, chunk, group, slots, max_keys, tile_keys;
+  Kv4Batch b;
+  __device__ __forceinline__ Seq seq(int s) const {
+    Seq q = {0, 0, 0, -1, 0, 0, 0u};
+    if (s >= B) return q;
+    const int len = b.keys[s];
+    q.rows = b.n_rows(s); q.row0 = b.row0(s); q.slot = b.slot(s, slots);
+    q.keys = q.slot < 0 ? 0 : max(0, min(len, max_keys));
+    q.tiles = (q.keys + tile_keys - 1) / tile_keys;
+    q.chunks = (q.rows * group + chunk - 1) / chunk;
+    q.count = (uint32_t)H * q.chunks * q.tiles;
+    return q;
+  }
+  // Tiles of the line and of a CTA's run; *before: tiles of the sequences ahead of `upto`.  `own` is seq(lane).  (Whole warp.)
+  // Sequences of one length: whole items where that costs the longest run no more than a fifth, since a split item's halves go
+  // through memory.
+  __device__ uint32_t survey(const Seq &own, uint32_t ctas, int upto, uint32_t *share, uint32_t *before) const {
+    const int lane = threadIdx.x & 31;
+    uint32_t total = 0, ahead = 0, lo = 0xffffffffu, hi = 0;
+    Seq q = own;
+    for (int s0 = 0;;) {
+      total += __reduce_add_sync(0xffffffffu, q.count);
+      ahead += __reduce_add_sync(0xffffffffu, s0 + lane < upto ? q.count : 0u);
+      lo = min(lo, __reduce_min_sync(0xffffffffu, q.chunks ? (uint32_t)q.tiles : 0xffffffffu));
+      hi = max(hi, __reduce_max_sync(0xffffffffu, q.chunks ? (uint32_t)q.tiles : 0u));
+      if ((s0 += 32) >= B) break;
+      q = seq(s0 + lane);
+    }
+    uint32_t even = (total + ctas - 1) / ctas;
+    if (lo == hi && hi) {
+      const uint32_t whole = (total / hi + ctas - 1) / ctas * hi;
+      if (whole <= even + even / 5) even = whole;
+    }
+    *share = even;
+    if (before) *before = ahead;
+    return total;
+  }
+  // The sequence that tile `pos` of the line belongs to, and the tiles before it.  (Whole warp, pos below the line's end.)
+  __device__ Seq find(const Seq &own, uint32_t pos, uint32_t *start) const {
+    const int lane = threadIdx.x & 31;
+    uint32_t run = 0;
+    Seq q = own;
+    for (int s0 = 0;;) {
+      uint32_t x = q.count;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const uint32_t y = __shfl_up_sync(0xffffffffu, x, o);
+        if (lane >= o) x += y;
+      }
+      const unsigned here = __ballot_sync(0xffffffffu, pos < run + x);
+      if (here || s0 + 32 >= B) {
+        const int l = here ? __ffs(here) - 1 : 31;
+        *start = run + __shfl_sync(0xffffffffu, x - q.count, l);
+        Seq r;
+        r.keys = __shfl_sync(0xffffffffu, q.keys, l); r.rows = __shfl_sync(0xffffffffu, q.rows, l);
+        r.row0 = __shfl_sync(0xffffffffu, q.row0, l); r.slot = __shfl_sync(0xffffffffu, q.slot, l);
+        r.tiles = __shfl_sync(0xffffffffu, q.tiles, l); r.chunks = __shfl_sync(0xffffffffu, q.chunks, l);
+        r.count = 0;
+        return r;
+      }
+      run += __shfl_sync(0xffffffffu, x, 31);
+      q = seq((s0 += 32) + lane);
+    }
+  }
+};
+
+struct AttnParams {
+  Kv4View c;
+  Line line;
+  int Hq;
+  const bf16 *q; bf16 *out; float *lse;
+  int64_t q_stride, out_stride;
+  float scale_log2;
+  float *part;             // [2 * CTAs][chunk][dh + 4]: O, M, L of a partial item
+  int32_t *status;
+};
+
+__host__ __device__ constexpr int part_floats(int chunk, int dh) { return chunk * (dh + 4); }
+
+__device__ __forceinline__ void fail(int32_t *status, int code) { if (status) atomicCAS(status, 0, code); }
+
+// attention_kv4_tc.cu: chunks of 32, 64 or 128 columns on tcgen05 (chunk: line.chunk; ctas: at most an SM each)
+cudaError_t launch_attention_kv4_tc(cudaStream_t st, const AttnParams &p, int dh, int ctas);
+constexpr int TC_TILE = 128;         // its key tiles
+
+}  // namespace kv4
+}  // namespace l2pd
