@@ -1,7 +1,7 @@
 // Attention over a key/value cache in 4 bits on the 5th-generation tensor cores, for 9 to 128 columns (query rows times query heads
 // that share a key head) of a sequence and key head at once.
 //
-// S = Q K^T and O += P V, the columns on the M side (128 lanes of tensor memory), tiles of 128 keys.  Two warpgroups turn codes into
+// S = Q K^T and O += P V, the columns on the M side (128 lanes of tensor memory), tiles of 64 keys.  Eight warps turn codes into
 // fp16 operands in shared memory, in the 128-byte swizzle:
 //     K: (c - 8) s 2^-E    exact: c - 8 has three significant bits (or is 8), s has eight.  The rest of the value, a = m + 8 s, reaches the scores
 //        through sixteen further products of depth: (a_hi, a_hi, a_lo) against (sum q_hi, sum q_lo, sum q_hi): no number of a key's
@@ -10,18 +10,20 @@
 // E belongs to 32 keys (a warp).  A code reaches fp16 as it lies, as the subnormal c 2^-24 (or 16 c 2^-24 from bits 4..7), and the
 // multiplication by s 2^24 (2^20) lifts it.  Eight codes of a word come out in the order 0 4 1 5 2 6 3 7: queries are written in that order, and
 // outputs read in it.
-// A softmax thread owns a lane: t = cf 2^E acc + (E_V - E0) - M, P = 2^t as fp16 over the scores, as the A operand of the second
-// product.  M is a reference that follows the running maximum lazily, E0 the largest E_V so far; O is rescaled when one moves.
+// Two groups of four softmax warps take the tiles alternately, each with sums, reference and O of its own, so that one is at its
+// exponentials while the other waits for the tensor pipe; they are added at the end of an item.  A thread owns a lane:
+// t = cf 2^E acc + (E_V - E0) - M, P = 2^t as fp16 over the scores, as the A operand of the second product.  M is a reference that follows
+// the running maximum lazily, E0 the largest E_V so far; O is rescaled when one moves.
 //
 // Fewer columns than lanes: chunks of 32 (64) columns stand four times (twice) in the lanes, and each copy takes its quarter (half) of a
 // tile's keys, its probabilities of the others being 0.  The tensor pipe and shared memory do the same work as for 128 columns, but the
-// exponentials are spread over all four warps; the copies are added at the end.
+// exponentials are spread over all warps; the copies are added at the end.
 //
 // What bounds it: shared memory.  128 keys of 128: 17 KB of codes in and out, 64 KB of operands out and in: 1300 cycles at 128 bytes; the
 // products 1090, the exponentials (128 columns) 1024.
 //
-// Warp roles (512 threads): 0 = copies of codes, 1 = MMA issuer (owns tensor memory), 4-7 softmax and output, 8-11 K, 12-15 V.
-// Tensor memory: S at 0 and 128, O at 256, Q at 384.
+// Warp roles (576 threads): 0-3 and 4-7 softmax and output, 8-11 and 12-15 operands (two warps K, two V), 16 copies of codes, 17 MMA
+// issuer (owns tensor memory).  Tensor memory: S at 0 and 64, O at 128 and 256, Q at 384.
 #include <cuda_fp16.h>
 #include <math.h>
 
@@ -32,20 +34,20 @@ namespace kv4 {
 
 namespace {
 
-constexpr int RING = 3;
-constexpr uint32_t ATOM = 128 * 128;               // 128 rows x 64 fp16
-constexpr int REGS_LEAN = 56, REGS_SOFTMAX = 208, REGS_CODES = 104;   // 128 (56 + 208 + 2 x 104) of 512 x 128
+constexpr int RING = 5, NB = 4;                    // tiles of codes on their way; operand buffers
+constexpr uint32_t ATOM = TC_TILE * 128;           // 64 rows x 64 fp16
 constexpr int NONE = -1000;                        // no exponent
-constexpr int LDS_O = 36;                          // floats of a staged row of 32
+constexpr int LDS_O = 20;                          // floats of a staged row of 16
+constexpr int SOFTMAX = 256, THREADS = 576;
 
 template <int DH> struct Tc {
-  static constexpr int ATOMS = DH / 64, TILE32 = KV4_TILE * (DH + 8), STAGE = 4 * TILE32;
-  static constexpr uint32_t K = 0, AUG = 2 * ATOMS * ATOM, V = AUG + ATOM, CODES = V + 2 * ATOMS * ATOM,
-                            STAGING = CODES + RING * STAGE, BYTES = STAGING + 128 * LDS_O * 4;
+  static constexpr int ATOMS = DH / 64, TILE32 = KV4_TILE * (DH + 8), STAGE = 2 * TILE32;
+  static constexpr uint32_t K = 0, AUG = NB * ATOMS * ATOM, V = AUG + ATOM, CODES = V + NB * ATOMS * ATOM,
+                            STAGING = CODES + RING * STAGE, BYTES = STAGING + 2 * 128 * LDS_O * 4;
 };
 
-enum { B_FULL = 0, B_EMPTY = B_FULL + RING, B_KRDY = B_EMPTY + RING, B_KFREE = B_KRDY + 2, B_VRDY = B_KFREE + 2, B_VFREE = B_VRDY + 2,
-       B_SFULL = B_VFREE + 2, B_PRDY = B_SFULL + 2, B_QRDY = B_PRDY + 2, B_OFREE = B_QRDY + 1, B_COUNT = B_OFREE + 1 };
+enum { B_FULL = 0, B_EMPTY = B_FULL + RING, B_KRDY = B_EMPTY + RING, B_KFREE = B_KRDY + NB, B_VRDY = B_KFREE + NB, B_VFREE = B_VRDY + NB,
+       B_SFULL = B_VFREE + NB, B_PRDY = B_SFULL + 2, B_QRDY = B_PRDY + 2, B_OFREE = B_QRDY + 1, B_COUNT = B_OFREE + 1 };
 
 __device__ __forceinline__ float pow2(int n) { return __uint_as_float((uint32_t)(127 + n) << 23); }   // -126 <= n <= 127
 // x 2^n for n beyond one exponent's range
@@ -57,7 +59,7 @@ __device__ __forceinline__ uint32_t hfma2(uint32_t a, uint32_t b, uint32_t c) {
   asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(d) : "r"(a), "r"(b), "r"(c));
   return d;
 }
-__device__ __forceinline__ void softmax_sync() { asm volatile("bar.sync 1, 128;" ::: "memory"); }
+__device__ __forceinline__ void softmax_sync() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
 
 // One row of codes to its fp16 row: value = c s + o, s and o given times the powers of two above.  `row` and `out`: shared
 // addresses of the codes and of the row in its first atom, r: the tile row.  The quarters of a row are read in an order that
@@ -80,37 +82,40 @@ __device__ __forceinline__ void unpack_row(uint32_t row, uint32_t out, int r, ui
   }
 }
 
-template <int DH>
-__global__ void __launch_bounds__(512, 1) attention_kv4_tc_kernel(const AttnParams p) {
+template <int DH, int COPIES>
+__global__ void __launch_bounds__(THREADS, 1) attention_kv4_tc_kernel(const AttnParams p) {
   using T = Tc<DH>;
+  constexpr int CHUNK = 128 / COPIES, NK = TC_TILE / COPIES;   // columns; keys of a tile that a copy takes
   extern __shared__ uint8_t smem_raw[];
   __shared__ __align__(8) uint64_t bars[B_COUNT];
   __shared__ uint32_t tmem_slot;
   __shared__ int abort_flag;
-  // exponents of a tile's four groups of 32 keys.  K runs ahead of the softmax: its buffer is free once the scores are there
-  __shared__ int expo_k[4][4], expo_v[2][4];
+  // exponents of a tile's two groups of 32 keys.  K runs ahead of the softmax: its buffer is free once the scores are there
+  __shared__ int expo_k[2 * NB][2], expo_v[NB][2];
   __shared__ int lost;                             // a softmax warp's wait ran out
-  __shared__ float2 ml[128];                       // a lane's reference and sum
+  __shared__ float2 ml[2][128];                    // a lane's reference and sum
+  __shared__ float q_factor[128];
   const int warp = ptx::warp_index(), lane = threadIdx.x & 31;
   const uint32_t base = (ptx::smem_u32(smem_raw) + 1023u) & ~1023u;
   const uint32_t bar0 = ptx::smem_u32(bars);
   auto bar = [&](int i) { return bar0 + 8u * i; };
   if (threadIdx.x == 0) {
-    for (int i = 0; i < RING; ++i) { ptx::mbar_init(bar(B_FULL + i), 1); ptx::mbar_init(bar(B_EMPTY + i), 8); }
-    for (int i = 0; i < 2; ++i) {
-      ptx::mbar_init(bar(B_KRDY + i), 4); ptx::mbar_init(bar(B_KFREE + i), 1); ptx::mbar_init(bar(B_VRDY + i), 4);
-      ptx::mbar_init(bar(B_VFREE + i), 1); ptx::mbar_init(bar(B_SFULL + i), 2); ptx::mbar_init(bar(B_PRDY + i), 4);
+    for (int i = 0; i < RING; ++i) { ptx::mbar_init(bar(B_FULL + i), 1); ptx::mbar_init(bar(B_EMPTY + i), 4); }
+    for (int i = 0; i < NB; ++i) {
+      ptx::mbar_init(bar(B_KRDY + i), 2); ptx::mbar_init(bar(B_KFREE + i), 1);
+      ptx::mbar_init(bar(B_VRDY + i), 2); ptx::mbar_init(bar(B_VFREE + i), 1);
     }
-    ptx::mbar_init(bar(B_QRDY), 4); ptx::mbar_init(bar(B_OFREE), 4);
+    for (int i = 0; i < 2; ++i) { ptx::mbar_init(bar(B_SFULL + i), 2); ptx::mbar_init(bar(B_PRDY + i), 4); }
+    ptx::mbar_init(bar(B_QRDY), 4); ptx::mbar_init(bar(B_OFREE), 8);
     abort_flag = 0; lost = 0;
     ptx::fence_barrier_init();
     ptx::fence_proxy_async();
   }
-  if (warp == 1) { ptx::tmem_alloc(ptx::smem_u32(&tmem_slot), 512); ptx::tmem_relinquish(); }
+  if (warp == 17) { ptx::tmem_alloc(ptx::smem_u32(&tmem_slot), 512); ptx::tmem_relinquish(); }
   ptx::tc_fence_before_sync();
   __syncthreads();
   ptx::tc_fence_after_sync();
-  const uint32_t tS = tmem_slot, tO = tS + 256, tQ = tS + 384;
+  const uint32_t tS = tmem_slot, tO = tS + 128, tQ = tS + 384;
   int32_t *const status = p.status;
   grid_dep_launch();
   grid_dep_wait();
@@ -129,103 +134,97 @@ __global__ void __launch_bounds__(512, 1) attention_kv4_tc_kernel(const AttnPara
     const int item = (int)((pos - before) / sq.tiles);
     w.nt = sq.tiles; w.t0 = (int)(pos - before) - item * sq.tiles;
     w.t1 = (int)min((uint32_t)sq.tiles, w.t0 + (end - pos));
-    w.h = item / sq.chunks; w.c0 = (item - w.h * sq.chunks) * ln.chunk; w.cols = min(ln.chunk, sq.rows * ln.group - w.c0);
+    w.h = item / sq.chunks; w.c0 = (item - w.h * sq.chunks) * CHUNK; w.cols = min(CHUNK, sq.rows * ln.group - w.c0);
     w.keys = sq.keys; w.row0 = sq.row0; w.slot = sq.slot;
     return w;
   };
 
-  if (warp < 4) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(REGS_LEAN));
-    if (warp == 0) {
-      // ---------------------------------------------------------------- codes: up to four tiles of the cache, one contiguous piece
-      int slot = 0;
-      uint32_t par = 1;
-      for (uint32_t pos = begin; pos < end;) {
-        const Piece w = piece_at(pos);
-        const uint8_t *src = p.c.tile(w.slot, w.h, 0);
-        for (int t = w.t0; t < w.t1; ++t) {
-          const bool ok = ptx::mbar_wait_or_abort(bar(B_EMPTY + slot), par, &abort_flag, status, DEV_TIMEOUT_PRODUCER);
-          const uint32_t bytes = min(4, (w.keys - t * TC_TILE + KV4_TILE - 1) / KV4_TILE) * T::TILE32;
-          if (ptx::elect_one() && ok) {
-            ptx::mbar_arrive_expect_tx(bar(B_FULL + slot), bytes);
-            ptx::bulk_load(base + T::CODES + slot * T::STAGE, src + (int64_t)t * T::STAGE, bytes, bar(B_FULL + slot));
-          }
-          if (++slot == RING) { slot = 0; par ^= 1u; }
-        }
-        pos += w.t1 - w.t0;
-      }
-    } else if (warp == 1) {
-      // ---------------------------------------------------------------- MMA issuer: S(0) S(1) PV(0) S(2) PV(1) ...
-      constexpr uint32_t F32 = 1u << 4, M128 = (128u >> 4) << 24;
-      const uint32_t idesc_s = F32 | M128 | ((128u >> 3) << 17), idesc_o = F32 | M128 | ((DH >> 3) << 17) | (1u << 16);
-      uint32_t ts = 0, tp = 0, qpar = 0, opar = 1;   // tiles whose S, whose PV was issued
-      auto scores = [&]() {
-        const uint32_t b = ts & 1u, par = (ts >> 1) & 1u;
-        const bool ok = ptx::mbar_wait_or_abort(bar(B_KRDY + b), par, &abort_flag, status, DEV_TIMEOUT_MMA);
-        ptx::tc_fence_after_sync();
-        const uint64_t kd = ptx::smem_desc_sw128(base + T::K + b * T::ATOMS * ATOM), ad = ptx::smem_desc_sw128(base + T::AUG) + 2u * b;
+  if (warp == 16) {
+    // ------------------------------------------------------------------ codes: one or two tiles of the cache, one contiguous piece
+    int slot = 0;
+    uint32_t par = 1;
+    for (uint32_t pos = begin; pos < end;) {
+      const Piece w = piece_at(pos);
+      const uint8_t *src = p.c.tile(w.slot, w.h, 0);
+      for (int t = w.t0; t < w.t1; ++t) {
+        const bool ok = ptx::mbar_wait_or_abort(bar(B_EMPTY + slot), par, &abort_flag, status, DEV_TIMEOUT_PRODUCER);
+        const uint32_t bytes = min(2, (w.keys - t * TC_TILE + KV4_TILE - 1) / KV4_TILE) * T::TILE32;
         if (ptx::elect_one() && ok) {
-#pragma unroll
-          for (int k = 0; k < DH / 16; ++k)
-            ptx::mma_bf16_ts(tS + b * 128, tQ + 8 * k, kd + (k >> 2) * (ATOM >> 4) + 2u * (k & 3), idesc_s, k ? 1u : 0u);
-          ptx::mma_bf16_ts(tS + b * 128, tQ + DH / 2, ad, idesc_s, 1u);
-          ptx::mma_commit(bar(B_KFREE + b));
-          ptx::mma_commit(bar(B_SFULL + b));
-          ptx::mbar_arrive(bar(B_SFULL + b));        // passes on what the K warps wrote besides
+          ptx::mbar_arrive_expect_tx(bar(B_FULL + slot), bytes);
+          ptx::bulk_load(base + T::CODES + slot * T::STAGE, src + (int64_t)t * T::STAGE, bytes, bar(B_FULL + slot));
         }
-        ++ts;
-      };
-      auto output = [&](bool first) {
-        const uint32_t b = tp & 1u, par = (tp >> 1) & 1u;
-        bool ok = ptx::mbar_wait_or_abort(bar(B_VRDY + b), par, &abort_flag, status, DEV_TIMEOUT_MMA);
-        if (first) {                               // the piece before has been read out of O
-          ok = ptx::mbar_wait_or_abort(bar(B_OFREE), opar, &abort_flag, status, DEV_TIMEOUT_MMA) && ok;
-          opar ^= 1u;
-        }
-        ok = ptx::mbar_wait_or_abort(bar(B_PRDY + b), par, &abort_flag, status, DEV_TIMEOUT_MMA) && ok;
-        ptx::tc_fence_after_sync();
-        const uint64_t vd = ptx::smem_desc_sw128_mn(base + T::V + b * T::ATOMS * ATOM, ATOM);
-        if (ptx::elect_one() && ok) {
-#pragma unroll
-          for (int k = 0; k < TC_TILE / 16; ++k)
-            ptx::mma_bf16_ts(tO, tS + b * 128 + 8 * k, vd + k * (2048u >> 4), idesc_o, k ? 1u : first ? 0u : 1u);
-          ptx::mma_commit(bar(B_VFREE + b));
-        }
-        ++tp;
-      };
-      int behind = 0;                              // the tile whose second product is still to come: 1, 2 = the first of its piece
-      for (uint32_t pos = begin; pos < end;) {
-        const Piece w = piece_at(pos);
-        ptx::mbar_wait_or_abort(bar(B_QRDY), qpar, &abort_flag, status, DEV_TIMEOUT_MMA);
-        qpar ^= 1u;
-        for (int t = w.t0; t < w.t1; ++t) {
-          scores();
-          if (behind) output(behind == 2);
-          behind = t == w.t0 ? 2 : 1;
-        }
-        // the next piece's queries come after this piece's last probabilities
-        if (behind) output(behind == 2);
-        behind = 0;
-        pos += w.t1 - w.t0;
+        if (++slot == RING) { slot = 0; par ^= 1u; }
       }
+      pos += w.t1 - w.t0;
+    }
+  } else if (warp == 17) {
+    // ------------------------------------------------------------------ MMA issuer: S(0) S(1) PV(0) S(2) PV(1) S(3) ...
+    constexpr uint32_t F32 = 1u << 4, M128 = (128u >> 4) << 24;
+    const uint32_t idesc_s = F32 | M128 | ((TC_TILE >> 3) << 17), idesc_o = F32 | M128 | ((DH >> 3) << 17) | (1u << 16);
+    uint32_t ts = 0, tp = 0, qpar = 0, opar = 1;     // tiles whose S, whose PV was issued
+    auto scores = [&]() {
+      const uint32_t b = ts % NB, g = ts & 1u;
+      const bool ok = ptx::mbar_wait_or_abort(bar(B_KRDY + b), (ts / NB) & 1u, &abort_flag, status, DEV_TIMEOUT_MMA);
+      ptx::tc_fence_after_sync();
+      const uint64_t kd = ptx::smem_desc_sw128(base + T::K + b * T::ATOMS * ATOM), ad = ptx::smem_desc_sw128(base + T::AUG) + 2u * b;
+      if (ptx::elect_one() && ok) {
+#pragma unroll
+        for (int k = 0; k < DH / 16; ++k)
+          ptx::mma_bf16_ts(tS + g * TC_TILE, tQ + 8 * k, kd + (k >> 2) * (ATOM >> 4) + 2u * (k & 3), idesc_s, k ? 1u : 0u);
+        ptx::mma_bf16_ts(tS + g * TC_TILE, tQ + DH / 2, ad, idesc_s, 1u);
+        ptx::mma_commit(bar(B_KFREE + b));
+        ptx::mma_commit(bar(B_SFULL + g));
+        ptx::mbar_arrive(bar(B_SFULL + g));          // passes on what the K warps wrote besides
+      }
+      ++ts;
+    };
+    auto output = [&](bool first, bool wait_o) {
+      const uint32_t b = tp % NB, g = tp & 1u;
+      bool ok = ptx::mbar_wait_or_abort(bar(B_VRDY + b), (tp / NB) & 1u, &abort_flag, status, DEV_TIMEOUT_MMA);
+      if (wait_o) {                                  // the piece before has been read out of O
+        ok = ptx::mbar_wait_or_abort(bar(B_OFREE), opar, &abort_flag, status, DEV_TIMEOUT_MMA) && ok;
+        opar ^= 1u;
+      }
+      ok = ptx::mbar_wait_or_abort(bar(B_PRDY + g), (tp >> 1) & 1u, &abort_flag, status, DEV_TIMEOUT_MMA) && ok;
+      ptx::tc_fence_after_sync();
+      const uint64_t vd = ptx::smem_desc_sw128_mn(base + T::V + b * T::ATOMS * ATOM, ATOM);
+      if (ptx::elect_one() && ok) {
+#pragma unroll
+        for (int k = 0; k < TC_TILE / 16; ++k)
+          ptx::mma_bf16_ts(tO + g * 128, tS + g * TC_TILE + 8 * k, vd + k * (2048u >> 4), idesc_o, k ? 1u : first ? 0u : 1u);
+        ptx::mma_commit(bar(B_VFREE + b));
+      }
+      ++tp;
+    };
+    for (uint32_t pos = begin; pos < end;) {
+      const Piece w = piece_at(pos);
+      const int n = w.t1 - w.t0;
+      ptx::mbar_wait_or_abort(bar(B_QRDY), qpar, &abort_flag, status, DEV_TIMEOUT_MMA);
+      qpar ^= 1u;
+      scores();
+      if (n > 1) scores();
+      for (int i = 0; i < n; ++i) {
+        output(i < 2, i == 0);
+        if (i + 2 < n) scores();
+      }
+      pos += n;
     }
   } else if (warp >= 8) {
-    // ------------------------------------------------------------------ codes to operands
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(REGS_CODES));
-    const bool is_v = warp >= 12;
-    const int grp = warp & 3, r = 32 * grp + lane, swz = is_v ? kv4_v_swizzle(lane, DH) : 0;
+    // ------------------------------------------------------------------ codes to operands: every other tile
+    const bool is_v = warp & 2;
+    const int grp = warp & 1, r = 32 * grp + lane, swz = is_v ? kv4_v_swizzle(lane, DH) : 0;
     const uint32_t out = base + (is_v ? T::V : T::K) + r * 128, aug = base + T::AUG + r * 128;
     const uint32_t row_off = grp * T::TILE32 + (is_v ? kv4_off_v(DH) : 0) + lane * (DH / 2);
     const uint32_t meta_off = grp * T::TILE32 + (is_v ? kv4_off_vmeta(DH) : kv4_off_kmeta(DH)) + 4 * lane;
-    int slot = 0;
-    uint32_t par = 0, tile = 0;
+    uint32_t tile = 0;
     bool ok = true;
     for (uint32_t pos = begin; pos < end && ok;) {
       const Piece w = piece_at(pos);
       for (int t = w.t0; t < w.t1 && ok; ++t, ++tile) {
-        const uint32_t b = tile & 1u;
-        ok = ptx::mbar_wait_warp(bar(B_FULL + slot), par);
-        ok = ok && ptx::mbar_wait_warp(bar((is_v ? B_VFREE : B_KFREE) + b), ((tile >> 1) & 1u) ^ 1u);
+        if ((tile & 1u) != (uint32_t)(warp >= 12)) continue;
+        const uint32_t b = tile % NB, slot = tile % RING;
+        ok = ptx::mbar_wait_warp(bar(B_FULL + slot), (tile / RING) & 1u);
+        ok = ok && ptx::mbar_wait_warp(bar((is_v ? B_VFREE : B_KFREE) + b), ((tile / NB) & 1u) ^ 1u);
         if (!ok) break;
         const uint32_t stage = base + T::CODES + slot * T::STAGE;
         uint32_t meta = 0;
@@ -237,7 +236,7 @@ __global__ void __launch_bounds__(512, 1) attention_kv4_tc_kernel(const AttnPara
         const bool none = is_v && __all_sync(0xffffffffu, (meta & 0x7fff7fffu) == 0u);   // values that are all 0 have no exponent
         e = max((int)__reduce_max_sync(0xffffffffu, (uint32_t)max(e, 0)) - 126, -100);
         if (is_v) {
-          e += 1;                                  // |value| < 2^e; as fp16 times 2^-(e + 5)
+          e += 1;                                    // |value| < 2^e; as fp16 times 2^-(e + 5)
           const float s1 = scaled(s, -(e + 5)), m1 = scaled(m, -(e + 5));
           unpack_row<DH>(stage + row_off, out + b * T::ATOMS * ATOM, r, dup(s1 * 16777216.f), dup(s1 * 1048576.f), dup(m1), swz);
         } else {
@@ -249,7 +248,7 @@ __global__ void __launch_bounds__(512, 1) attention_kv4_tc_kernel(const AttnPara
           ptx::st_shared_v4(at ^ 16u, make_uint4(0u, 0u, 0u, 0u));
         }
         if (lane == 0) {
-          if (is_v) expo_v[b][grp] = none ? NONE : e; else expo_k[tile & 3u][grp] = e;
+          if (is_v) expo_v[b][grp] = none ? NONE : e; else expo_k[tile % (2 * NB)][grp] = e;
         }
         ptx::fence_proxy_async();
         __syncwarp();
@@ -257,25 +256,23 @@ __global__ void __launch_bounds__(512, 1) attention_kv4_tc_kernel(const AttnPara
           ptx::mbar_arrive(bar((is_v ? B_VRDY : B_KRDY) + b));
           ptx::mbar_arrive(bar(B_EMPTY + slot));
         }
-        if (++slot == RING) { slot = 0; par ^= 1u; }
       }
       pos += w.t1 - w.t0;
     }
     if (!ok) { fail(status, DEV_TIMEOUT_PRODUCER); abort_flag = 1; }
   } else {
     // ------------------------------------------------------------------ queries, softmax, output
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(REGS_SOFTMAX));
-    const int q = warp & 3, row = 32 * q + lane, chunk = ln.chunk, copies = 128 / chunk;
-    const int col = row & (chunk - 1);               // this lane's column of the chunk
-    const int g0 = q / (4 / copies) * (4 / copies), ng = 4 / copies;   // its first group of 32 keys, and how many
-    const uint32_t lane_base = (uint32_t)(32 * q) << 16;
+    const int g = warp >> 2, q = warp & 3, row = 32 * q + lane;
+    const int col = row & (CHUNK - 1);               // this lane's column of the chunk
+    const int k0 = q / (4 / COPIES) * NK;            // first key of a tile that it takes
+    constexpr int NG = NK > 32 ? NK / 32 : 1, GK = NK / NG;   // its groups of one exponent, their keys
+    const uint32_t lane_base = (uint32_t)(32 * q) << 16, tSg = tS + lane_base + g * TC_TILE, tOg = tO + lane_base + g * 128;
     uint32_t tile = 0;
     bool ok = true;
     for (uint32_t pos = begin; pos < end;) {
       const Piece w = piece_at(pos);
-      // queries to tensor memory: the largest of a row becomes 2^7 .. 2^8
-      float cf;
-      {
+      if (g == 0) {
+        // queries to tensor memory: the largest of a row becomes 2^7 .. 2^8
         const int c = w.c0 + col, rr = c / ln.group;
         const bool there = col < w.cols;
         const bf16 *src = p.q + (int64_t)(w.row0 + rr) * p.q_stride + (int64_t)(w.h * ln.group + c - rr * ln.group) * DH;
@@ -288,11 +285,10 @@ __global__ void __launch_bounds__(512, 1) attention_kv4_tc_kernel(const AttnPara
 #pragma unroll
         for (int j = 0; j < DH / 2; ++j) top = max(top, max((raw[j] << 16) & 0x7fffffffu, raw[j] & 0x7fff0000u));
         const bool finite = top < 0x7f800000u;
-        const int u = min(7 - ((int)(top >> 23) - 127), 126);
-        const float up = pow2(finite ? u : 0);
-        cf = p.scale_log2 * pow2(finite ? -u : 0);
+        const int u = finite ? min(7 - ((int)(top >> 23) - 127), 126) : 0;
+        const float up = pow2(u);
+        q_factor[row] = p.scale_log2 * pow2(-u);
         float sum = 0.f;
-        uint32_t f[DH / 2];
 #pragma unroll
         for (int j = 0; j < DH / 8; ++j) {
           float y[8];
@@ -303,210 +299,196 @@ __global__ void __launch_bounds__(512, 1) attention_kv4_tc_kernel(const AttnPara
             sum += y[2 * i] + y[2 * i + 1];
           }
 #pragma unroll
-          for (int i = 0; i < 4; ++i) f[4 * j + i] = pair(y[i], y[i + 4]);
+          for (int i = 0; i < 4; ++i) raw[4 * j + i] = pair(y[i], y[i + 4]);
         }
 #pragma unroll
-        for (int j = 0; j < DH / 2; j += 32) ptx::tmem_st_x32(tQ + lane_base + j, f + j);
-        uint32_t z[32];
+        for (int j = 0; j < DH / 2; j += 32) ptx::tmem_st_x32(tQ + lane_base + j, raw + j);
         const float hi = __half2float(__float2half_rn(sum));
-        z[0] = finite ? pair(hi, sum - hi) : 0x7fff7fffu;            // a NaN here makes every score of the row NaN
-        z[1] = pair(hi * (1.f / 2048.f), 0.f);
+        raw[0] = finite ? pair(hi, sum - hi) : 0x7fff7fffu;          // a NaN here makes every score of the row NaN
+        raw[1] = pair(hi * (1.f / 2048.f), 0.f);
 #pragma unroll
-        for (int i = 2; i < 32; ++i) z[i] = 0u;
-        ptx::tmem_st_x32(tQ + lane_base + DH / 2, z);
+        for (int i = 2; i < 32; ++i) raw[i] = 0u;
+        ptx::tmem_st_x32(tQ + lane_base + DH / 2, raw);
         ptx::tmem_st_wait();
         ptx::tc_fence_before_sync();
         __syncwarp();
         if (lane == 0) ptx::mbar_arrive(bar(B_QRDY));
       }
+      softmax_sync();
+      const float cf = q_factor[row];
       float m_ref = 0.f, l = 0.f;
       int e0 = NONE;
+      uint32_t last_v = 0;                           // this group's tile before, plus one
       bool first = true;
       for (int t = w.t0; t < w.t1 && ok; ++t, ++tile) {
-        const uint32_t b = tile & 1u, par = (tile >> 1) & 1u;
+        if ((tile & 1u) != (uint32_t)g) continue;
         // the exponents of V come with its operands
-        ok = ptx::mbar_wait_warp(bar(B_VRDY + b), par);
-        ok = ok && ptx::mbar_wait_warp(bar(B_SFULL + b), par);
+        ok = ptx::mbar_wait_warp(bar(B_VRDY + tile % NB), (tile / NB) & 1u);
+        ok = ok && ptx::mbar_wait_warp(bar(B_SFULL + g), (tile >> 1) & 1u);
         if (!ok) break;
         ptx::tc_fence_after_sync();
-        const uint32_t tSb = tS + lane_base + b * 128;
-        const int left = w.keys - t * TC_TILE;
-        int e_top = NONE, ek[4], ev[4];
+        uint32_t s[NK];
+        if (NK == 16) ptx::tmem_ld_x16(tSg + k0, s);
+        else {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          ek[i] = i < ng ? expo_k[tile & 3u][g0 + i] : 0;
-          ev[i] = i < ng ? expo_v[b][g0 + i] : NONE;
-          e_top = max(e_top, ev[i]);
+          for (int i = 0; i < NK; i += 32) ptx::tmem_ld_x32(tSg + k0 + i, s + i);
         }
-        float fac = 1.f;
-        if (e_top > e0) {                            // warp-uniform
-          fac = first ? 0.f : pow2(max(e0 - (e_top + 2), -126));
-          e0 = e_top + 2;
+        float k[NG], o[NG], w_of[NG], fac = 1.f;
+        {
+          int ek[NG], ev[NG], e_top = NONE;
+#pragma unroll
+          for (int i = 0; i < NG; ++i) {
+            ek[i] = expo_k[tile % (2 * NB)][(k0 >> 5) + i];
+            ev[i] = expo_v[tile % NB][(k0 >> 5) + i];
+            e_top = max(e_top, ev[i]);
+          }
+          if (e_top > e0) {                          // warp-uniform
+            fac = first ? 0.f : pow2(max(e0 - (e_top + 2), -126));
+            e0 = e_top + 2;
+          }
+#pragma unroll
+          for (int i = 0; i < NG; ++i) {
+            const int e = ev[i] == NONE ? 0 : max(ev[i] - e0, -120);
+            k[i] = scaled(cf, ek[i] + 9); o[i] = (float)e - m_ref; w_of[i] = pow2(-e);
+          }
         }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) ev[i] = ev[i] == NONE ? 0 : max(ev[i] - e0, -120);   // from here on relative to e0
-        uint32_t s[128];
-        float top = -INFINITY;
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if (i < ng) ptx::tmem_ld_x32(tSb + 32 * (g0 + i), s + 32 * i);
+        const int left = w.keys - t * TC_TILE - k0;
         ptx::tmem_ld_wait();
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if (i < ng) {
-            const float k = scaled(cf, ek[i] + 9), o = (float)ev[i] - m_ref;
+        for (int j = 0; j < NK; ++j) s[j] = __float_as_uint(fmaf(__uint_as_float(s[j]), k[j / GK], o[j / GK]));
+        if (left < NK) {
 #pragma unroll
-            for (int j = 0; j < 32; ++j) {
-              const float x = fmaf(__uint_as_float(s[32 * i + j]), k, o);
-              s[32 * i + j] = __float_as_uint(x);
-            }
-            if (left < TC_TILE) {
+          for (int j = 0; j < NK; ++j) if (j >= left) s[j] = 0xff800000u;
+        }
+        float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-              for (int j = 0; j < 32; ++j) if (32 * (g0 + i) + j >= left) s[32 * i + j] = 0xff800000u;
-            }
+        for (int j = 0; j < NK; j += 4)
 #pragma unroll
-            for (int j = 0; j < 32; ++j) top = fmaxf(top, __uint_as_float(s[32 * i + j]));
-          }
+          for (int e = 0; e < 4; ++e) mx[e] = fmaxf(mx[e], __uint_as_float(s[j + e]));
+        const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
         // a copy whose keys all lie behind the end keeps an open reference
         const bool grow = first ? top > -INFINITY : top > LAZY;
-        float d = 0.f;
-        if (grow) {
-          d = top;
-          m_ref += d;
-          if (first) fac = 0.f; else { const float x = ptx::ex2(-d); fac *= x; l *= x; }
-        }
         if (__any_sync(0xffffffffu, grow)) {
+          const float d = grow ? top : 0.f;
+          m_ref += d;
+          const float x = first ? 0.f : ptx::ex2(-d);
+          fac *= x; l *= x;
 #pragma unroll
-          for (int i = 0; i < 4; ++i)
-            if (i < ng) {
-#pragma unroll
-              for (int j = 0; j < 32; ++j) s[32 * i + j] = __float_as_uint(__uint_as_float(s[32 * i + j]) - d);
-            }
-        }
-        const bool rescale = t > w.t0 && fac != 1.f;
-        // probabilities
-        uint32_t pk[64];
-#pragma unroll
-        for (int j = 0; j < 64; ++j) pk[j] = 0u;
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if (i < ng) {
-            float sum[2] = {0.f, 0.f};
-#pragma unroll
-            for (int j = 0; j < 32; j += 2) {
-              const float p0 = ptx::ex2(__uint_as_float(s[32 * i + j])), p1 = ptx::ex2(__uint_as_float(s[32 * i + j + 1]));
-              sum[(j >> 1) & 1] += p0 + p1;
-              pk[16 * i + (j >> 1)] = pair(p0, p1);
-            }
-            l = fmaf(sum[0] + sum[1], pow2(-ev[i]), l);
-          }
-        if (ng == 4) {
-          ptx::tmem_st_x32(tSb, pk);
-          ptx::tmem_st_x32(tSb + 32, pk + 32);
-        } else {
-          // zeros where the other copies' keys are
-          uint32_t z[32];
-#pragma unroll
-          for (int j = 0; j < 32; ++j) z[j] = 0u;
-          if (ng == 2) {
-            ptx::tmem_st_x32(tSb + 16 * g0, pk);
-            ptx::tmem_st_x32(tSb + (32 - 16 * g0), z);
-          } else {
-            // 16 columns of its own in one of the two halves
-            const bool up = g0 & 1;
-#pragma unroll
-            for (int j = 0; j < 16; ++j) { z[j] = up ? 0u : pk[j]; z[j + 16] = up ? pk[j] : 0u; }
-            ptx::tmem_st_x32(tSb + (g0 >> 1) * 32, z);
-#pragma unroll
-            for (int j = 0; j < 32; ++j) z[j] = 0u;
-            ptx::tmem_st_x32(tSb + (32 - (g0 >> 1) * 32), z);
-          }
+          for (int j = 0; j < NK; ++j) s[j] = __float_as_uint(__uint_as_float(s[j]) - d);
         }
         first = first && !(top > -INFINITY);
+        // probabilities
+        float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int j = 0; j < NK; j += 2) {
+          const float p0 = ptx::ex2(__uint_as_float(s[j])), p1 = ptx::ex2(__uint_as_float(s[j + 1]));
+          float &acc = sum[NG == 2 ? 2 * (j / GK) + ((j >> 1) & 1) : (j >> 1) & 3];
+          acc += p0 + p1;
+          s[j >> 1] = pair(p0, p1);
+        }
+        if (NG == 2) l = fmaf(sum[2] + sum[3], w_of[NG - 1], fmaf(sum[0] + sum[1], w_of[0], l));
+        else l = fmaf((sum[0] + sum[1]) + (sum[2] + sum[3]), w_of[0], l);
+        if (COPIES == 1) ptx::tmem_st_x32(tSg, s);
+        else {
+          // zeros where the other copies' keys are
+          constexpr int OWN = NK / 2;
+          uint32_t z[32];
+#pragma unroll
+          for (int j = 0; j < 32; ++j) z[j] = j / OWN == k0 / NK ? s[j % OWN] : 0u;
+          ptx::tmem_st_x32(tSg, z);
+        }
+        const bool rescale = last_v && fac != 1.f;
         if (__any_sync(0xffffffffu, rescale)) {
-          ok = ptx::mbar_wait_warp(bar(B_VFREE + ((tile - 1) & 1u)), ((tile - 1) >> 1) & 1u);
+          ok = ptx::mbar_wait_warp(bar(B_VFREE + (last_v - 1) % NB), ((last_v - 1) / NB) & 1u);
           ptx::tc_fence_after_sync();
 #pragma unroll
-          for (int i = 0; i < DH; i += 32) {
-            uint32_t v[32];
-            ptx::tmem_ld_x32(tO + lane_base + i, v);
+          for (int i = 0; i < DH; i += 16) {
+            uint32_t v[16];
+            ptx::tmem_ld_x16(tOg + i, v);
             ptx::tmem_ld_wait();
 #pragma unroll
-            for (int j = 0; j < 32; ++j) v[j] = __float_as_uint(__uint_as_float(v[j]) * (rescale ? fac : 1.f));
-            ptx::tmem_st_x32(tO + lane_base + i, v);
+            for (int j = 0; j < 16; ++j) v[j] = __float_as_uint(__uint_as_float(v[j]) * (rescale ? fac : 1.f));
+            ptx::tmem_st_x16(tOg + i, v);
           }
         }
+        last_v = tile + 1;
         ptx::tmem_st_wait();
         ptx::tc_fence_before_sync();
         __syncwarp();
-        if (lane == 0) ptx::mbar_arrive(bar(B_PRDY + b));
+        if (lane == 0) ptx::mbar_arrive(bar(B_PRDY + g));
       }
-      // ---------------------------------------------------------------- the copies of a column meet; 32 dimensions at a time
-      ml[row] = make_float2(first ? -INFINITY : m_ref, l);
+      // ---------------------------------------------------------------- groups and copies of a column meet; 16 dimensions at a time
+      ml[g][row] = make_float2(first ? -INFINITY : m_ref, l);
+      if (last_v && ok) ok = ptx::mbar_wait_warp(bar(B_VFREE + (last_v - 1) % NB), ((last_v - 1) / NB) & 1u);
       if (!ok) lost = 1;
       softmax_sync();
-      if (lost) break;                               // all four warps or none: they meet at barriers
+      if (lost) break;                               // all eight warps or none: they meet at barriers
       float m = -INFINITY, sum = 0.f;
-      for (int i = 0; i < copies; ++i) m = fmaxf(m, ml[col + i * chunk].x);
-      for (int i = 0; i < copies; ++i) {
-        const float2 x = ml[col + i * chunk];
+#pragma unroll
+      for (int i = 0; i < 2 * COPIES; ++i) m = fmaxf(m, ml[i & 1][col + (i >> 1) * CHUNK].x);
+#pragma unroll
+      for (int i = 0; i < 2 * COPIES; ++i) {
+        const float2 x = ml[i & 1][col + (i >> 1) * CHUNK];
         sum = fmaf(x.y, x.x == -INFINITY ? 0.f : ptx::ex2(x.x - m), sum);
       }
       const bool whole = w.t0 == 0 && w.t1 == w.nt;
-      // the lane's own factor: to the common reference, to the values' unit, and the quotient where the item is whole
+      // the lane's own factor: to the common reference, and the quotient where the item is whole
       const float own_f = (first ? 0.f : ptx::ex2(m_ref - m)) * (whole ? 1.f / sum : 1.f);
-      float *part = p.part + (int64_t)(2 * blockIdx.x + (w.t0 == 0 ? 1 : 0)) * part_floats(chunk, DH);
-      if (row < w.cols) {                            // of the first copy
+      float *part = p.part + (int64_t)(2 * blockIdx.x + (w.t0 == 0 ? 1 : 0)) * part_floats(CHUNK, DH);
+      if (g == 0 && row < w.cols) {                  // of the first copy
         const int c = w.c0 + row, rr = c / ln.group;
         if (!whole) { part[row * (DH + 4) + DH] = m; part[row * (DH + 4) + DH + 1] = sum; }
         else if (p.lse) p.lse[(int64_t)(w.row0 + rr) * p.Hq + w.h * ln.group + c - rr * ln.group] = (m + log2f(sum)) * 0.6931471805599453f;
       }
-      ok = ptx::mbar_wait_warp(bar(B_VFREE + ((tile - 1) & 1u)), ((tile - 1) >> 1) & 1u);
       ptx::tc_fence_after_sync();
       const uint32_t staging = base + T::STAGING;
-      for (int i = 0; i < DH; i += 32) {
-        uint32_t v[32];
-        ptx::tmem_ld_x32(tO + lane_base + i, v);
-        ptx::tmem_ld_wait();
-        if (i + 32 == DH) {
+      for (int i = 0; i < DH; i += 16) {
+        uint32_t v[16];
+        if (last_v) {
+          ptx::tmem_ld_x16(tOg + i, v);
+          ptx::tmem_ld_wait();
+        } else {                                     // no tile of this piece was the group's
+#pragma unroll
+          for (int j = 0; j < 16; ++j) v[j] = 0u;
+        }
+        if (i + 16 == DH) {
           ptx::tc_fence_before_sync();
           __syncwarp();
           if (lane == 0) ptx::mbar_arrive(bar(B_OFREE));
         }
 #pragma unroll
-        for (int j = 0; j < 32; j += 4) {
+        for (int j = 0; j < 16; j += 4) {
           uint4 x;
           uint32_t *xw = &x.x;
 #pragma unroll
-          for (int k = 0; k < 4; ++k) xw[k] = __float_as_uint(scaled(__uint_as_float(v[j + k]), max(e0, -200) + 5) * own_f);
-          ptx::st_shared_v4(staging + row * (LDS_O * 4) + j * 4, x);
+          for (int e = 0; e < 4; ++e) xw[e] = __float_as_uint(scaled(__uint_as_float(v[j + e]), max(e0, -200) + 5) * own_f);
+          ptx::st_shared_v4(staging + (g * 128 + row) * (LDS_O * 4) + j * 4, x);
         }
         softmax_sync();
-        // eight dimensions of a column a thread: words 0 4 1 5 2 6 3 7
-        for (int x = threadIdx.x & 127; x < w.cols * 4; x += 128) {
-          const int c = x >> 2, d = (x & 3) * 8;
+        // eight dimensions of a column a thread: they lie in the order 0 4 1 5 2 6 3 7
+        for (int x = threadIdx.x; x < w.cols * 2; x += SOFTMAX) {
+          const int c = x >> 1, d = (x & 1) * 8;
           float y[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-          for (int k = 0; k < copies; ++k) {
-            const uint32_t at = staging + (c + k * chunk) * (LDS_O * 4) + d * 4;
+#pragma unroll
+          for (int e = 0; e < 2 * COPIES; ++e) {
+            const uint32_t at = staging + ((e & 1) * 128 + c + (e >> 1) * CHUNK) * (LDS_O * 4) + d * 4;
             const uint4 lo = ptx::ld_shared_v4(at), hi = ptx::ld_shared_v4(at + 16);
             y[0] += __uint_as_float(lo.x); y[4] += __uint_as_float(lo.y); y[1] += __uint_as_float(lo.z); y[5] += __uint_as_float(lo.w);
             y[2] += __uint_as_float(hi.x); y[6] += __uint_as_float(hi.y); y[3] += __uint_as_float(hi.z); y[7] += __uint_as_float(hi.w);
           }
           if (whole) {
             const int cc = w.c0 + c, rr = cc / ln.group;
-            Vec8<bf16> o;
+            Vec8<bf16> ov;
 #pragma unroll
-            for (int k = 0; k < 8; ++k) o.set(k, y[k]);
-            o.store(p.out + (int64_t)(w.row0 + rr) * p.out_stride + (int64_t)(w.h * ln.group + cc - rr * ln.group) * DH + i + d);
+            for (int e = 0; e < 8; ++e) ov.set(e, y[e]);
+            ov.store(p.out + (int64_t)(w.row0 + rr) * p.out_stride + (int64_t)(w.h * ln.group + cc - rr * ln.group) * DH + i + d);
           } else {
             float4 *dst = reinterpret_cast<float4 *>(part + c * (DH + 4) + i + d);
             dst[0] = make_float4(y[0], y[1], y[2], y[3]); dst[1] = make_float4(y[4], y[5], y[6], y[7]);
           }
         }
-        if (!ok) lost = 1;
         softmax_sync();
       }
-      if (lost) break;
       pos += w.t1 - w.t0;
     }
     if (lost) { fail(status, DEV_TIMEOUT_EPILOGUE); abort_flag = 1; }
@@ -521,23 +503,31 @@ __global__ void __launch_bounds__(512, 1) attention_kv4_tc_kernel(const AttnPara
     while (ptx::globaltimer() - t0 < 200000ull) __nanosleep(1000);
     __syncthreads();
   }
-  if (warp == 1) {
+  if (warp == 17) {
     ptx::tc_fence_after_sync();
     ptx::tmem_dealloc(tS, 512);
   }
 }
 
-template <int DH> cudaError_t launch(cudaStream_t st, const AttnParams &p, int ctas) {
+template <int DH, int COPIES> cudaError_t launch(cudaStream_t st, const AttnParams &p, int ctas) {
   constexpr int smem = Tc<DH>::BYTES + 1024;
-  cudaError_t e = cudaFuncSetAttribute(attention_kv4_tc_kernel<DH>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  cudaError_t e = cudaFuncSetAttribute(attention_kv4_tc_kernel<DH, COPIES>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
   if (e != cudaSuccess) return e;
-  return launch_kernel(attention_kv4_tc_kernel<DH>, dim3(ctas), dim3(512), (size_t)smem, st, p);
+  return launch_kernel(attention_kv4_tc_kernel<DH, COPIES>, dim3(ctas), dim3(THREADS), (size_t)smem, st, p);
+}
+
+template <int DH> cudaError_t launch_chunk(cudaStream_t st, const AttnParams &p, int ctas) {
+  switch (p.line.chunk) {
+    case 32: return launch<DH, 4>(st, p, ctas);
+    case 64: return launch<DH, 2>(st, p, ctas);
+    default: return launch<DH, 1>(st, p, ctas);
+  }
 }
 
 }  // namespace
 
 cudaError_t launch_attention_kv4_tc(cudaStream_t st, const AttnParams &p, int dh, int ctas) {
-  return dh == 128 ? launch<128>(st, p, ctas) : launch<64>(st, p, ctas);
+  return dh == 128 ? launch_chunk<128>(st, p, ctas) : launch_chunk<64>(st, p, ctas);
 }
 
 }  // namespace kv4
