@@ -10,10 +10,11 @@
 // E belongs to 32 keys (a warp).  A code reaches fp16 as it lies, as the subnormal c 2^-24 (or 16 c 2^-24 from bits 4..7), and the
 // multiplication by s 2^24 (2^20) lifts it.  Eight codes of a word come out in the order 0 4 1 5 2 6 3 7: queries are written in that order, and
 // outputs read in it.
-// Two softmax threads own a lane, each with half of a tile's keys: t = cf 2^E acc + (E_V - E0) - M, P = 2^t as fp16 over the scores, as the
-// A operand of the second product.  M is a reference that follows the running maximum lazily, E0 the largest E_V so far; O is rescaled
-// when one moves.  The two agree on M where it has to move (first tile, a score 2^6 above it): the barrier at which all of them say
-// whether one does is also the point from which the scores may be overwritten.
+// Two groups of four softmax warps take the tiles alternately, a thread a lane: t = cf 2^E acc + (E_V - E0) - M, P = 2^t as fp16 over the
+// second half of the scores, as the A operand of the second product.  M is a reference that follows the running maximum lazily, E0 the
+// largest E_V so far; O is rescaled when one moves.  The thread that has fixed them for a tile hands them to the other group's thread
+// of its lane before its exponentials.  128 keys of a lane are worked on in two halves, the second first: its probabilities go
+// over its own scores while the first half still stands.
 //
 // Fewer columns than lanes: chunks of 32 (64) columns stand four times (twice) in the lanes, and each copy takes its quarter (half) of a
 // tile's keys, its probabilities of the others being 0.  The tensor pipe and shared memory do the same work as for 128 columns, but the
@@ -22,8 +23,8 @@
 // What bounds it: shared memory.  128 keys of 128: 17 KB of codes in and out, 64 KB of operands out and in: 1300 cycles at 128 bytes; the
 // products 1090, the exponentials (128 columns) 1024.
 //
-// Warp roles (576 threads): 0-3 softmax and output, 4-7 softmax and the next piece's queries meanwhile, 8-11 K, 12-15 V, 16 copies of
-// codes, 17 MMA issuer (owns tensor memory).  Tensor memory: S at 0 and 128, O at 256, Q at 384.
+// Warp roles (640 threads): 0-3 softmax and output, 4-7 softmax and the next piece's queries meanwhile, 8-11 K, 12-15 V, 16 copies of
+// codes, 17 MMA issuer (owns tensor memory), 18 and 19 none.  Tensor memory: S at 0 and 128, O at 256, Q at 384.
 #include <cuda_fp16.h>
 #include <math.h>
 
@@ -38,7 +39,8 @@ constexpr int RING = 3, NB = 2;                    // tiles of codes on their wa
 constexpr uint32_t ATOM = TC_TILE * 128;           // 128 rows x 64 fp16
 constexpr int NONE = -1000;                        // no exponent
 constexpr int LDS_O = 36;                          // floats of a staged row of 32
-constexpr int THREADS = 576;
+constexpr int THREADS = 640;
+constexpr int REGS_SOFTMAX = 120, REGS_CODES = 88, REGS_LEAN = 56;   // 256 x 120 + 256 x 88 + 128 x 56 of 640 x 96
 
 template <int DH> struct Tc {
   static constexpr int ATOMS = DH / 64, TILE32 = KV4_TILE * (DH + 8), STAGE = 4 * TILE32;
@@ -47,7 +49,7 @@ template <int DH> struct Tc {
 };
 
 enum { B_FULL = 0, B_EMPTY = B_FULL + RING, B_KRDY = B_EMPTY + RING, B_KFREE = B_KRDY + NB, B_VRDY = B_KFREE + NB, B_VFREE = B_VRDY + NB,
-       B_SFULL = B_VFREE + NB, B_PRDY = B_SFULL + 2, B_QRDY = B_PRDY + 2, B_OFREE = B_QRDY + 1, B_COUNT = B_OFREE + 1 };
+       B_SFULL = B_VFREE + NB, B_PRDY = B_SFULL + 2, B_QRDY = B_PRDY + 2, B_OFREE = B_QRDY + 1, B_HAND = B_OFREE + 1, B_COUNT = B_HAND + 8 };
 
 __device__ __forceinline__ float pow2(int n) { return __uint_as_float((uint32_t)(127 + n) << 23); }   // -126 <= n <= 127
 // x 2^n for n beyond one exponent's range
@@ -61,13 +63,6 @@ __device__ __forceinline__ uint32_t hfma2(uint32_t a, uint32_t b, uint32_t c) {
 }
 __device__ __forceinline__ void softmax_sync() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
 __device__ __forceinline__ void output_sync() { asm volatile("bar.sync 2, 128;" ::: "memory"); }
-// softmax_sync, and whether any of the threads said so
-__device__ __forceinline__ bool softmax_any(bool x) {
-  uint32_t r;
-  asm volatile("{\n\t.reg .pred a, b;\n\tsetp.ne.u32 a, %1, 0;\n\tbar.red.or.pred b, 1, 256, a;\n\tselp.u32 %0, 1, 0, b;\n\t}" : "=r"(r) : "r"((uint32_t)x) : "memory");
-  return r != 0;
-}
-
 // A row of codes, its quarters in an order that differs from row to row: eight lanes touch all banks, reading and writing.
 template <int DH> struct Row {
   uint4 w[DH / 32];
@@ -95,7 +90,7 @@ template <int DH> struct Row {
 template <int DH, int COPIES>
 __global__ void __launch_bounds__(THREADS, 1) attention_kv4_tc_kernel(const AttnParams p) {
   using T = Tc<DH>;
-  constexpr int CHUNK = 128 / COPIES, NK = TC_TILE / COPIES / 2;   // columns; keys of a tile that a thread takes
+  constexpr int CHUNK = 128 / COPIES, KEYS = TC_TILE / COPIES;   // columns; keys of a tile that a copy takes
   extern __shared__ uint8_t smem_raw[];
   __shared__ __align__(8) uint64_t bars[B_COUNT];
   __shared__ uint32_t tmem_slot;
@@ -103,9 +98,9 @@ __global__ void __launch_bounds__(THREADS, 1) attention_kv4_tc_kernel(const Attn
   // exponents of a tile's four groups of 32 keys.  K runs ahead of the softmax: its buffer is free once the scores are there
   __shared__ int expo_k[2 * NB][4], expo_v[NB][4];
   __shared__ int lost;                             // a softmax warp's wait ran out
-  __shared__ float tops[2][128];                   // of a lane's two threads
+  __shared__ float2 hand[2][128];                  // [group][lane]: reference and E0 of the group's last tile
+  __shared__ float2 sums[2][128];                  // [group][lane]: the reference its sum is against, the sum
   __shared__ float2 ml[128];                       // a lane's reference and sum
-  __shared__ float sum_1[128];                     // sum of the lane's second thread
   __shared__ float q_factor[2][128];
   const int warp = ptx::warp_index(), lane = threadIdx.x & 31;
   const uint32_t base = (ptx::smem_u32(smem_raw) + 1023u) & ~1023u;
@@ -117,8 +112,9 @@ __global__ void __launch_bounds__(THREADS, 1) attention_kv4_tc_kernel(const Attn
       ptx::mbar_init(bar(B_KRDY + i), 4); ptx::mbar_init(bar(B_KFREE + i), 1);
       ptx::mbar_init(bar(B_VRDY + i), 4); ptx::mbar_init(bar(B_VFREE + i), 1);
     }
-    for (int i = 0; i < 2; ++i) { ptx::mbar_init(bar(B_SFULL + i), 2); ptx::mbar_init(bar(B_PRDY + i), 8); }
+    for (int i = 0; i < 2; ++i) { ptx::mbar_init(bar(B_SFULL + i), 2); ptx::mbar_init(bar(B_PRDY + i), 4); }
     ptx::mbar_init(bar(B_QRDY), 4); ptx::mbar_init(bar(B_OFREE), 4);
+    for (int i = 0; i < 8; ++i) ptx::mbar_init(bar(B_HAND + i), 1);
     abort_flag = 0; lost = 0;
     ptx::fence_barrier_init();
     ptx::fence_proxy_async();
@@ -151,6 +147,7 @@ __global__ void __launch_bounds__(THREADS, 1) attention_kv4_tc_kernel(const Attn
     return w;
   };
 
+  if (warp >= 16) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(REGS_LEAN));
   if (warp == 16) {
     // ------------------------------------------------------------------ codes: up to four tiles of the cache, one contiguous piece
     int slot = 0;
@@ -203,7 +200,7 @@ __global__ void __launch_bounds__(THREADS, 1) attention_kv4_tc_kernel(const Attn
       if (ptx::elect_one() && ok) {
 #pragma unroll
         for (int k = 0; k < TC_TILE / 16; ++k)
-          ptx::mma_bf16_ts(tO, tS + b * TC_TILE + 8 * k, vd + k * (2048u >> 4), idesc_o, k ? 1u : first ? 0u : 1u);
+          ptx::mma_bf16_ts(tO, tS + b * TC_TILE + 64 + 8 * k, vd + k * (2048u >> 4), idesc_o, k ? 1u : first ? 0u : 1u);
         ptx::mma_commit(bar(B_VFREE + b));
       }
       ++tp;
@@ -220,7 +217,9 @@ __global__ void __launch_bounds__(THREADS, 1) attention_kv4_tc_kernel(const Attn
       }
       pos += n;
     }
+  } else if (warp >= 18) {
   } else if (warp >= 8) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(REGS_CODES));
     // ------------------------------------------------------------------ codes to operands
     const bool is_v = warp >= 12;
     const int grp = warp & 3, r = 32 * grp + lane;
@@ -274,11 +273,12 @@ __global__ void __launch_bounds__(THREADS, 1) attention_kv4_tc_kernel(const Attn
     if (!ok) { fail(status, DEV_TIMEOUT_PRODUCER); abort_flag = 1; }
   } else {
     // ------------------------------------------------------------------ queries, softmax, output
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(REGS_SOFTMAX));
     const int g = warp >> 2, q = warp & 3, row = 32 * q + lane;
     const int col = row & (CHUNK - 1);               // this lane's column of the chunk
-    const int copy = q / (4 / COPIES), k0 = (2 * copy + g) * NK;   // the lane's copy, the thread's first key of a tile
-    constexpr int CG = TC_TILE / COPIES / 32;        // exponents of a copy's keys
-    constexpr int NG = NK > 32 ? NK / 32 : 1, GK = NK / NG;   // of the thread's keys, and their keys
+    const int copy = q / (4 / COPIES);               // its first key of a tile: copy * KEYS
+    constexpr int NG = KEYS / 32, HALF = KEYS < 64 ? KEYS : 64, HG = HALF / 32;   // exponents of a copy's keys; keys taken at once
+    const uint32_t mine = bar(B_HAND + 4 * g + q), theirs = bar(B_HAND + 4 * (g ^ 1) + q);
     const uint32_t lane_base = (uint32_t)(32 * q) << 16, tOr = tO + lane_base;
     uint32_t tile = 0, piece = 0;
     bool ok = true;
@@ -298,8 +298,9 @@ __global__ void __launch_bounds__(THREADS, 1) attention_kv4_tc_kernel(const Attn
       for (int j = 0; j < DH / 2; ++j) top = max(top, max((raw[j] << 16) & 0x7fffffffu, raw[j] & 0x7fff0000u));
       const bool finite = top < 0x7f800000u;
       const int u = finite ? min(7 - ((int)(top >> 23) - 127), 126) : 0;
-      const float up = pow2(u);
-      q_factor[parity][row] = p.scale_log2 * pow2(-u);
+      // the scale's sign goes with the queries: the largest product is then the largest score
+      const float up = p.scale_log2 < 0.f ? -pow2(u) : pow2(u);
+      q_factor[parity][row] = fabsf(p.scale_log2) * pow2(-u);
       float sum = 0.f;
 #pragma unroll
       for (int j = 0; j < DH / 8; ++j) {
@@ -329,113 +330,130 @@ __global__ void __launch_bounds__(THREADS, 1) attention_kv4_tc_kernel(const Attn
     if (g == 1 && begin < end) queries(begin, 0);
     for (uint32_t pos = begin; pos < end; ++piece) {
       const Piece w = piece_at(pos);
-      float m_ref = 0.f, l = 0.f, cf = 0.f;
-      int e0 = NONE;
-      bool first = true;
+      float m_own = -INFINITY, l = 0.f, cf = 0.f;    // the reference l is against
       for (int t = w.t0; t < w.t1; ++t, ++tile) {
-        const uint32_t b = tile & 1u, par = (tile >> 1) & 1u;
+        if ((tile & 1u) != (uint32_t)g) continue;
+        const uint32_t b = (uint32_t)g, par = (tile >> 1) & 1u;
         // the exponents of V come with its operands
         ok = ok && ptx::mbar_wait_warp(bar(B_VRDY + b), par);
         ok = ok && ptx::mbar_wait_warp(bar(B_SFULL + b), par);
+        if (!ok) break;
         ptx::tc_fence_after_sync();
-        const uint32_t tSr = tS + lane_base + b * TC_TILE;
-        uint32_t s[NK];
-        if (NK == 16) ptx::tmem_ld_x16(tSr + k0, s);
-        else {
+        if (m_own == -INFINITY) cf = q_factor[piece & 1u][row];
+        const uint32_t tSr = tS + lane_base + b * TC_TILE, tSk = tSr + copy * KEYS;
+        float k[NG];
+        int ev[NG], e_top = NONE;
 #pragma unroll
-          for (int i = 0; i < NK; i += 32) ptx::tmem_ld_x32(tSr + k0 + i, s + i);
+        for (int i = 0; i < NG; ++i) {
+          ev[i] = expo_v[b][copy * NG + i];
+          k[i] = fmaxf(scaled(cf, expo_k[tile % (2 * NB)][copy * NG + i] + 9), 1.2e-38f);   // never 0: -inf times it stays -inf
+          e_top = max(e_top, ev[i]);
         }
-        if (t == w.t0) cf = q_factor[piece & 1u][row];
-        float k[NG], o[NG], w_of[NG], fac = 1.f;
-        bool moved = false;                          // E0 did; the same in both threads of a lane
-        {
-          int ev[CG], e_top = NONE;
+        const int left = w.keys - t * TC_TILE - copy * KEYS;
+        uint32_t s[HALF];
+        auto load = [&](int from) {
 #pragma unroll
-          for (int i = 0; i < CG; ++i) {
-            ev[i] = expo_v[b][copy * CG + i];
-            e_top = max(e_top, ev[i]);
+          for (int i = 0; i < HALF; i += 32) ptx::tmem_ld_x32(tSk + from + i, s + i);
+          ptx::tmem_ld_wait();
+          if (left - from < HALF) {
+#pragma unroll
+            for (int j = 0; j < HALF; ++j) if (j >= left - from) s[j] = 0xff800000u;
           }
-          if (e_top > e0) {
-            moved = true;
-            fac = pow2(max(e0 - (e_top + 2), -126));
-            e0 = e_top + 2;
+        };
+        // the largest score plus its exponent
+        float top = -INFINITY;
+#pragma unroll
+        for (int from = 0; from < KEYS; from += HALF) {
+          load(from);
+#pragma unroll
+          for (int i = 0; i < HG; ++i) {
+            float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+            for (int j = 0; j < 32; ++j) mx[j & 3] = fmaxf(mx[j & 3], __uint_as_float(s[32 * i + j]));
+            const int x = ev[from / 32 + i];
+            top = fmaxf(top, fmaf(fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])), k[from / 32 + i], x == NONE ? -1e30f : (float)x));
           }
+        }
+        // reference and E0: those of the tile before, moved where need be
+        float m_was = -INFINITY;
+        int e_was = NONE;
+        if (t > w.t0) {
+          ok = ptx::mbar_wait_warp(theirs, ((tile - 1) >> 1) & 1u);
+          if (!ok) break;
+          const float2 x = hand[g ^ 1][row];
+          m_was = x.x; e_was = __float_as_int(x.y);
+        }
+        const int e0 = e_top > e_was ? e_top + 2 : e_was;
+        float fac = e0 == e_was ? 1.f : pow2(max(e_was - e0, -126));
+        // keys whose values are all 0 have no exponent: they count as E0
+        bool none = false;
 #pragma unroll
-          for (int i = 0; i < NG; ++i) {
-            const int x = CG == NG ? ev[i] : g ? ev[CG / 2 + i < CG ? CG / 2 + i : 0] : ev[i];
-            const int e = x == NONE ? 0 : max(x - e0, -120);
-            k[i] = scaled(cf, expo_k[tile % (2 * NB)][(k0 >> 5) + i] + 9); o[i] = (float)e - m_ref; w_of[i] = pow2(-e);
+        for (int i = 0; i < NG; ++i) none = none || ev[i] == NONE;
+        float rise = top - (float)e0;
+        if (none) {                                  // warp-uniform, rare: their scores again
+          rise = -INFINITY;
+#pragma unroll
+          for (int from = 0; from < KEYS; from += HALF) {
+            load(from);
+#pragma unroll
+            for (int j = 0; j < HALF; ++j)
+              rise = fmaxf(rise, fmaf(__uint_as_float(s[j]), k[from / 32 + j / 32], ev[from / 32 + j / 32] == NONE ? 0.f : (float)(ev[from / 32 + j / 32] - e0)));
           }
         }
-        const int left = w.keys - t * TC_TILE - k0;
-        ptx::tmem_ld_wait();
+        // a copy whose keys all lie behind the end keeps an open reference
+        float m_ref = m_was;
+        if (m_was == -INFINITY) { m_ref = rise; fac = 0.f; }
+        else if (rise - m_was > LAZY) { m_ref = rise; fac *= ptx::ex2(m_was - rise); }
+        hand[g][row] = make_float2(m_ref, __int_as_float(e0));
+        __syncwarp();
+        if (lane == 0) ptx::mbar_arrive(mine);
+        if (m_own != m_ref) l *= m_own == -INFINITY ? 0.f : ptx::ex2(m_own - m_ref);
+        m_own = m_ref;
+        const float m_use = m_ref == -INFINITY ? 0.f : m_ref;
+        // probabilities, the second half first
+        float w_of[NG];
 #pragma unroll
-        for (int j = 0; j < NK; ++j) s[j] = __float_as_uint(fmaf(__uint_as_float(s[j]), k[j / GK], o[j / GK]));
-        if (left < NK) {
-#pragma unroll
-          for (int j = 0; j < NK; ++j) if (j >= left) s[j] = 0xff800000u;
+        for (int i = 0; i < NG; ++i) {
+          const int e = ev[i] == NONE ? 0 : max(ev[i] - e0, -120);
+          ev[i] = __float_as_int((float)e - m_use); w_of[i] = pow2(-e);
         }
-        float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-        for (int j = 0; j < NK; j += 4)
+        for (int from = KEYS - HALF; from >= 0; from -= HALF) {
+          if (from != KEYS - HALF || none) load(from);
 #pragma unroll
-          for (int e = 0; e < 4; ++e) mx[e] = fmaxf(mx[e], __uint_as_float(s[j + e]));
-        const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
-        if (!ok) lost = 1;
-        ptx::tc_fence_before_sync();
-        const bool move = softmax_any(t == w.t0 || moved || (first ? top > -INFINITY : top > LAZY));
-        if (lost) break;                             // all eight warps or none: they meet at barriers
-        ptx::tc_fence_after_sync();
-        if (move) {
-          tops[g][row] = top;
-          softmax_sync();
-          const float both = fmaxf(tops[0][row], tops[1][row]);
-          // a copy whose keys all lie behind the end keeps an open reference
-          const float d = first ? (both > -INFINITY ? both : 0.f) : both > LAZY ? both : 0.f;
-          const float x = ptx::ex2(-d);
-          m_ref += d;
-          fac = first ? 0.f : fac * x;
-          l *= first ? 0.f : x;
-          first = first && !(both > -INFINITY);
+          for (int i = 0; i < HG; ++i) {
+            const float kk = k[from / 32 + i], oo = __int_as_float(ev[from / 32 + i]);
+            float sum[2] = {0.f, 0.f};
 #pragma unroll
-          for (int j = 0; j < NK; ++j) s[j] = __float_as_uint(__uint_as_float(s[j]) - d);
+            for (int j = 0; j < 32; j += 2) {
+              const float p0 = ptx::ex2(fmaf(__uint_as_float(s[32 * i + j]), kk, oo)), p1 = ptx::ex2(fmaf(__uint_as_float(s[32 * i + j + 1]), kk, oo));
+              sum[(j >> 1) & 1] += p0 + p1;
+              s[16 * i + (j >> 1)] = pair(p0, p1);
+            }
+            l = fmaf(sum[0] + sum[1], w_of[from / 32 + i], l);
+          }
+          const uint32_t at = tSr + 64 + (copy * KEYS + from) / 2;
+          if (HALF == 64) ptx::tmem_st_x32(at, s); else ptx::tmem_st_x16(at, s);
         }
-        // probabilities
-        float sum[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int j = 0; j < NK; j += 2) {
-          const float p0 = ptx::ex2(__uint_as_float(s[j])), p1 = ptx::ex2(__uint_as_float(s[j + 1]));
-          float &acc = sum[NG == 2 ? 2 * (j / GK) + ((j >> 1) & 1) : (j >> 1) & 3];
-          acc += p0 + p1;
-          s[j >> 1] = pair(p0, p1);
-        }
-        if (NG == 2) l = fmaf(sum[2] + sum[3], w_of[NG - 1], fmaf(sum[0] + sum[1], w_of[0], l));
-        else l = fmaf((sum[0] + sum[1]) + (sum[2] + sum[3]), w_of[0], l);
-        if (COPIES == 1) ptx::tmem_st_x32(tSr + k0 / 2, s);
-        else {
-          // zeros where the other copies' keys are, half of them from each thread of the lane
+        if (COPIES > 1) {                            // zeros where the other copies' keys are
           uint32_t z[16];
 #pragma unroll
           for (int j = 0; j < 16; ++j) z[j] = 0u;
 #pragma unroll
-          for (int c = 0; c < COPIES; ++c) {
-            const uint32_t at = tSr + (2 * c + g) * (NK / 2);
-            if (COPIES == 2) { if (c == copy) ptx::tmem_st_x16(at, s); else ptx::tmem_st_x16(at, z); }
-            else { if (c == copy) ptx::tmem_st_x8(at, s); else ptx::tmem_st_x8(at, z); }
-          }
+          for (int c = 0; c < 64; c += 16) if (c / (KEYS / 2) != copy) ptx::tmem_st_x16(tSr + 64 + c, z);
         }
-        if (move && t > w.t0 && __any_sync(0xffffffffu, fac != 1.f)) {
-          // each thread of the lane rescales half of O, once the product of the tile before is complete
+        if (t > w.t0 && __any_sync(0xffffffffu, fac != 1.f)) {
+          // once the product of the tile before is complete
           ok = ptx::mbar_wait_warp(bar(B_VFREE + (b ^ 1u)), ((tile - 1) >> 1) & 1u);
           ptx::tc_fence_after_sync();
 #pragma unroll
-          for (int i = 0; i < DH / 2; i += 16) {
-            uint32_t v[16];
-            ptx::tmem_ld_x16(tOr + g * (DH / 2) + i, v);
+          for (int i = 0; i < DH; i += 32) {
+            uint32_t v[32];
+            ptx::tmem_ld_x32(tOr + i, v);
             ptx::tmem_ld_wait();
 #pragma unroll
-            for (int j = 0; j < 16; ++j) v[j] = __float_as_uint(__uint_as_float(v[j]) * fac);
-            ptx::tmem_st_x16(tOr + g * (DH / 2) + i, v);
+            for (int j = 0; j < 32; ++j) v[j] = __float_as_uint(__uint_as_float(v[j]) * fac);
+            ptx::tmem_st_x32(tOr + i, v);
           }
         }
         ptx::tmem_st_wait();
@@ -443,18 +461,23 @@ __global__ void __launch_bounds__(THREADS, 1) attention_kv4_tc_kernel(const Attn
         __syncwarp();
         if (lane == 0) ptx::mbar_arrive(bar(B_PRDY + b));
       }
-      if (lost) break;
       // ---------------------------------------------------------------- the end of a piece
       pos += w.t1 - w.t0;
-      if (g == 1) sum_1[row] = l;
+      sums[g][row] = make_float2(m_own, l);
+      if (!ok) lost = 1;
       softmax_sync();
+      if (lost) break;                               // all eight warps or none: they meet at barriers
+      const float2 last = hand[(tile - 1) & 1u][row], x0 = sums[0][row], x1 = sums[1][row];
+      softmax_sync();                                // the next piece may write them again
       if (g == 1) {
         if (pos < end) queries(pos, (piece + 1) & 1u);
         continue;
       }
       // group 0: the copies of a column meet, 32 dimensions at a time
-      l += sum_1[row];
-      ml[row] = make_float2(first ? -INFINITY : m_ref, l);
+      const float m_ref = last.x;
+      const int e0 = __float_as_int(last.y);
+      l = x0.y * (x0.x == -INFINITY ? 0.f : ptx::ex2(x0.x - m_ref)) + x1.y * (x1.x == -INFINITY ? 0.f : ptx::ex2(x1.x - m_ref));
+      ml[row] = make_float2(m_ref, l);
       ok = ok && ptx::mbar_wait_warp(bar(B_VFREE + ((tile - 1) & 1u)), ((tile - 1) >> 1) & 1u);
       output_sync();
       float m = -INFINITY, sum = 0.f;
@@ -467,7 +490,7 @@ __global__ void __launch_bounds__(THREADS, 1) attention_kv4_tc_kernel(const Attn
       }
       const bool whole = w.t0 == 0 && w.t1 == w.nt;
       // the lane's own factor: to the common reference, and the quotient where the item is whole
-      const float own_f = (first ? 0.f : ptx::ex2(m_ref - m)) * (whole ? 1.f / sum : 1.f);
+      const float own_f = (m_ref == -INFINITY ? 0.f : ptx::ex2(m_ref - m)) * (whole ? 1.f / sum : 1.f);
       float *part = p.part + (int64_t)(2 * blockIdx.x + (w.t0 == 0 ? 1 : 0)) * part_floats(CHUNK, DH);
       if (row < w.cols) {                            // of the first copy
         const int c = w.c0 + row, rr = c / ln.group;
