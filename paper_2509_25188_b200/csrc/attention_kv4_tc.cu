@@ -49,7 +49,7 @@ template <int DH> struct Tc {
 };
 
 enum { B_FULL = 0, B_EMPTY = B_FULL + RING, B_KRDY = B_EMPTY + RING, B_KFREE = B_KRDY + NB, B_VRDY = B_KFREE + NB, B_VFREE = B_VRDY + NB,
-       B_SFULL = B_VFREE + NB, B_PRDY = B_SFULL + 2, B_QRDY = B_PRDY + 2, B_OFREE = B_QRDY + 1, B_HAND = B_OFREE + 1, B_COUNT = B_HAND + 8 };
+       B_SFULL = B_VFREE + NB, B_PRDY = B_SFULL + 2, B_QRDY = B_PRDY + 2, B_OFREE = B_QRDY + 1, B_HAND = B_OFREE + 1, B_EXPO = B_HAND + 8, B_COUNT = B_EXPO + 4 };
 
 __device__ __forceinline__ float pow2(int n) { return __uint_as_float((uint32_t)(127 + n) << 23); }   // -126 <= n <= 127
 // x 2^n for n beyond one exponent's range
@@ -95,8 +95,8 @@ __global__ void __launch_bounds__(THREADS, 1) attention_kv4_tc_kernel(const Attn
   __shared__ __align__(8) uint64_t bars[B_COUNT];
   __shared__ uint32_t tmem_slot;
   __shared__ int abort_flag;
-  // exponents of a tile's four groups of 32 keys.  K runs ahead of the softmax: its buffer is free once the scores are there
-  __shared__ int expo_k[2 * NB][4], expo_v[NB][4];
+  // [tile % 4][group of 32 keys]: exponents.  Those of V are told ahead of the operands, those of K come with the scores
+  __shared__ int expo_k[4][4], expo_v[4][4];
   __shared__ int lost;                             // a softmax warp's wait ran out
   __shared__ float2 hand[2][128];                  // [group][lane]: reference and E0 of the group's last tile
   __shared__ float2 sums[2][128];                  // [group][lane]: the reference its sum is against, the sum
@@ -115,6 +115,7 @@ __global__ void __launch_bounds__(THREADS, 1) attention_kv4_tc_kernel(const Attn
     for (int i = 0; i < 2; ++i) { ptx::mbar_init(bar(B_SFULL + i), 2); ptx::mbar_init(bar(B_PRDY + i), 4); }
     ptx::mbar_init(bar(B_QRDY), 4); ptx::mbar_init(bar(B_OFREE), 4);
     for (int i = 0; i < 8; ++i) ptx::mbar_init(bar(B_HAND + i), 1);
+    for (int i = 0; i < 4; ++i) ptx::mbar_init(bar(B_EXPO + i), 4);
     abort_flag = 0; lost = 0;
     ptx::fence_barrier_init();
     ptx::fence_proxy_async();
@@ -250,7 +251,13 @@ __global__ void __launch_bounds__(THREADS, 1) attention_kv4_tc_kernel(const Attn
         const int down = -(e + (is_v ? 5 : 9));
         const float s1 = scaled(s, down), m1 = scaled(m, down), o = is_v ? m1 : -8.f * s1, a = m1 + 8.f * s1;
         __syncwarp();
-        if (lane == 0) ptx::mbar_arrive(bar(B_EMPTY + slot));
+        if (lane == 0) {
+          ptx::mbar_arrive(bar(B_EMPTY + slot));
+          if (is_v) {
+            expo_v[tile & 3u][grp] = none ? NONE : e;
+            ptx::mbar_arrive(bar(B_EXPO + (tile & 3u)));
+          }
+        }
         ok = ptx::mbar_wait_warp(bar((is_v ? B_VFREE : B_KFREE) + b), ((tile >> 1) & 1u) ^ 1u);
         if (!ok) break;
         row.store(out + b * T::ATOMS * ATOM, r, dup(s1 * 16777216.f), dup(s1 * 1048576.f), dup(o));
@@ -260,9 +267,7 @@ __global__ void __launch_bounds__(THREADS, 1) attention_kv4_tc_kernel(const Attn
           ptx::st_shared_v4(at, make_uint4(pair(hi, hi), pair((a - hi) * 2048.f, 0.f), 0u, 0u));
           ptx::st_shared_v4(at ^ 16u, make_uint4(0u, 0u, 0u, 0u));
         }
-        if (lane == 0) {
-          if (is_v) expo_v[b][grp] = none ? NONE : e; else expo_k[tile % (2 * NB)][grp] = e;
-        }
+        if (!is_v && lane == 0) expo_k[tile & 3u][grp] = e;
         ptx::fence_proxy_async();
         __syncwarp();
         if (lane == 0) ptx::mbar_arrive(bar((is_v ? B_VRDY : B_KRDY) + b));
@@ -282,9 +287,8 @@ __global__ void __launch_bounds__(THREADS, 1) attention_kv4_tc_kernel(const Attn
     const uint32_t lane_base = (uint32_t)(32 * q) << 16, tOr = tO + lane_base;
     uint32_t tile = 0, piece = 0;
     bool ok = true;
-    // Queries of the piece at `pos` to tensor memory (group 1): the largest of a row becomes 2^7 .. 2^8
-    auto queries = [&](uint32_t pos, uint32_t parity) {
-      const Piece w = piece_at(pos);
+    // Queries of a piece to tensor memory (group 1): the largest of a row becomes 2^7 .. 2^8
+    auto queries = [&](const Piece &w, uint32_t parity) {
       const int c = w.c0 + col, rr = c / ln.group;
       const bool there = col < w.cols;
       const bf16 *src = p.q + (int64_t)(w.row0 + rr) * p.q_stride + (int64_t)(w.h * ln.group + c - rr * ln.group) * DH;
@@ -327,15 +331,14 @@ __global__ void __launch_bounds__(THREADS, 1) attention_kv4_tc_kernel(const Attn
       __syncwarp();
       if (lane == 0) ptx::mbar_arrive(bar(B_QRDY));
     };
-    if (g == 1 && begin < end) queries(begin, 0);
     for (uint32_t pos = begin; pos < end; ++piece) {
       const Piece w = piece_at(pos);
+      if (g == 1) queries(w, piece & 1u);            // group 0 may still be at the output of the piece before
       float m_own = -INFINITY, l = 0.f, cf = 0.f;    // the reference l is against
       for (int t = w.t0; t < w.t1; ++t, ++tile) {
         if ((tile & 1u) != (uint32_t)g) continue;
         const uint32_t b = (uint32_t)g, par = (tile >> 1) & 1u;
-        // the exponents of V come with its operands
-        ok = ok && ptx::mbar_wait_warp(bar(B_VRDY + b), par);
+        ok = ok && ptx::mbar_wait_warp(bar(B_EXPO + (tile & 3u)), (tile >> 2) & 1u);
         ok = ok && ptx::mbar_wait_warp(bar(B_SFULL + b), par);
         if (!ok) break;
         ptx::tc_fence_after_sync();
@@ -345,8 +348,8 @@ __global__ void __launch_bounds__(THREADS, 1) attention_kv4_tc_kernel(const Attn
         int ev[NG], e_top = NONE;
 #pragma unroll
         for (int i = 0; i < NG; ++i) {
-          ev[i] = expo_v[b][copy * NG + i];
-          k[i] = fmaxf(scaled(cf, expo_k[tile % (2 * NB)][copy * NG + i] + 9), 1.2e-38f);   // never 0: -inf times it stays -inf
+          ev[i] = expo_v[tile & 3u][copy * NG + i];
+          k[i] = fmaxf(scaled(cf, expo_k[tile & 3u][copy * NG + i] + 9), 1.2e-38f);   // never 0: -inf times it stays -inf
           e_top = max(e_top, ev[i]);
         }
         const int left = w.keys - t * TC_TILE - copy * KEYS;
@@ -360,8 +363,7 @@ __global__ void __launch_bounds__(THREADS, 1) attention_kv4_tc_kernel(const Attn
             for (int j = 0; j < HALF; ++j) if (j >= left - from) s[j] = 0xff800000u;
           }
         };
-        // the largest score plus its exponent
-        float top = -INFINITY;
+        float top[NG];                               // largest scores of the groups
 #pragma unroll
         for (int from = 0; from < KEYS; from += HALF) {
           load(from);
@@ -370,8 +372,7 @@ __global__ void __launch_bounds__(THREADS, 1) attention_kv4_tc_kernel(const Attn
             float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
             for (int j = 0; j < 32; ++j) mx[j & 3] = fmaxf(mx[j & 3], __uint_as_float(s[32 * i + j]));
-            const int x = ev[from / 32 + i];
-            top = fmaxf(top, fmaf(fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])), k[from / 32 + i], x == NONE ? -1e30f : (float)x));
+            top[from / 32 + i] = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * k[from / 32 + i];
           }
         }
         // reference and E0: those of the tile before, moved where need be
@@ -384,21 +385,12 @@ __global__ void __launch_bounds__(THREADS, 1) attention_kv4_tc_kernel(const Attn
           m_was = x.x; e_was = __float_as_int(x.y);
         }
         const int e0 = e_top > e_was ? e_top + 2 : e_was;
-        float fac = e0 == e_was ? 1.f : pow2(max(e_was - e0, -126));
-        // keys whose values are all 0 have no exponent: they count as E0
-        bool none = false;
+        float fac = e0 == e_was ? 1.f : pow2(max(e_was - e0, -126)), rise = -INFINITY, w_of[NG], o[NG];
 #pragma unroll
-        for (int i = 0; i < NG; ++i) none = none || ev[i] == NONE;
-        float rise = top - (float)e0;
-        if (none) {                                  // warp-uniform, rare: their scores again
-          rise = -INFINITY;
-#pragma unroll
-          for (int from = 0; from < KEYS; from += HALF) {
-            load(from);
-#pragma unroll
-            for (int j = 0; j < HALF; ++j)
-              rise = fmaxf(rise, fmaf(__uint_as_float(s[j]), k[from / 32 + j / 32], ev[from / 32 + j / 32] == NONE ? 0.f : (float)(ev[from / 32 + j / 32] - e0)));
-          }
+        for (int i = 0; i < NG; ++i) {               // keys whose values are all 0 have no exponent: they count as E0
+          const int e = ev[i] == NONE ? 0 : max(ev[i] - e0, -120);
+          rise = fmaxf(rise, top[i] + (float)e);
+          o[i] = (float)e; w_of[i] = pow2(-e);
         }
         // a copy whose keys all lie behind the end keeps an open reference
         float m_ref = m_was;
@@ -410,19 +402,15 @@ __global__ void __launch_bounds__(THREADS, 1) attention_kv4_tc_kernel(const Attn
         if (m_own != m_ref) l *= m_own == -INFINITY ? 0.f : ptx::ex2(m_own - m_ref);
         m_own = m_ref;
         const float m_use = m_ref == -INFINITY ? 0.f : m_ref;
-        // probabilities, the second half first
-        float w_of[NG];
 #pragma unroll
-        for (int i = 0; i < NG; ++i) {
-          const int e = ev[i] == NONE ? 0 : max(ev[i] - e0, -120);
-          ev[i] = __float_as_int((float)e - m_use); w_of[i] = pow2(-e);
-        }
+        for (int i = 0; i < NG; ++i) o[i] -= m_use;
+        // probabilities, the second half first
 #pragma unroll
         for (int from = KEYS - HALF; from >= 0; from -= HALF) {
-          if (from != KEYS - HALF || none) load(from);
+          if (from != KEYS - HALF) load(from);
 #pragma unroll
           for (int i = 0; i < HG; ++i) {
-            const float kk = k[from / 32 + i], oo = __int_as_float(ev[from / 32 + i]);
+            const float kk = k[from / 32 + i], oo = o[from / 32 + i];
             float sum[2] = {0.f, 0.f};
 #pragma unroll
             for (int j = 0; j < 32; j += 2) {
@@ -469,10 +457,7 @@ __global__ void __launch_bounds__(THREADS, 1) attention_kv4_tc_kernel(const Attn
       if (lost) break;                               // all eight warps or none: they meet at barriers
       const float2 last = hand[(tile - 1) & 1u][row], x0 = sums[0][row], x1 = sums[1][row];
       softmax_sync();                                // the next piece may write them again
-      if (g == 1) {
-        if (pos < end) queries(pos, (piece + 1) & 1u);
-        continue;
-      }
+      if (g == 1) continue;
       // group 0: the copies of a column meet, 32 dimensions at a time
       const float m_ref = last.x;
       const int e0 = __float_as_int(last.y);
