@@ -1628,6 +1628,9 @@ l2pd_status l2pd_kv4_weights(void *stream, const l2pd_kv4 *cache, const void *q,
   if (r != L2PD_OK) return r;
   if ((rows && !d_lse) || !d_in || !d_out) return refuse(L2PD_ERR_ARG, call, "null pointer");
   a.max_len = max_len; a.Hq = Hq; a.q = (const bf16 *)q; a.lse = d_lse; a.q_stride = q_stride; a.scale = scale; a.w_in = d_in; a.w_out = d_out;
+  if (!attention_kv4_fits(a.c, B, 1, a.c.heads, max_len)) return refuse(L2PD_ERR_SHAPE, call, "2^31 tiles of work or more");
+  a.status = standalone_status();
+  if (!a.status) return refuse(L2PD_ERR_CUDA, call, "no status word");
   return kv4_launched(call, launch_kv4_weights((cudaStream_t)stream, a, device_sms()));
 }
 

@@ -523,7 +523,7 @@ cudaError_t launch_attention_kv4(cudaStream_t st, const Kv4AttnArgs &a, int sms)
   p.scale_log2 = a.scale * 1.4426950408889634f; p.part = a.scratch; p.status = a.status;
   Line &ln = p.line;
   ln.B = a.b.B; ln.H = a.c.heads; ln.chunk = pl.chunk; ln.group = a.Hq / a.c.heads; ln.slots = a.c.slots;
-  ln.max_keys = a.max_len < a.c.cap ? a.max_len : a.c.cap; ln.tile_keys = pl.tc ? TC_TILE : KV4_TILE; ln.b = a.b;
+  ln.max_keys = a.max_len < a.c.cap ? a.max_len : a.c.cap; ln.tile_keys = pl.tc ? TC_TILE : KV4_TILE; ln.min_chunks = 0; ln.b = a.b;
   const int cols = a.b.rows * ln.group;
   cudaError_t e;
   if (pl.tc) e = launch_attention_kv4_tc(st, p, a.c.dh, pl.ctas);
@@ -533,6 +533,11 @@ cudaError_t launch_attention_kv4(cudaStream_t st, const Kv4AttnArgs &a, int sms)
 }
 
 // ---- weights -----------------------------------------------------------------------------------------------------------
+// w_out = w_in + the probabilities exp(scale q . k - lse) of a key, summed over the columns of its head.  The scores alone: the first half
+// of a cache tile, codes and (s, m) of K.  A warp keeps 32 keys as A fragments in registers and passes the columns by them, whose B
+// fragments lie in shared memory for all warps of the CTA; more than 64 columns in several passes over the CTA's run.
+//
+// Few columns: bound by memory.  Many: by the products, 16 MMAs of 8 cycles for 32 keys and 8 columns.
 namespace {
 
 struct WeighParams {
@@ -543,66 +548,176 @@ struct WeighParams {
   int64_t q_stride;
   float scale_log2;
   const float *w_in; float *w_out;
+  int32_t *status;
 };
 
-// A warp takes 16 keys at a time and all columns of their head.
+constexpr int WEIGH_COLS = 64;       // columns of a pass
+
+template <int DH> struct WeighShape {
+  static constexpr int PART = KV4_TILE * (DH / 2 + 4), STAGES = 4, RING = STAGES * PART;   // codes and (s, m) of K
+  static constexpr int OFF_Q = WARPS * RING, SMEM = OFF_Q + WEIGH_COLS * DH * 2;
+};
+
 template <int DH>
-__global__ void __launch_bounds__(256) kv4_weights_kernel(const WeighParams p) {
-  constexpr int W = DH / 32;
+__global__ void __launch_bounds__(WARPS * 32, 4) kv4_weights_kernel(const WeighParams p) {
+  using Sh = WeighShape<DH>;
+  constexpr int W = DH / 32, STAGES = Sh::STAGES;
+  extern __shared__ __align__(128) uint8_t smem[];
+  __shared__ __align__(8) uint64_t bars[WARPS * STAGES];
+  __shared__ float2 of_col[WEIGH_COLS];            // sum of the scaled queries, minus the log-sum
+  __shared__ uint32_t qtop[WARPS];
+  __shared__ int abort_flag;
+  const int warp = ptx::warp_index(), lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+  const uint32_t bar0 = ptx::smem_u32(&bars[warp * STAGES]);
+  uint8_t *const ring = smem + warp * Sh::RING;
+  const uint32_t ring_u = ptx::smem_u32(ring);
+  uint4 *const qs = reinterpret_cast<uint4 *>(smem + Sh::OFF_Q);
+  if (lane == 0) {
+    for (int i = 0; i < STAGES; ++i) ptx::mbar_init(bar0 + 8 * i, 1);
+    ptx::fence_barrier_init();
+    ptx::fence_proxy_async();
+  }
+  if (threadIdx.x == 0) abort_flag = 0;
+  __syncthreads();
   grid_dep_launch();
   grid_dep_wait();
-  const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+
   const Line &ln = p.line;
-  const int b = blockIdx.y, h = blockIdx.z, key0 = blockIdx.x * 128 + (threadIdx.x >> 5) * 16;
-  const Seq sq = ln.seq(b);
-  const int n_keys = sq.keys, slot = sq.slot, cols = sq.rows * ln.group, row0 = sq.row0;
-  if (key0 >= n_keys) return;
-  const uint8_t *tile = p.c.tile(slot, h, key0 / KV4_TILE);
-  const int kr = key0 % KV4_TILE + g;
-  uint32_t ka[W], kb[W];
+  const Seq own = ln.seq(lane);
+  uint32_t share;
+  const uint32_t total = ln.survey(own, gridDim.x, 0, &share, nullptr);
+  uint32_t pos = (uint32_t)min((uint64_t)share * blockIdx.x, (uint64_t)total);
+  const uint32_t end = min(total, pos + share);
+  uint32_t used = 0;
+  while (pos < end) {
+    uint32_t before;
+    const Seq sq = ln.find(own, pos, &before);
+    const int nt = sq.tiles, h = (int)((pos - before) / nt), t0 = (int)(pos - before) - h * nt, t1 = (int)min((uint32_t)nt, t0 + (end - pos));
+    const int cols = sq.rows * ln.group;
+    const uint8_t *src = p.c.tile(sq.slot, h, 0);
+    const int64_t w_at = ((int64_t)sq.slot * p.c.heads + h) * p.c.cap;
+    pos += t1 - t0;
+    const int mine = (t1 - t0 - warp + WARPS - 1) / WARPS;   // this warp's tiles: t0 + warp, + WARPS, ...
+    for (int c0 = 0; c0 == 0 || c0 < cols; c0 += WEIGH_COLS) {
+      const int here = min(WEIGH_COLS, cols - c0), nts = (here + 7) / 8;
+      auto request = [&](int i) {
+        if (i < mine && ptx::elect_one()) {
+          const uint32_t s = (used + i) % STAGES;
+          ptx::mbar_arrive_expect_tx(bar0 + 8 * s, Sh::PART);
+          ptx::bulk_load(ring_u + s * Sh::PART, src + (int64_t)(t0 + warp + i * WARPS) * kv4_tile_bytes(DH), Sh::PART, bar0 + 8 * s);
+        }
+      };
+      for (int i = 0; i < STAGES; ++i) request(i);
+      // queries: each warp converts every fourth eight of columns.  Two rounds: the largest of all, then the conversion
+      auto column = [&](int n, bool *there) {
+        const int col = c0 + 8 * n + g, r = col / ln.group;
+        *there = 8 * n + g < here;
+        return (int64_t)(sq.row0 + r) * p.Hq + h * ln.group + col - r * ln.group;   // row and query head
+      };
+      auto address = [&](int64_t x) { return p.q + x / p.Hq * p.q_stride + x % p.Hq * DH + t * (DH / 4); };
+      uint32_t top = 0;
+      for (int n = warp; n < nts; n += WARPS) {
+        bool there;
+        const int64_t x = column(n, &there);
+        Queries<DH> qn;
+        qn.load(address(x), there);
+        if (qn.finite()) top = max(top, qn.top);
+      }
+      top = __reduce_max_sync(0xffffffffu, top);
+      if (lane == 0) qtop[warp] = top;
+      __syncthreads();
+      const int u = query_exponent(max(max(qtop[0], qtop[1]), max(qtop[2], qtop[3])));
+      const float cf = query_factor(p.scale_log2, u);
+      for (int n = warp; n < nts; n += WARPS) {
+        bool there;
+        const int64_t x = column(n, &there);
+        Queries<DH> qn;
+        qn.load(address(x), there);
+        uint32_t f[DH / 8];
+        const float cs = qn.convert(u, f);
+        if (t == 0) {
+          float l = there ? p.lse[x] * 1.4426950408889634f : INFINITY;
+          if (l == -INFINITY) l = INFINITY;        // a row without keys gives no weight
+          of_col[8 * n + g] = make_float2(cs, -l);
+        }
 #pragma unroll
-  for (int j = 0; j < W; ++j) {
-    ka[j] = *reinterpret_cast<const uint32_t *>(tile + kr * (DH / 2) + t * (DH / 8) + 4 * j);
-    kb[j] = *reinterpret_cast<const uint32_t *>(tile + (kr + 8) * (DH / 2) + t * (DH / 8) + 4 * j);
-  }
-  const uint32_t m0 = *reinterpret_cast<const uint32_t *>(tile + kv4_off_kmeta(DH) + 4 * kr);
-  const uint32_t m1 = *reinterpret_cast<const uint32_t *>(tile + kv4_off_kmeta(DH) + 4 * kr + 32);
-  float w0 = 0.f, w1 = 0.f;
-  for (int n = 0; n < cols; n += 8) {
-    const int col = n + g, r = col / ln.group, hq = h * ln.group + col - r * ln.group;
-    const bool there = col < cols;
-    uint32_t qf[DH / 8];
-    Queries<DH> qn;
-    qn.load(p.q + (int64_t)(row0 + r) * p.q_stride + (int64_t)hq * DH + t * (DH / 4), there);
-    const int qe = query_exponent(qn.finite() ? qn.top : 0u);
-    const float cf = query_factor(p.scale_log2, qe);
-    float cs = qn.convert(qe, qf);
-    float lse = there ? p.lse[(int64_t)(row0 + r) * p.Hq + hq] * 1.4426950408889634f : INFINITY;
-    if (lse == -INFINITY) lse = INFINITY;          // a row without keys gives no weight
-    float acc[4] = {0.f, 0.f, 0.f, 0.f};
+        for (int j = 0; j < W; ++j) qs[(n * W + j) * 32 + lane] = make_uint4(f[4 * j], f[4 * j + 1], f[4 * j + 2], f[4 * j + 3]);
+      }
+      __syncthreads();
+      bool ok = true;
+      for (int i = 0; i < mine; ++i) {
+        const uint32_t s = (used + i) % STAGES;
+        const int key0 = (t0 + warp + i * WARPS) * KV4_TILE, key = key0 + g + 8 * t;   // the key whose weight this lane writes
+        const bool real = key < sq.keys;
+        const float was = !real ? 0.f : c0 ? p.w_out[w_at + key] : p.w_in[w_at + key];
+        ok = ptx::mbar_wait_warp(bar0 + 8 * s, ((used + i) / STAGES) & 1u);
+        if (!ok) break;
+        const uint8_t *tile = ring + s * Sh::PART;
+        uint32_t k[4][W];                          // rows g, g + 8, g + 16, g + 24
+        float ks[4], km[4], w[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int j = 0; j < W; ++j) {
-      uint32_t x[4], y[4];
-      spread(ka[j], x); spread(kb[j], y);
-      ptx::mma_f16_16x8x16(acc, x[0], y[0], x[1], y[1], qf[4 * j], qf[4 * j + 1]);
-      ptx::mma_f16_16x8x16(acc, x[2], y[2], x[3], y[3], qf[4 * j + 2], qf[4 * j + 3]);
+        for (int e = 0; e < 4; ++e) {
+          const uint8_t *a = tile + (g + 8 * e) * (DH / 2) + t * (DH / 8);
+          if (DH == 128) *reinterpret_cast<uint4 *>(k[e]) = *reinterpret_cast<const uint4 *>(a);
+          else *reinterpret_cast<uint2 *>(k[e]) = *reinterpret_cast<const uint2 *>(a);
+          const uint32_t m = *reinterpret_cast<const uint32_t *>(tile + kv4_off_kmeta(DH) + 4 * (g + 8 * e));
+          ks[e] = kv4_scale(m) * cf; km[e] = kv4_min(m) * cf;
+        }
+        __syncwarp();
+        request(i + STAGES);
+        uint32_t x[4][4 * W];
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+#pragma unroll
+          for (int j = 0; j < W; ++j) spread(k[e][j], &x[e][4 * j]);
+#pragma unroll 1
+        for (int n = 0; n < nts; ++n) {
+          float acc[2][4];
+#pragma unroll
+          for (int j = 0; j < W; ++j) {
+            const uint4 f = qs[(n * W + j) * 32 + lane];
+#pragma unroll
+            for (int m = 0; m < 2; ++m) {
+              if (j == 0) ptx::mma_f16_16x8x16_first(acc[m], x[2 * m][0], x[2 * m + 1][0], x[2 * m][1], x[2 * m + 1][1], f.x, f.y);
+              else ptx::mma_f16_16x8x16(acc[m], x[2 * m][4 * j], x[2 * m + 1][4 * j], x[2 * m][4 * j + 1], x[2 * m + 1][4 * j + 1], f.x, f.y);
+            }
+#pragma unroll
+            for (int m = 0; m < 2; ++m)
+              ptx::mma_f16_16x8x16(acc[m], x[2 * m][4 * j + 2], x[2 * m + 1][4 * j + 2], x[2 * m][4 * j + 3], x[2 * m + 1][4 * j + 3], f.z, f.w);
+          }
+          const float4 of = *reinterpret_cast<const float4 *>(&of_col[8 * n + 2 * t]);   // columns 2t and 2t + 1
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float *a = &acc[e >> 1][2 * (e & 1)];
+            w[e] += ptx::ex2(fmaf(a[0], ks[e], fmaf(km[e], of.x, of.y))) + ptx::ex2(fmaf(a[1], ks[e], fmaf(km[e], of.z, of.w)));
+          }
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          w[e] += __shfl_xor_sync(0xffffffffu, w[e], 1);
+          w[e] += __shfl_xor_sync(0xffffffffu, w[e], 2);
+        }
+        const float sum = t == 0 ? w[0] : t == 1 ? w[1] : t == 2 ? w[2] : w[3];
+        if (real) p.w_out[w_at + key] = was + sum;
+      }
+      if (!ok) { fail(p.status, DEV_TIMEOUT_EPILOGUE); abort_flag = 1; }
+      used += max(mine, 0);
+      __syncthreads();                             // the queries may be overwritten
+      if (abort_flag) break;
     }
-    cs *= cf;
-#pragma unroll
-    for (int e = 0; e < 2; ++e) {
-      const float f = __shfl_sync(0xffffffffu, cf, 8 * t + 4 * e), z = __shfl_sync(0xffffffffu, cs, 8 * t + 4 * e);
-      const float l = __shfl_sync(0xffffffffu, lse, 8 * t + 4 * e);
-      w0 += ptx::ex2(fmaf(acc[e] * f, kv4_scale(m0), fmaf(kv4_min(m0), z, -l)));
-      w1 += ptx::ex2(fmaf(acc[2 + e] * f, kv4_scale(m1), fmaf(kv4_min(m1), z, -l)));
-    }
+    if (abort_flag) break;
   }
-#pragma unroll
-  for (int x = 1; x < 4; x <<= 1) { w0 += __shfl_xor_sync(0xffffffffu, w0, x); w1 += __shfl_xor_sync(0xffffffffu, w1, x); }
-  if (t == 0) {
-    const int64_t at = ((int64_t)slot * p.c.heads + h) * p.c.cap + key0 + g;
-    if (key0 + g < n_keys) p.w_out[at] = p.w_in[at] + w0;
-    if (key0 + g + 8 < n_keys) p.w_out[at + 8] = p.w_in[at + 8] + w1;
+  if (abort_flag) {                                // a wait ran out: copies in flight land before shared memory goes away
+    const uint64_t start = ptx::globaltimer();
+    while (ptx::globaltimer() - start < 200000ull) __nanosleep(1000);
   }
+}
+
+template <int DH> cudaError_t launch_weigh(cudaStream_t st, const WeighParams &p, int ctas) {
+  constexpr int smem = WeighShape<DH>::SMEM;
+  cudaError_t e = cudaFuncSetAttribute(kv4_weights_kernel<DH>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  if (e != cudaSuccess) return e;
+  return launch_kernel(kv4_weights_kernel<DH>, dim3(ctas), dim3(WARPS * 32), (size_t)smem, st, p);
 }
 
 }  // namespace
@@ -610,13 +725,14 @@ __global__ void __launch_bounds__(256) kv4_weights_kernel(const WeighParams p) {
 cudaError_t launch_kv4_weights(cudaStream_t st, const Kv4WeighArgs &a, int sms) {
   WeighParams p;
   p.c = a.c; p.Hq = a.Hq; p.q = a.q; p.lse = a.lse; p.q_stride = a.q_stride; p.scale_log2 = a.scale * 1.4426950408889634f;
-  p.w_in = a.w_in; p.w_out = a.w_out;
+  p.w_in = a.w_in; p.w_out = a.w_out; p.status = a.status;
   Line &ln = p.line;
-  ln.B = a.b.B; ln.H = a.c.heads; ln.chunk = 8; ln.group = a.Hq / a.c.heads; ln.slots = a.c.slots;
+  // one item a head, whatever its columns: a key's weight is written by one thread.  Sequences without rows too: their weights are copied
+  ln.B = a.b.B; ln.H = a.c.heads; ln.chunk = 0x7fffffff; ln.min_chunks = 1; ln.group = a.Hq / a.c.heads; ln.slots = a.c.slots;
   ln.max_keys = a.max_len < a.c.cap ? a.max_len : a.c.cap; ln.tile_keys = KV4_TILE; ln.b = a.b;
-  const dim3 grid((unsigned)ceil_div(a.max_len, 128), a.b.B, a.c.heads);
-  if (a.c.dh == 128) return launch_kernel(kv4_weights_kernel<128>, grid, dim3(256), 0, st, p);
-  return launch_kernel(kv4_weights_kernel<64>, grid, dim3(256), 0, st, p);
+  const int64_t want = ceil_div64((int64_t)a.b.B * a.c.heads * ceil_div(ln.max_keys, KV4_TILE), WARPS);
+  const int ctas = (int)(want < 1 ? 1 : want < sms * 4 ? want : sms * 4);
+  return a.c.dh == 128 ? launch_weigh<128>(st, p, ctas) : launch_weigh<64>(st, p, ctas);
 }
 
 }  // namespace l2pd

@@ -14,7 +14,7 @@ constexpr float LAZY = 6.0f;         // log2 units the running maximum may pass 
 // sequences are one round of loads.
 struct Seq { int keys, rows, row0, slot, tiles, chunks; uint32_t count; };
 struct Line {
-  int B, H, chunk, group, slots, max_keys, tile_keys;
+  int B, H, chunk, group, slots, max_keys, tile_keys, min_chunks;
   Kv4Batch b;
   __device__ __forceinline__ Seq seq(int s) const {
     Seq q = {0, 0, 0, -1, 0, 0, 0u};
@@ -23,7 +23,7 @@ struct Line {
     q.rows = b.n_rows(s); q.row0 = b.row0(s); q.slot = b.slot(s, slots);
     q.keys = q.slot < 0 ? 0 : max(0, min(len, max_keys));
     q.tiles = (q.keys + tile_keys - 1) / tile_keys;
-    q.chunks = (q.rows * group + chunk - 1) / chunk;
+    q.chunks = max(min_chunks, (int)(((uint32_t)(q.rows * group) + (uint32_t)chunk - 1u) / (uint32_t)chunk));
     q.count = (uint32_t)H * q.chunks * q.tiles;
     return q;
   }
