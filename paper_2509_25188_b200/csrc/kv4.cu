@@ -1,94 +1,152 @@
 // A key/value cache in 4 bits: rows written into it, read back as values, and evicted from it.
 #include "kv4.cuh"
+#include "ptx.cuh"
 
 namespace l2pd {
 
 namespace {
 
 // ---- store -------------------------------------------------------------------------------------------------------------
-// dh / 8 threads hold a row, eight values each.  The codes are those of the exact quotient (x - m) / s: the fp32 quotient is
-// within 5e-6 of it, so where it comes within 1e-4 of a border the thread decides its eight codes in 64 bits.
-__device__ __forceinline__ uint32_t kv4_codes(const float *x, float m, float s) {
+// A thread holds 32 values, in four pieces.  The codes are those of the exact quotient (x - m) / s, half to even; quotients of
+// bf16 numbers lie on a border once in a hundred values, so borders are no rare case.  1 / s is taken a little too small, by 2^-21: the
+// fp32 quotient is below the exact one, by less than 1e-5, and its rounding c too small by one where the rest e = (x - m) - c s says so:
+// e > s / 2, or e = s / 2 and c odd.  e is exact if x - m is, which holds where the row's exponents lie within 15 of each other; in other
+// rows (WIDE) what x - m lost decides at a border.  Steps s so small that they lack bits: in 64 bits.
+// Many rows: bound by the instructions a value takes, then by memory.  Two values an instruction for the least and the largest, the
+// rounding by an addition of 1.5 2^23, whose sum ends in the code's bits; 32 values a thread, so that what a row takes counts little
+// (8 a thread: 34 instructions a value, 183 us for 8 x 2048 rows of 32 heads).
+template <bool WIDE>
+__device__ __forceinline__ uint32_t kv4_codes(const uint32_t *raw, float m, float s, float inv) {
+  constexpr float MAGIC = 12582912.f;
+  const float half = 0.5f * s;
+  const uint32_t up = __float_as_uint(half) + 1u;           // the next number, for even codes
   uint32_t w = 0;
-  if (!(s > 0.f)) return w;
-  const float inv = 1.f / s;
-  bool sure = true;
+  const ptx::F2 less = ptx::f2(-m, -m), inv2 = ptx::f2(inv, inv), magic = ptx::f2(MAGIC, MAGIC), back = ptx::f2(-MAGIC, -MAGIC), step = ptx::f2(-s, -s);
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const float t = (x[i] - m) * inv, c = rintf(t);
-    sure = sure && fabsf(t - c) < 0.4999f;           // false for the NaN of an overflown 1 / s too
-    w |= (uint32_t)fminf(c, 15.f) << (4 * i);
+  for (int i = 0; i < 4; ++i) {
+    const ptx::F2 x2 = ptx::f2(__uint_as_float(raw[i] << 16), __uint_as_float(raw[i] & 0xffff0000u));
+    const ptx::F2 d2 = ptx::add2(x2, less), c2 = ptx::fma2(d2, inv2, magic), e2 = ptx::fma2(step, ptx::add2(c2, back), d2);
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      float c = j ? ptx::f2_hi(c2) : ptx::f2_lo(c2);
+      const float e = j ? ptx::f2_hi(e2) : ptx::f2_lo(e2);
+      bool fix = e >= __uint_as_float(up - (__float_as_uint(c) & 1u));
+      if (WIDE) {
+        const float x = j ? ptx::f2_hi(x2) : ptx::f2_lo(x2), d = j ? ptx::f2_hi(d2) : ptx::f2_lo(d2);
+        const float t = d - x, lost = (x - (d - t)) + (-m - t);
+        if (e == half && lost != 0.f) fix = lost > 0.f;
+      }
+      if (fix) c += 1.f;
+      w += __float_as_uint(c) << (4 * (2 * i + j));
+    }
   }
-  if (sure) return w;
-  w = 0;
+  return w - 0x4b400000u * 0x11111111u;                     // the sums' upper bits, shifted and added
+}
+__device__ __noinline__ uint32_t kv4_codes_64(uint4 raw4, float m, float s) {
+  const uint32_t raw[4] = {raw4.x, raw4.y, raw4.z, raw4.w};
+  uint32_t w = 0;
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    const double c = rint(((double)x[i] - (double)m) / (double)s);
+    const double x = __uint_as_float(i & 1 ? raw[i >> 1] & 0xffff0000u : raw[i >> 1] << 16);
+    const double c = rint((x - (double)m) / (double)s);
     w |= (uint32_t)(c < 15.0 ? c : 15.0) << (4 * i);
   }
   return w;
 }
-
-// A block takes rows of one head; a thread has four of them in flight.
-template <int DH> constexpr int STORE_ROWS = 4 * 256 / (DH / 8);
+// Larger of two signed 16-bit numbers, twice
+__device__ __forceinline__ uint32_t max_s2(uint32_t a, uint32_t b) {
+  uint32_t d;
+  asm("max.s16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+  return d;
+}
+// x / 15, correctly rounded: the reciprocal's product and one correction (every fp32 mantissa was checked); for tiny x a division.
+__device__ __forceinline__ float fifteenth(float x) {
+  constexpr float R = 1.f / 15.f;
+  const float q = x * R;
+  return x > 1e-30f ? fmaf(fmaf(-15.f, q, x), R, q) : __fdiv_rn(x, 15.f);
+}
+// Least and largest of two bf16 at a time; NaN wins.
+__device__ __forceinline__ uint32_t min2(uint32_t a, uint32_t b) {
+  uint32_t d;
+  asm("min.NaN.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+  return d;
+}
+__device__ __forceinline__ uint32_t max2(uint32_t a, uint32_t b) {
+  uint32_t d;
+  asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+  return d;
+}
 
 template <int DH>
-__global__ void __launch_bounds__(256) kv4_store_kernel(const Kv4View c, const bf16 *k, const bf16 *v, const Kv4Batch b, int64_t k_stride,
+__global__ void __launch_bounds__(256, 5) kv4_store_kernel(const Kv4View c, const bf16 *k, const bf16 *v, const Kv4Batch b, int64_t k_stride,
                                                         int64_t v_stride) {
-  constexpr int G = DH / 8, STEP = 256 / G;
+  constexpr int G = DH / 32, ROWS = 256 / G;           // threads of a row, rows of a block
   grid_dep_launch();
   grid_dep_wait();
-  const int seq = blockIdx.y, h = blockIdx.x % c.heads, r0 = blockIdx.x / c.heads * STORE_ROWS<DH> + threadIdx.x / G;
+  const int seq = blockIdx.y, h = blockIdx.x % c.heads, first = blockIdx.x / c.heads * ROWS, r = first + threadIdx.x / G;
   const int n = b.n_rows(seq), slot = b.slot(seq, c.slots);
-  if (slot < 0 || blockIdx.x / c.heads * STORE_ROWS<DH> >= n) return;
+  if (slot < 0 || first >= n) return;
   const bool is_v = blockIdx.z;
   const int64_t stride = is_v ? v_stride : k_stride;
-  const int li = threadIdx.x % G, start = b.keys ? b.keys[seq] : 0;
-  const bf16 *src = (is_v ? v : k) + b.row0(seq) * stride + (int64_t)h * DH + 8 * li;
+  const int part = threadIdx.x % G, start = b.keys ? b.keys[seq] : 0;
+  const bf16 *src = (is_v ? v : k) + (b.row0(seq) + (int64_t)min(r, n - 1)) * stride + (int64_t)h * DH + 32 * part;
   uint4 raw[4];
 #pragma unroll
-  for (int u = 0; u < 4; ++u)
-    raw[u] = r0 + u * STEP < n ? *reinterpret_cast<const uint4 *>(src + (r0 + u * STEP) * stride) : make_uint4(0, 0, 0, 0);
+  for (int i = 0; i < 4; ++i) raw[i] = reinterpret_cast<const uint4 *>(src)[i];
+  const uint32_t *wv = &raw[0].x;
+  // the least magnitude that is not 0, as 0x8000 minus its bits: a 0 becomes the smallest signed number
+  uint32_t lo = wv[0], hi = wv[0], near = 0x80008000u;
 #pragma unroll
-  for (int u = 0; u < 4; ++u) {
-    const uint32_t wv[4] = {raw[u].x, raw[u].y, raw[u].z, raw[u].w};
-    float x[8], mn = INFINITY, mx = -INFINITY;
+  for (int i = 0; i < 16; ++i) {
+    lo = min2(lo, wv[i]); hi = max2(hi, wv[i]);
+    near = max_s2(near, 0x80008000u - (wv[i] & 0x7fff7fffu));
+  }
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      x[i] = __uint_as_float(i & 1 ? wv[i >> 1] & 0xffff0000u : wv[i >> 1] << 16);
-      mn = fminf(mn, x[i]);
-      mx = fabsf(x[i]) < INFINITY ? fmaxf(mx, x[i]) : INFINITY;
-    }
-#pragma unroll
-    for (int o = G / 2; o; o >>= 1) {
-      mn = fminf(mn, __shfl_xor_sync(0xffffffffu, mn, o));
-      mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
-    }
-    const float range = mx - mn;
-    const bool fine = range < INFINITY;               // no infinity, no NaN, no range beyond fp32
-    const float s = fine ? __bfloat162float(__float2bfloat16_rn(__fdiv_rn(range, 15.f))) : __uint_as_float(0x7fc00000u);
-    const uint32_t codes = fine ? kv4_codes(x, mn, s) : 0u;
-    const int64_t key = (int64_t)start + r0 + u * STEP;
-    if (r0 + u * STEP >= n || key < 0 || key >= c.cap) continue;
-    uint8_t *t = c.tile(slot, h, (int)(key / KV4_TILE));
-    const int kr = (int)(key % KV4_TILE);
-    const int off = is_v ? kv4_off_v(DH) + kr * (DH / 2) + ((4 * li) ^ kv4_v_swizzle(kr, DH)) : kr * (DH / 2) + 4 * li;
-    *reinterpret_cast<uint32_t *>(t + off) = codes;
-    if (li == 0) {
-      const uint32_t meta = (__float_as_uint(s) >> 16) | (fine ? __float_as_uint(mn) & 0xffff0000u : 0x7fc00000u);
-      *reinterpret_cast<uint32_t *>(t + (is_v ? kv4_off_vmeta(DH) : kv4_off_kmeta(DH)) + 4 * kr) = meta;
-    }
+  for (int o = G / 2; o; o >>= 1) {
+    lo = min2(lo, __shfl_xor_sync(0xffffffffu, lo, o));
+    hi = max2(hi, __shfl_xor_sync(0xffffffffu, hi, o));
+    near = max_s2(near, __shfl_xor_sync(0xffffffffu, near, o));
+  }
+  lo = min2(lo, lo >> 16); hi = max2(hi, hi >> 16); near = max_s2(near, near >> 16);   // the lower halves
+  const int least = (int)((0x8000u - (near & 0xffffu)) & 0x7fffu) >> 7, most = (int)max(lo & 0x7fffu, hi & 0x7fffu) >> 7;   // exponents
+  const float mn = __uint_as_float(lo << 16), range = __uint_as_float(hi << 16) - mn;
+  const bool fine = range < INFINITY;                  // no infinity, no NaN, no range beyond fp32
+  const float s = fine ? __bfloat162float(__float2bfloat16_rn(fifteenth(range))) : __uint_as_float(0x7fc00000u);
+  uint4 codes = make_uint4(0u, 0u, 0u, 0u);
+  if (fine && s > 1e-36f) {
+    float inv;
+    asm("rcp.approx.f32 %0, %1;" : "=f"(inv) : "f"(s));
+    inv = fmaf(inv, -4.76837158203125e-7f, inv);
+    if (least && most - least > 15)
+      codes = make_uint4(kv4_codes<true>(wv, mn, s, inv), kv4_codes<true>(wv + 4, mn, s, inv), kv4_codes<true>(wv + 8, mn, s, inv), kv4_codes<true>(wv + 12, mn, s, inv));
+    else
+      codes = make_uint4(kv4_codes<false>(wv, mn, s, inv), kv4_codes<false>(wv + 4, mn, s, inv), kv4_codes<false>(wv + 8, mn, s, inv), kv4_codes<false>(wv + 12, mn, s, inv));
+  } else if (fine && s > 0.f) {
+    codes = make_uint4(kv4_codes_64(raw[0], mn, s), kv4_codes_64(raw[1], mn, s), kv4_codes_64(raw[2], mn, s), kv4_codes_64(raw[3], mn, s));
+  }
+  const int64_t key = (int64_t)start + r;
+  if (r >= n || key < 0 || key >= c.cap) return;
+  uint8_t *t = c.tile(slot, h, (int)(key / KV4_TILE));
+  const int kr = (int)(key % KV4_TILE);
+  const int off = is_v ? kv4_off_v(DH) + kr * (DH / 2) + ((16 * part) ^ kv4_v_swizzle(kr, DH)) : kr * (DH / 2) + 16 * part;
+  *reinterpret_cast<uint4 *>(t + off) = codes;
+  if (part == 0) {
+    const uint32_t meta = (__float_as_uint(s) >> 16) | (fine ? __float_as_uint(mn) & 0xffff0000u : 0x7fc00000u);
+    *reinterpret_cast<uint32_t *>(t + (is_v ? kv4_off_vmeta(DH) : kv4_off_kmeta(DH)) + 4 * kr) = meta;
   }
 }
 
 // ---- load --------------------------------------------------------------------------------------------------------------
-// As store, backwards.  Rows whose key or slot does not exist read as 0.
+// As store, backwards, with dh / 8 threads a row: a warp then writes whole lines.  Rows whose key or slot does not exist read as 0.
+// A block takes rows of one head; a thread has four of them in flight.
+template <int DH> constexpr int LOAD_ROWS = 4 * 256 / (DH / 8);
+
 template <int DH, typename T>
 __global__ void __launch_bounds__(256) kv4_load_kernel(const Kv4View c, T *k, T *v, const Kv4Batch b, int64_t k_stride, int64_t v_stride) {
   constexpr int G = DH / 8, STEP = 256 / G;
   grid_dep_launch();
   grid_dep_wait();
-  const int seq = blockIdx.y, h = blockIdx.x % c.heads, r0 = blockIdx.x / c.heads * STORE_ROWS<DH> + threadIdx.x / G;
+  const int seq = blockIdx.y, h = blockIdx.x % c.heads, r0 = blockIdx.x / c.heads * LOAD_ROWS<DH> + threadIdx.x / G;
   const int n = b.n_rows(seq), slot = b.slot(seq, c.slots);
   if (r0 >= n) return;
   const bool is_v = blockIdx.z;
@@ -279,14 +337,14 @@ __global__ void __launch_bounds__(256) kv4_move_kernel(const Kv4EvictArgs a) {
 
 cudaError_t launch_kv4_store(cudaStream_t st, const Kv4View &c, const bf16 *k, const bf16 *v, const Kv4Batch &b, int64_t k_stride,
                              int64_t v_stride) {
-  const dim3 grid((unsigned)(ceil_div(b.rows, c.dh == 128 ? STORE_ROWS<128> : STORE_ROWS<64>) * c.heads), b.B, 2);
+  const dim3 grid((unsigned)(ceil_div(b.rows, 256 / (c.dh / 32)) * c.heads), b.B, 2);
   if (c.dh == 128) return launch_kernel(kv4_store_kernel<128>, grid, dim3(256), 0, st, c, k, v, b, k_stride, v_stride);
   return launch_kernel(kv4_store_kernel<64>, grid, dim3(256), 0, st, c, k, v, b, k_stride, v_stride);
 }
 
 cudaError_t launch_kv4_load(cudaStream_t st, const Kv4View &c, int dtype, void *k, void *v, const Kv4Batch &b, int64_t k_stride,
                             int64_t v_stride) {
-  const dim3 grid((unsigned)(ceil_div(b.rows, c.dh == 128 ? STORE_ROWS<128> : STORE_ROWS<64>) * c.heads), b.B, 2);
+  const dim3 grid((unsigned)(ceil_div(b.rows, c.dh == 128 ? LOAD_ROWS<128> : LOAD_ROWS<64>) * c.heads), b.B, 2);
   if (dtype == L2PD_BF16) {
     auto fn = c.dh == 128 ? kv4_load_kernel<128, bf16> : kv4_load_kernel<64, bf16>;
     return launch_kernel(fn, grid, dim3(256), 0, st, c, (bf16 *)k, (bf16 *)v, b, k_stride, v_stride);
