@@ -5,8 +5,8 @@
 //
 // Bound by memory: every value is read and written once.  A block takes R rows: their sines and cosines (R dh/2 of them, for all
 // heads) go to shared memory while the first rows are on their way.  A thread holds eight values of a head's first half and the
-// eight they are paired with, dh / 16 threads a head, so that the sum of squares needs log2(dh / 16) shuffles; four such items are
-// loaded before the first is worked on.
+// eight they are paired with, dh / 16 threads a head, so that the sum of squares needs log2(dh / 16) shuffles; the next such item is
+// loaded before one is worked on.  16384 rows of 40 heads of 128: four items in flight in 124 registers a thread 128 us, one ahead in 64: 67 us (floor 51).
 #include "kv4.cuh"
 
 namespace l2pd {
@@ -17,7 +17,7 @@ constexpr int MAX_HALF = 128;   // dh <= 256
 
 struct Freq { double f[MAX_HALF]; };   // turns (angle / 2 pi) of pair i per position
 
-constexpr int ITEMS = 4, TABLE = 1024;   // items in flight of a thread; (cos, sin) pairs in shared memory
+constexpr int TABLE = 1024;   // (cos, sin) pairs in shared memory
 
 __device__ __forceinline__ float2 turn(double pos, double turns_per_position) {
   double t = pos * turns_per_position;
@@ -29,74 +29,71 @@ __device__ __forceinline__ float2 turn(double pos, double turns_per_position) {
 
 // L = dh / 16 threads a head, a power of two
 template <typename T>
-__global__ void __launch_bounds__(256) qk_norm_rope_vec_kernel(const NormRopeArgs p, const __grid_constant__ Freq freq, int R, int L) {
+__global__ void __launch_bounds__(256, 4) qk_norm_rope_vec_kernel(const NormRopeArgs p, const __grid_constant__ Freq freq, int R, int L) {
   __shared__ float4 table[TABLE / 2];        // row r, pairs 8 c + 2 q, + 1 at [(r * 4 + q) * L + c]: no bank conflicts over c
   const int heads = p.Hq + p.Hk, half = p.dh >> 1, row0 = blockIdx.x * R, rows = min(R, p.rows - row0), per_row = heads * L;
   const int n = rows * per_row, c = threadIdx.x & (L - 1);
   grid_dep_launch();
   grid_dep_wait();
-  for (int base = 0; base < n; base += 256 * ITEMS) {
-    Vec8<T> lo[ITEMS], hi[ITEMS];
-    int r[ITEMS], h[ITEMS];
+  const int step = 256 / L;                  // heads that a round advances by
+  int row = (int)(threadIdx.x / L) / heads, head = (int)(threadIdx.x / L) - row * heads;   // of the item under way
+  Vec8<T> lo, hi;
+  auto fetch = [&](Vec8<T> &a, Vec8<T> &b, int r, int h) {
+    if (r >= rows) return;
+    const T *x = h >= p.Hq ? (const T *)p.k + (row0 + r) * p.k_stride + (int64_t)(h - p.Hq) * p.dh
+                           : (const T *)p.q + (row0 + r) * p.q_stride + (int64_t)h * p.dh;
+    a.load(x + 8 * c);
+    b.load(x + 8 * c + half);
+  };
 #pragma unroll
-    for (int u = 0; u < ITEMS; ++u) {
-      const int it = base + u * 256 + threadIdx.x;
-      r[u] = it / per_row;
-      h[u] = (it - r[u] * per_row) / L;
-      if (it < n) {
-        const bool is_k = h[u] >= p.Hq;
-        const T *x = is_k ? (const T *)p.k + (row0 + r[u]) * p.k_stride + (int64_t)(h[u] - p.Hq) * p.dh
-                          : (const T *)p.q + (row0 + r[u]) * p.q_stride + (int64_t)h[u] * p.dh;
-        lo[u].load(x + 8 * c);
-        hi[u].load(x + 8 * c + half);
-      } else {
-        r[u] = -1;
+  for (int i = 0; i < 8; ++i) { lo.set(i, 0.f); hi.set(i, 0.f); }
+  fetch(lo, hi, row, head);
+  for (int i = threadIdx.x; i < rows * half; i += 256) {
+    const int tr = i / half, k = i - tr * half;
+    const int64_t pos = p.positions ? p.positions[row0 + tr] : row0 + tr;
+    reinterpret_cast<float2 *>(table)[2 * ((tr * 4 + ((k >> 1) & 3)) * L + (k >> 3)) + (k & 1)] = turn((double)pos, freq.f[k]);
+  }
+  __syncthreads();
+  const float inv_dh = 1.f / p.dh;
+  for (int done = 0; done < n; done += 256) {
+    Vec8<T> next_lo = lo, next_hi = hi;
+    int next_row = row, next_head = head + step;
+    while (next_head >= heads) { next_head -= heads; ++next_row; }
+    fetch(next_lo, next_hi, next_row, next_head);
+    float ss = 0.f;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) { lo[u].set(i, 0.f); hi[u].set(i, 0.f); }
-      }
-    }
-    if (base == 0) {
-      for (int i = threadIdx.x; i < rows * half; i += 256) {
-        const int tr = i / half, k = i - tr * half;
-        const int64_t pos = p.positions ? p.positions[row0 + tr] : row0 + tr;
-        reinterpret_cast<float2 *>(table)[2 * ((tr * 4 + ((k >> 1) & 3)) * L + (k >> 3)) + (k & 1)] = turn((double)pos, freq.f[k]);
-      }
-      __syncthreads();
-    }
-#pragma unroll
-    for (int u = 0; u < ITEMS; ++u) {
-      float ss = 0.f;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) ss = fmaf(lo[u].get(i), lo[u].get(i), fmaf(hi[u].get(i), hi[u].get(i), ss));
-      for (int o = L >> 1; o; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
-      if (r[u] < 0) continue;
-      const bool is_k = h[u] >= p.Hq;
+    for (int i = 0; i < 8; ++i) ss = fmaf(lo.get(i), lo.get(i), fmaf(hi.get(i), hi.get(i), ss));
+    for (int o = L >> 1; o; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
+    if (row < rows) {
+      const bool is_k = head >= p.Hq;
       const float *g = is_k ? p.k_gain : p.q_gain;
-      const float norm = g ? rsqrtf(ss / p.dh + p.eps) : 1.f;
-      float ga[8], gb[8];
+      const float norm = g ? rsqrtf(fmaf(ss, inv_dh, p.eps)) : 1.f;
+      T *y = is_k ? (T *)p.k_out + (row0 + row) * p.ko_stride + (int64_t)(head - p.Hq) * p.dh
+                  : (T *)p.q_out + (row0 + row) * p.qo_stride + (int64_t)head * p.dh;
 #pragma unroll
-      for (int i = 0; i < 8; i += 4) {
-        const float4 one = make_float4(1.f, 1.f, 1.f, 1.f);
-        *reinterpret_cast<float4 *>(ga + i) = g ? *reinterpret_cast<const float4 *>(g + 8 * c + i) : one;
-        *reinterpret_cast<float4 *>(gb + i) = g ? *reinterpret_cast<const float4 *>(g + 8 * c + half + i) : one;
-      }
+      for (int q4 = 0; q4 < 2; ++q4) {
+        float4 ga = make_float4(1.f, 1.f, 1.f, 1.f), gb = ga;
+        if (g) {
+          ga = *reinterpret_cast<const float4 *>(g + 8 * c + 4 * q4);
+          gb = *reinterpret_cast<const float4 *>(g + 8 * c + half + 4 * q4);
+        }
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const float4 cs = table[(r[u] * 4 + q) * L + c];
+        for (int q = 0; q < 2; ++q) {
+          const float4 cs = table[(row * 4 + 2 * q4 + q) * L + c];
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          const int i = 2 * q + e;
-          const float co = e ? cs.z : cs.x, si = e ? cs.w : cs.y;
-          const float a = lo[u].get(i) * norm * ga[i], b = hi[u].get(i) * norm * gb[i];
-          lo[u].set(i, a * co - b * si);
-          hi[u].set(i, b * co + a * si);
+          for (int e = 0; e < 2; ++e) {
+            const int i = 4 * q4 + 2 * q + e;
+            const float co = e ? cs.z : cs.x, si = e ? cs.w : cs.y;
+            const float a = lo.get(i) * norm * (&ga.x)[2 * q + e], b = hi.get(i) * norm * (&gb.x)[2 * q + e];
+            lo.set(i, a * co - b * si);
+            hi.set(i, b * co + a * si);
+          }
         }
       }
-      T *y = is_k ? (T *)p.k_out + (row0 + r[u]) * p.ko_stride + (int64_t)(h[u] - p.Hq) * p.dh
-                  : (T *)p.q_out + (row0 + r[u]) * p.qo_stride + (int64_t)h[u] * p.dh;
-      lo[u].store(y + 8 * c);
-      hi[u].store(y + 8 * c + half);
+      lo.store(y + 8 * c);
+      hi.store(y + 8 * c + half);
     }
+    lo = next_lo; hi = next_hi; row = next_row; head = next_head;
   }
 }
 
@@ -152,8 +149,8 @@ cudaError_t launch_qk_norm_rope(cudaStream_t st, const NormRopeArgs &a, int sms)
   for (int i = 0; i < half; ++i, x *= step) f.f[i] = (double)x;
   const int L = a.dh / 16, heads = a.Hq + a.Hk;
   if (a.vec && (L & (L - 1)) == 0) {
-    // rows of a block: four items a thread, but no fewer than two blocks an SM
-    const int64_t fill = (int64_t)ITEMS * 256 / ((int64_t)heads * L), share = a.rows / (2 * sms);
+    // rows of a block: sixteen rounds, but no fewer than four blocks an SM
+    const int64_t fill = (int64_t)16 * 256 / ((int64_t)heads * L), share = a.rows / (4 * sms);
     int64_t R = fill < share ? fill : share;
     if (R > TABLE / half) R = TABLE / half;
     if (R < 1) R = 1;
