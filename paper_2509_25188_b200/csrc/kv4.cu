@@ -186,7 +186,8 @@ __device__ __forceinline__ uint32_t weight_rank(float w, bool is_protected) {
   return u >> 31 ? ~u : u | 0x80000000u;
 }
 
-constexpr int SELECT_THREADS = 1024;
+constexpr int SELECT_THREADS = 512;
+constexpr int SELECT_CACHE = 32768;   // ranks of a CTA's slice that fit its shared memory
 
 // Exclusive sum over the block of one value a thread; *total receives the sum.
 __device__ __forceinline__ int block_scan(int x, int *warp_sums, int *total) {
@@ -214,45 +215,93 @@ __device__ __forceinline__ int block_scan(int x, int *warp_sums, int *total) {
   return s - x + (w ? warp_sums[w - 1] : 0);
 }
 
-// One block per (head, sequence).  The rank of the last kept key is found digit by digit (four histograms of 256); a bitmap of
-// the kept keys with the running count before each word then answers both "how many free places before j" and "which is the
-// i-th kept key", so that no list is built.
-__global__ void __launch_bounds__(SELECT_THREADS) kv4_select_kernel(const Kv4EvictArgs a) {
+// One cluster of CTAs per (head, sequence), each with a slice of the keys.  The rank of the last kept key is found digit by digit (four
+// histograms of 256, added over the cluster); a bitmap of the kept keys with the running count before each word then answers both "how many
+// free places before j" and "which is the i-th kept key", in the slice of any CTA, so that no list is built.
+// Bound by the latency of its steps: 8 heads x 4 sequences of 65000 keys, one CTA each 141 us.
+__device__ __forceinline__ uint32_t ld_cluster(const void *p, uint32_t rank) {
+  uint32_t v;
+  asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(ptx::mapa(ptx::smem_u32(p), rank)));
+  return v;
+}
+
+__global__ void __launch_bounds__(SELECT_THREADS) kv4_select_kernel(const Kv4EvictArgs a, int cluster, int slice) {
   extern __shared__ uint32_t sm[];
-  __shared__ int hist[256], warp_sums[32], pick[2];
+  __shared__ int hist[4][256], sums[256], warp_sums[32], pick[2];
+  __shared__ int counts[3];                       // of the slice: ties, kept keys, kept keys below the new length
   grid_dep_launch();
   grid_dep_wait();
-  const int h = blockIdx.x, seq = blockIdx.y, H = a.src.heads, tid = threadIdx.x;
+  const int me = blockIdx.x % cluster, h = blockIdx.x / cluster, seq = blockIdx.y, H = a.src.heads, tid = threadIdx.x;
   const int slot = a.b.slot(seq, min(a.src.slots, a.dst.slots));
   const int n = slot < 0 ? 0 : max(0, min(min(a.b.keys[seq], a.max_len), a.src.cap)), m = min(n, a.keep);
   int32_t *kept = a.kept + ((int64_t)seq * H + h) * a.keep;
-  if (h == 0 && tid == 0) a.lens_out[seq] = m;
-  for (int j = m + tid; j < a.keep; j += SELECT_THREADS) kept[j] = -1;
-  if (n <= a.keep) {
-    for (int j = tid; j < n; j += SELECT_THREADS) kept[j] = j;
+  if (blockIdx.x == 0 && tid == 0) a.lens_out[seq] = m;
+  for (int j = m + me * SELECT_THREADS + tid; j < a.keep; j += cluster * SELECT_THREADS) kept[j] = -1;
+  if (n <= a.keep) {                              // the whole cluster
+    for (int j = me * SELECT_THREADS + tid; j < n; j += cluster * SELECT_THREADS) kept[j] = j;
     return;
   }
-  const int64_t base = ((int64_t)slot * H + h) * a.src.cap;
+  const int lo = min(me * slice, n), count = min(slice, n - lo), words = (count + 31) >> 5;   // slice: a multiple of 32
+  uint32_t *bits = sm;
+  int *before = reinterpret_cast<int *>(sm) + slice / 32;
+  uint32_t *cache = sm + slice / 16;
+  const bool cached = slice <= SELECT_CACHE;
+  const int64_t base = ((int64_t)slot * H + h) * a.src.cap + lo;
   const int from = a.protect_from ? a.protect_from[seq] : 0x7fffffff;
-  auto rank = [&](int j) {
-    const int pos = a.positions ? a.positions[base + j] : j;
+  auto rank_of = [&](int j) {
+    const int pos = a.positions ? a.positions[base + j] : lo + j;
     return weight_rank(a.weights[base + j], pos < a.first || pos >= from);
   };
+  auto rank = [&](int j) { return cached ? cache[j] : rank_of(j); };
+  for (int i = tid; i < 1024; i += SELECT_THREADS) hist[i >> 8][i & 255] = 0;
+  if (tid < 3) counts[tid] = 0;
+  if (cached) {
+#pragma unroll 4
+    for (int j = tid; j < count; j += SELECT_THREADS) cache[j] = rank_of(j);
+  }
+  __syncthreads();
   uint32_t prefix = 0, mask = 0;
   int need = m;                                   // of the keys whose leading digits equal the prefix, this many are kept
-  for (int shift = 24; shift >= 0; shift -= 8) {
-    if (tid < 256) hist[tid] = 0;
-    __syncthreads();
-    for (int j = tid; j < n; j += SELECT_THREADS) {
+  for (int pass = 0; pass < 4; ++pass) {
+    const int shift = 24 - 8 * pass;
+    for (int j = tid; j < count; j += SELECT_THREADS) {
       const uint32_t r = rank(j);
-      if ((r & mask) == prefix) atomicAdd(&hist[(r >> shift) & 255u], 1);
+      if ((r & mask) == prefix) atomicAdd(&hist[pass][(r >> shift) & 255u], 1);
     }
-    __syncthreads();
-    // keys in higher digits, counted from the top
-    int total;
-    const int x = tid < 256 ? hist[255 - tid] : 0;
-    const int above = block_scan(x, warp_sums, &total);
-    if (tid < 256 && above < need && above + x >= need) { pick[0] = 255 - tid; pick[1] = above; }
+    if (cluster == 1) __syncthreads();
+    else {
+      ptx::cluster_sync();
+      if (tid < 256) {
+        int x[8], y = 0;
+#pragma unroll
+        for (int c = 0; c < 8; ++c) x[c] = c < cluster ? (int)ld_cluster(&hist[pass][tid], c) : 0;
+#pragma unroll
+        for (int c = 0; c < 8; ++c) y += x[c];
+        sums[tid] = y;
+      }
+      __syncthreads();
+    }
+    if (tid < 32) {                               // keys in higher digits, counted from the top: lane l has the digits 255 - 8 l and below
+      const int *of = (cluster == 1 ? hist[pass] : sums) + 248 - 8 * tid;
+      int x[8], own = 0, digit = -1;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[i] = of[i];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) own += x[i];
+      int above = own;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int y = __shfl_up_sync(0xffffffffu, above, o);
+        if (tid >= o) above += y;
+      }
+      above -= own;
+#pragma unroll
+      for (int i = 7; i >= 0; --i) {              // the digit that the need-th key falls into
+        if (above < need && above + x[i] >= need) { digit = 248 - 8 * tid + i; own = above; }
+        above += x[i];
+      }
+      if (digit >= 0) { pick[0] = digit; pick[1] = own; }
+    }
     __syncthreads();
     prefix |= (uint32_t)pick[0] << shift;
     mask |= 255u << shift;
@@ -260,17 +309,19 @@ __global__ void __launch_bounds__(SELECT_THREADS) kv4_select_kernel(const Kv4Evi
     __syncthreads();
   }
   // bitmap: all above the last kept rank, and of the equal ones the first `need`
-  const int words = (n + 31) >> 5, lane = tid & 31;
-  uint32_t *bits = sm;
-  int *before = reinterpret_cast<int *>(sm) + words;
+  const int lane = tid & 31;
+  int eqs = 0;
   for (int w = tid >> 5; w < words; w += SELECT_THREADS / 32) {
     const int j = w * 32 + lane;
-    const uint32_t r = j < n ? rank(j) : 0u;
-    const uint32_t up = __ballot_sync(0xffffffffu, j < n && r > prefix), eq = __ballot_sync(0xffffffffu, j < n && r == prefix);
-    if (lane == 0) { bits[w] = up; before[w] = (int)eq; }
+    const uint32_t r = j < count ? rank(j) : 0u;
+    const uint32_t up = __ballot_sync(0xffffffffu, j < count && r > prefix), eq = __ballot_sync(0xffffffffu, j < count && r == prefix);
+    if (lane == 0) { bits[w] = up; before[w] = (int)eq; eqs += __popc(eq); }
   }
-  __syncthreads();
-  int ties = 0, count = 0;
+  if (lane == 0 && eqs) atomicAdd(&counts[0], eqs);
+  ptx::cluster_sync();
+  int ties = 0;                                   // in the slices before this one
+  for (int c = 0; c < me; ++c) ties += (int)ld_cluster(&counts[0], c);
+  int sum = 0, low = 0;
   for (int w0 = 0; w0 < words; w0 += SELECT_THREADS) {
     const int w = w0 + tid;
     uint32_t eq = w < words ? (uint32_t)before[w] : 0u;
@@ -280,56 +331,108 @@ __global__ void __launch_bounds__(SELECT_THREADS) kv4_select_kernel(const Kv4Evi
     ties += total;
     for (; eq && room > 0; --room) { up |= eq & (0u - eq); eq &= eq - 1; }
     const int e = block_scan(__popc(up), warp_sums, &total);
-    if (w < words) { bits[w] = up; before[w] = count + e; }
-    count += total;
+    if (w < words) {
+      bits[w] = up;
+      before[w] = sum + e;
+      const int k = m - lo - w * 32;              // keys of this word below the new length
+      low += k >= 32 ? __popc(up) : k > 0 ? __popc(up & ((1u << k) - 1u)) : 0;
+    }
+    sum += total;
   }
-  __syncthreads();
-  auto kept_before = [&](int j) { return before[j >> 5] + __popc(bits[j >> 5] & ((1u << (j & 31)) - 1u)); };
-  const int front = kept_before(m);               // kept keys that stay where they are (m < n)
-  for (int j = tid; j < m; j += SELECT_THREADS) {
+  if (low) atomicAdd(&counts[2], low);
+  if (tid == 0) counts[1] = sum;
+  ptx::cluster_sync();
+  int held[8], front = 0;                         // kept keys of each slice; kept keys that stay where they are
+#pragma unroll
+  for (int c = 0; c < 8; ++c) {
+    held[c] = c < cluster ? (int)ld_cluster(&counts[1], c) : 0;
+    if (c < cluster) front += (int)ld_cluster(&counts[2], c);
+  }
+  auto peek = [&](const void *p, int c) { return cluster == 1 ? *reinterpret_cast<const uint32_t *>(p) : ld_cluster(p, c); };
+  // the places, dealt out to all threads of the cluster
+  for (int j = me * SELECT_THREADS + tid; j < m; j += cluster * SELECT_THREADS) {
+    const int owner = j / slice, at = (j - owner * slice) >> 5;
+    const uint32_t word = peek(&bits[at], owner), bit = 1u << (j & 31);
     int src = j;
-    if (!((bits[j >> 5] >> (j & 31)) & 1u)) {
-      int want = front + j - kept_before(j);      // the kept key with this many before it
-      int lo = m >> 5, hi = words - 1;            // its word: the last whose count does not pass `want`
-      while (lo < hi) {
-        const int mid = (lo + hi + 1) >> 1;
-        if (before[mid] <= want) lo = mid; else hi = mid - 1;
+    if (!(word & bit)) {
+      // the kept key with `want` of them before it: as many as there are free places before this one, behind the front
+      int want = front + j - (int)peek(&before[at], owner) - __popc(word & (bit - 1u)), c = 0;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) if (i < owner) want -= held[i];
+#pragma unroll
+      for (int i = 0; i < 7; ++i)
+        if (c == i && i < cluster - 1 && want >= held[i]) { want -= held[i]; ++c; }
+      int x = 0, y = (min(slice, n - c * slice) + 31) / 32 - 1;   // its word: the last whose count does not pass `want`
+      while (x < y) {
+        const int mid = (x + y + 1) >> 1;
+        if ((int)peek(&before[mid], c) <= want) x = mid; else y = mid - 1;
       }
-      uint32_t u = bits[lo];
-      for (want -= before[lo]; want > 0; --want) u &= u - 1;
-      src = lo * 32 + __ffs(u) - 1;
+      uint32_t u = peek(&bits[x], c);
+      want -= (int)peek(&before[x], c);             // the bit with `want` set ones below it, halving
+      int bit_at = 0;
+#pragma unroll
+      for (int half = 16; half; half >>= 1) {
+        const int below = __popc(u & ((1u << half) - 1u));
+        if (want >= below) { want -= below; bit_at += half; u >>= half; }
+      }
+      src = c * slice + x * 32 + bit_at;
     }
     kept[j] = src;
   }
+  ptx::cluster_sync();                            // others may still read this CTA's bitmap
 }
 
-// Moves the records: a block takes 64 places, four threads a place.  In place only the filled holes move; their sources lie at or
-// behind the new end, all destinations before it.
+// Moves the records: a block takes 128 places, four threads a place, two places a thread at once.  In place only the filled holes move;
+// their sources lie at or behind the new end, all destinations before it.
+constexpr int MOVE_PLACES = 128;
+
 __global__ void __launch_bounds__(256) kv4_move_kernel(const Kv4EvictArgs a) {
   grid_dep_launch();
   grid_dep_wait();
   const int seq = blockIdx.y, H = a.src.heads, h = blockIdx.x % H, part = threadIdx.x & 3;
-  const int j = blockIdx.x / H * 64 + (threadIdx.x >> 2);
-  if (j >= a.keep) return;
   const int slot = a.b.slot(seq, min(a.src.slots, a.dst.slots));
-  const int s = a.kept[((int64_t)seq * H + h) * a.keep + j];
-  if (slot < 0 || s < 0) return;
-  const int64_t from = ((int64_t)slot * H + h) * a.src.cap + s, to = ((int64_t)slot * H + h) * a.dst.cap + j;
-  if (part == 2 && a.weights_dst && a.weights + from != a.weights_dst + to) a.weights_dst[to] = a.weights[from];
-  if (part == 3 && a.positions_dst && !(a.positions && a.positions + from == a.positions_dst + to))
-    a.positions_dst[to] = a.positions ? a.positions[from] : s;
-  if (a.src.data == a.dst.data && s == j) return;
-  const int dh = a.src.dh, rs = s % KV4_TILE, rd = j % KV4_TILE, row = dh / 2;
-  const uint8_t *ts = a.src.tile(slot, h, s / KV4_TILE);
-  uint8_t *td = a.dst.tile(slot, h, j / KV4_TILE);
-  if (part * 16 < row) {
-    *reinterpret_cast<uint4 *>(td + rd * row + part * 16) = *reinterpret_cast<const uint4 *>(ts + rs * row + part * 16);
-    *reinterpret_cast<uint4 *>(td + kv4_off_v(dh) + rd * row + ((part * 16) ^ kv4_v_swizzle(rd, dh))) =
-        *reinterpret_cast<const uint4 *>(ts + kv4_off_v(dh) + rs * row + ((part * 16) ^ kv4_v_swizzle(rs, dh)));
+  if (slot < 0) return;
+  const int dh = a.src.dh, row = dh / 2, meta = part ? kv4_off_vmeta(dh) : kv4_off_kmeta(dh);
+  const int64_t head = (int64_t)slot * H + h;
+  int j[2], s[2];
+#pragma unroll
+  for (int u = 0; u < 2; ++u) {
+    j[u] = blockIdx.x / H * MOVE_PLACES + 64 * u + (threadIdx.x >> 2);
+    s[u] = j[u] < a.keep ? a.kept[((int64_t)seq * H + h) * a.keep + j[u]] : -1;
   }
-  if (part < 2) {
-    const int o = part ? kv4_off_vmeta(dh) : kv4_off_kmeta(dh);
-    *reinterpret_cast<uint32_t *>(td + o + 4 * rd) = *reinterpret_cast<const uint32_t *>(ts + o + 4 * rs);
+  uint4 k[2], v[2];
+  uint32_t m[2], x[2];
+  bool rec[2], val[2];                             // the record moves; the weight or position does
+#pragma unroll
+  for (int u = 0; u < 2; ++u) {
+    rec[u] = s[u] >= 0 && !(a.src.data == a.dst.data && s[u] == j[u]);
+    const int64_t from = head * a.src.cap + s[u], to = head * a.dst.cap + j[u];
+    val[u] = s[u] >= 0 && (part == 2 ? a.weights_dst && a.weights + from != a.weights_dst + to
+                           : part == 3 && a.positions_dst && !(a.positions && a.positions + from == a.positions_dst + to));
+    if (val[u]) x[u] = part == 2 ? __float_as_uint(a.weights[from]) : a.positions ? (uint32_t)a.positions[from] : (uint32_t)s[u];
+    if (rec[u]) {
+      const uint8_t *t = a.src.tile(slot, h, s[u] / KV4_TILE);
+      const int r = s[u] % KV4_TILE;
+      if (part * 16 < row) {
+        k[u] = *reinterpret_cast<const uint4 *>(t + r * row + part * 16);
+        v[u] = *reinterpret_cast<const uint4 *>(t + kv4_off_v(dh) + r * row + ((part * 16) ^ kv4_v_swizzle(r, dh)));
+      }
+      if (part < 2) m[u] = *reinterpret_cast<const uint32_t *>(t + meta + 4 * r);
+    }
+  }
+#pragma unroll
+  for (int u = 0; u < 2; ++u) {
+    const int64_t to = head * a.dst.cap + j[u];
+    if (val[u]) { if (part == 2) a.weights_dst[to] = __uint_as_float(x[u]); else a.positions_dst[to] = (int32_t)x[u]; }
+    if (rec[u]) {
+      uint8_t *t = a.dst.tile(slot, h, j[u] / KV4_TILE);
+      const int r = j[u] % KV4_TILE;
+      if (part * 16 < row) {
+        *reinterpret_cast<uint4 *>(t + r * row + part * 16) = k[u];
+        *reinterpret_cast<uint4 *>(t + kv4_off_v(dh) + r * row + ((part * 16) ^ kv4_v_swizzle(r, dh))) = v[u];
+      }
+      if (part < 2) *reinterpret_cast<uint32_t *>(t + meta + 4 * r) = m[u];
+    }
   }
 }
 
@@ -354,13 +457,25 @@ cudaError_t launch_kv4_load(cudaStream_t st, const Kv4View &c, int dtype, void *
 }
 
 cudaError_t launch_kv4_evict(cudaStream_t st, const Kv4EvictArgs &a) {
-  const size_t smem = (size_t)ceil_div(a.max_len, 32) * 8;
+  // CTAs of a cluster: a slice of 4096 keys each, eight at most
+  int cluster = 1;
+  while (cluster < 8 && a.max_len > 4096 * cluster) cluster *= 2;
+  const int slice = ceil_div(ceil_div(a.max_len > 1 ? a.max_len : 1, cluster), 32) * 32;
+  const size_t smem = (size_t)slice / 32 * 8 + (slice <= SELECT_CACHE ? (size_t)slice * 4 : 0);
   cudaError_t e = cudaSuccess;
-  if (smem > 32 * 1024) e = cudaFuncSetAttribute(kv4_select_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, KV4_MAX_EVICT / 32 * 8);
+  if (smem > 32 * 1024) e = cudaFuncSetAttribute(kv4_select_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, SELECT_CACHE * 4 + KV4_MAX_EVICT / 8 / 4);
   if (e != cudaSuccess) return e;
-  e = launch_kernel(kv4_select_kernel, dim3(a.src.heads, a.b.B), dim3(SELECT_THREADS), smem, st, a);
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(a.src.heads * cluster, a.b.B); cfg.blockDim = dim3(SELECT_THREADS); cfg.dynamicSmemBytes = smem; cfg.stream = st;
+  cudaLaunchAttribute at[2];
+  at[0].id = cudaLaunchAttributeClusterDimension;
+  at[0].val.clusterDim.x = cluster; at[0].val.clusterDim.y = 1; at[0].val.clusterDim.z = 1;
+  at[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[1].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = at; cfg.numAttrs = pdl_enabled() ? 2 : 1;
+  e = cudaLaunchKernelEx(&cfg, kv4_select_kernel, a, cluster, slice);
   if (e != cudaSuccess) return e;
-  return launch_kernel(kv4_move_kernel, dim3((unsigned)(ceil_div(a.keep, 64) * a.src.heads), a.b.B), dim3(256), 0, st, a);
+  return launch_kernel(kv4_move_kernel, dim3((unsigned)(ceil_div(a.keep, MOVE_PLACES) * a.src.heads), a.b.B), dim3(256), 0, st, a);
 }
 
 }  // namespace l2pd
