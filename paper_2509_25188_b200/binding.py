@@ -7,7 +7,6 @@ module without it raises, there is no fallback.
 from __future__ import annotations
 
 import ctypes as C
-import functools
 import os
 from typing import Dict, Optional
 
@@ -485,56 +484,32 @@ def attention_bf16(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, H: int, dh
 
 # ---- operators around a key/value cache in 4 bits --------------------------------------------------------------------
 
-def _rows(x: torch.Tensor, heads: int, dh: int, what: str, dtype=torch.bfloat16):
-    """A packed batch [N, heads, dh] or [B, rows, heads, dh]: its row stride, after the checks the library cannot make."""
-    if x.dtype != dtype or not x.is_cuda:
+def _rows(x: torch.Tensor, heads: int, dh: int, what: str, dtype=torch.bfloat16) -> int:
+    """Row stride of a packed batch [N, heads, dh] or [B, rows, heads, dh], after the checks the library cannot make."""
+    shape = x.shape
+    if x.dtype is not dtype or not x.is_cuda:
         raise ValueError("%s must be a %s tensor on a GPU" % (what, dtype))
-    if x.dim() not in (3, 4) or x.shape[-2] != heads or x.shape[-1] != dh:
+    if len(shape) not in (3, 4) or shape[-2] != heads or shape[-1] != dh:
         raise ValueError("%s must be [rows, %d, %d] or [sequences, rows, %d, %d]" % (what, heads, dh, heads, dh))
     if x.is_contiguous():
         return heads * dh
     st = x.stride()
-    if st[-1] != 1 or (heads > 1 and st[-2] != dh) or (x.dim() == 4 and x.shape[0] > 1 and st[0] != x.shape[1] * st[1]):
+    four = len(shape) == 4 and shape[0] > 1
+    if st[-1] != 1 or (heads > 1 and st[-2] != dh) or (four and shape[1] > 1 and st[0] != shape[1] * st[1]):
         raise ValueError("%s: heads and their numbers must be contiguous, sequences one row stride apart" % what)
-    return st[-3] if x.shape[-3] > 1 else (st[0] if x.dim() == 4 and x.shape[0] > 1 else max(st[-3], heads * dh))
+    return st[-3] if shape[-3] > 1 else st[0] if four else heads * dh
 
 
 def _ints(x: Optional[torch.Tensor], n: int, what: str, device):
     """Address of an int32 array of at least n entries, or None."""
     if x is None:
         return None
-    if x.dtype != torch.int32 or x.device != device or not x.is_contiguous() or x.numel() < n:
+    if x.dtype is not torch.int32 or x.device != device or not x.is_contiguous() or x.numel() < n:
         raise ValueError("%s must be a contiguous int32 tensor of at least %d entries on %s" % (what, n, device))
     return x.data_ptr()
 
 
-def _batch(x: torch.Tensor, row_start: Optional[torch.Tensor], max_rows: Optional[int]):
-    """(sequences, most rows of one, address of row_start) of a packed batch."""
-    if x.dim() == 4:
-        if row_start is not None:
-            raise ValueError("row_start goes with packed rows [N, heads, head_dim]")
-        return int(x.shape[0]), int(x.shape[1]), None
-    if row_start is None:
-        return 1, int(x.shape[0]), None
-    if max_rows is None:
-        raise ValueError("row_start needs max_rows, the most rows of a sequence")
-    b = row_start.numel() - 1
-    return b, int(max_rows), _ints(row_start, 1, "row_start", x.device)
-
-
 _device_now, _raw_stream = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
-
-
-def _on_device(fn):
-    """Runs a call on the device of its cache, or of its first tensor."""
-    @functools.wraps(fn)
-    def call(subject, /, *args, **kw):
-        index = subject.device.index
-        if index is None or _device_now() == index:
-            return fn(subject, *args, **kw)
-        with torch.cuda.device(index):
-            return fn(subject, *args, **kw)
-    return call
 
 
 class KvCache4:
@@ -550,30 +525,50 @@ class KvCache4:
         self.slots, self.heads, self.head_dim, self.capacity = slots, heads, head_dim, capacity
         self.data = torch.zeros(n, dtype=torch.uint8, device="cuda:%d" % device)
         self.device = self.data.device
+        self._index = self.device.index
         self._c = Kv4(self.data.data_ptr(), slots, heads, head_dim, capacity)
         self._ref = C.addressof(self._c)
+        self._scratch = {}
 
-    def _same_device(self, *tensors):
-        for x in tensors:
-            if x is not None and x.device != self.device:
-                raise ValueError("a tensor is not on the cache's device %s" % self.device)
+    def _stream(self) -> int:
+        return _raw_stream(self._index)
 
-    @_on_device
+    def _elsewhere(self) -> bool:
+        """The cache's device is not the current one: the call runs again with it as the current one."""
+        return _device_now() != self._index
+
+    def _batch(self, x: torch.Tensor, row_start: Optional[torch.Tensor], max_rows: Optional[int]):
+        """(sequences, most rows of one, address of row_start) of a packed batch."""
+        if x.device != self.device:
+            raise ValueError("a tensor is not on the cache's device %s" % self.device)
+        if x.dim() == 4:
+            if row_start is not None:
+                raise ValueError("row_start goes with packed rows [N, heads, head_dim]")
+            return x.shape[0], x.shape[1], None
+        if row_start is None:
+            return 1, x.shape[0], None
+        if max_rows is None:
+            raise ValueError("row_start needs max_rows, the most rows of a sequence")
+        return row_start.numel() - 1, max_rows, _ints(row_start, 1, "row_start", self.device)
+
     def store(self, k: torch.Tensor, v: torch.Tensor, key_start=None, slots=None, row_start=None, max_rows=None):
         """Row r of sequence i becomes key key_start[i] + r (key_start None: r) of slot slots[i] (None: i)."""
+        if self._elsewhere():
+            with torch.cuda.device(self._index):
+                return self.store(k, v, key_start, slots, row_start, max_rows)
         ks, vs = _rows(k, self.heads, self.head_dim, "k"), _rows(v, self.heads, self.head_dim, "v")
-        if k.shape != v.shape:
-            raise ValueError("k and v differ in shape")
-        self._same_device(k, v)
-        b, rows, rs = _batch(k, row_start, max_rows)
-        stream = _raw_stream(self.device.index)
-        _check(lib.l2pd_kv4_store(stream, self._ref, k.data_ptr(), v.data_ptr(), b, rows, rs, _ints(slots, b, "slots", self.device),
+        if k.shape != v.shape or v.device != self.device:
+            raise ValueError("k and v differ in shape or device")
+        b, rows, rs = self._batch(k, row_start, max_rows)
+        _check(lib.l2pd_kv4_store(self._stream(), self._ref, k.data_ptr(), v.data_ptr(), b, rows, rs, _ints(slots, b, "slots", self.device),
                                   _ints(key_start, b, "key_start", self.device), ks, vs))
 
-    @_on_device
     def load(self, rows: int, key_start=None, slots=None, row_start=None, total_rows=None, dtype=torch.bfloat16):
         """The values of `rows` keys of each sequence, from key_start[i] on: (k, v), [sequences, rows, heads, head_dim].  With
         row_start: packed [total_rows, heads, head_dim], at most `rows` of a sequence."""
+        if self._elsewhere():
+            with torch.cuda.device(self._index):
+                return self.load(rows, key_start, slots, row_start, total_rows, dtype)
         if dtype not in (torch.bfloat16, torch.float32):
             raise ValueError("dtype is torch.bfloat16 or torch.float32")
         if row_start is not None:
@@ -587,76 +582,90 @@ class KvCache4:
         k = torch.empty(shape, dtype=dtype, device=self.device)
         v = torch.empty_like(k)
         st = self.heads * self.head_dim
-        stream = _raw_stream(self.device.index)
-        _check(lib.l2pd_kv4_load(stream, self._ref, L2PD_BF16 if dtype == torch.bfloat16 else L2PD_F32, k.data_ptr(), v.data_ptr(), b, rows,
+        _check(lib.l2pd_kv4_load(self._stream(), self._ref, L2PD_BF16 if dtype is torch.bfloat16 else L2PD_F32, k.data_ptr(), v.data_ptr(), b, rows,
                                  _ints(row_start, b + 1, "row_start", self.device), _ints(slots, b, "slots", self.device),
                                  _ints(key_start, b, "key_start", self.device), st, st))
         return k, v
 
-    @_on_device
+    def _scratch_bytes(self, b: int, rows: int, hq: int, max_len: int) -> int:
+        """Scratch of an attention call: its size depends on the batch through a few numbers, each asked for once."""
+        key = (b, rows, hq, max_len)
+        n = self._scratch.get(key)
+        if n is None:
+            if len(self._scratch) >= 64:
+                self._scratch.clear()
+            n = self._scratch[key] = lib.l2pd_attention_kv4_scratch_bytes(self._ref, b, rows, hq, max_len)
+        return n
+
     def attention(self, q: torch.Tensor, lens: torch.Tensor, max_len: int, row_start=None, max_rows=None, slots=None,
                   scale: Optional[float] = None, out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None, check: bool = False):
         """Softmax attention of q [.., Hq, head_dim] over the first lens[i] keys of each sequence, lens[i] <= max_len; scale None:
         1 / sqrt(head_dim).  Returns (out, lse), q's shape in bf16 and [.., Hq] in fp32."""
-        hq = q.shape[-2]
-        qs = _rows(q, hq, self.head_dim, "q")
-        b, rows, rs = _batch(q, row_start, max_rows)
+        if self._elsewhere():
+            with torch.cuda.device(self._index):
+                return self.attention(q, lens, max_len, row_start, max_rows, slots, scale, out, lse, check)
+        shape, device, dh = q.shape, self.device, self.head_dim
+        hq = shape[-2]
+        qs = _rows(q, hq, dh, "q")
+        b, rows, rs = self._batch(q, row_start, max_rows)
         if out is None:
-            out = torch.empty_like(q, memory_format=torch.contiguous_format)
+            out, os = torch.empty(shape, dtype=torch.bfloat16, device=device), hq * dh
+        else:
+            os = _rows(out, hq, dh, "out")
         if lse is None:
-            lse = torch.empty(q.shape[:-1], dtype=torch.float32, device=self.device)
-        self._same_device(q, out, lse)
-        if out.shape != q.shape or lse.shape != q.shape[:-1] or lse.dtype != torch.float32 or not lse.is_contiguous():
-            raise ValueError("out has q's shape, lse [.., Hq] in contiguous fp32")
-        stream = _raw_stream(self.device.index)
-        n = lib.l2pd_attention_kv4_scratch_bytes(self._ref, b, rows, hq, max_len)
-        scratch = torch.empty(max(n, 16), dtype=torch.uint8, device=self.device)
-        _check(lib.l2pd_attention_kv4(stream, self._ref, q.data_ptr(), out.data_ptr(), lse.data_ptr(), b, rows, rs,
-                                      _ints(slots, b, "slots", self.device), _ints(lens, b, "lens", self.device), max_len, hq, qs,
-                                      _rows(out, hq, self.head_dim, "out"), 1.0 / self.head_dim ** 0.5 if scale is None else scale,
-                                      scratch.data_ptr(), n, int(check)))
+            lse = torch.empty(shape[:-1], dtype=torch.float32, device=device)
+        elif lse.shape != shape[:-1] or lse.dtype is not torch.float32 or lse.device != device or not lse.is_contiguous():
+            raise ValueError("lse must be [.., Hq] in contiguous fp32 on %s" % device)
+        if out.shape != shape or out.device != device:
+            raise ValueError("out must have q's shape and device")
+        n = self._scratch_bytes(b, rows, hq, max_len)
+        scratch = torch.empty(n, dtype=torch.uint8, device=device)
+        _check(lib.l2pd_attention_kv4(self._stream(), self._ref, q.data_ptr(), out.data_ptr(), lse.data_ptr(), b, rows, rs,
+                                      _ints(slots, b, "slots", device), _ints(lens, b, "lens", device), max_len, hq, qs, os,
+                                      1.0 / dh ** 0.5 if scale is None else scale, scratch.data_ptr(), n, check))
         return out, lse
 
     def _per_key(self, x: torch.Tensor, dtype, what: str):
-        if x.shape != (self.slots, self.heads, self.capacity) or x.dtype != dtype or not x.is_contiguous():
+        if x.shape != (self.slots, self.heads, self.capacity) or x.dtype is not dtype or x.device != self.device or not x.is_contiguous():
             raise ValueError("%s must be a contiguous %s tensor [slots, heads, capacity] of its cache" % (what, dtype))
-        self._same_device(x)
         return x.data_ptr()
 
-    @_on_device
     def attention_weights(self, q: torch.Tensor, lse: torch.Tensor, lens: torch.Tensor, max_len: int, weights: torch.Tensor,
                           out: Optional[torch.Tensor] = None, row_start=None, max_rows=None, slots=None, scale: Optional[float] = None):
         """out = weights + what every key receives from these rows, weights [slots, heads, capacity] in fp32 (out None: in place).
         lse is attention()'s.  Returns out; keys at and behind a sequence's length are not written."""
+        if self._elsewhere():
+            with torch.cuda.device(self._index):
+                return self.attention_weights(q, lse, lens, max_len, weights, out, row_start, max_rows, slots, scale)
         hq = q.shape[-2]
         qs = _rows(q, hq, self.head_dim, "q")
-        b, rows, rs = _batch(q, row_start, max_rows)
+        b, rows, rs = self._batch(q, row_start, max_rows)
         out = weights if out is None else out
-        self._same_device(q, lse)
-        if lse.shape != q.shape[:-1] or lse.dtype != torch.float32 or not lse.is_contiguous():
-            raise ValueError("lse must be [.., Hq] in contiguous fp32")
-        stream = _raw_stream(self.device.index)
-        _check(lib.l2pd_kv4_weights(stream, self._ref, q.data_ptr(), lse.data_ptr(), self._per_key(weights, torch.float32, "weights"),
+        if lse.shape != q.shape[:-1] or lse.dtype is not torch.float32 or lse.device != self.device or not lse.is_contiguous():
+            raise ValueError("lse must be [.., Hq] in contiguous fp32 on %s" % self.device)
+        _check(lib.l2pd_kv4_weights(self._stream(), self._ref, q.data_ptr(), lse.data_ptr(), self._per_key(weights, torch.float32, "weights"),
                                     self._per_key(out, torch.float32, "out"), b, rows, rs, _ints(slots, b, "slots", self.device),
                                     _ints(lens, b, "lens", self.device), max_len, hq, qs,
                                     1.0 / self.head_dim ** 0.5 if scale is None else scale))
         return out
 
-    @_on_device
     def evict(self, weights: torch.Tensor, lens: torch.Tensor, max_len: int, keep: int, positions=None, first: int = 0, protect_from=None,
               slots=None, into: Optional["KvCache4"] = None, weights_into=None, positions_into=None):
         """Keeps the `keep` heaviest keys of every head (see l2pd_kv4_evict) in `into`, or in place, where weights and positions
         follow in place too unless arrays for them are given.  Returns (kept [sequences, heads, keep], the new lengths)."""
+        if self._elsewhere():
+            with torch.cuda.device(self._index):
+                return self.evict(weights, lens, max_len, keep, positions, first, protect_from, slots, into, weights_into, positions_into)
         dst = self if into is None else into
         if dst is self:
             weights_into = weights if weights_into is None else weights_into
             positions_into = positions if positions_into is None else positions_into
+        elif dst.device != self.device:
+            raise ValueError("the destination is not on the cache's device %s" % self.device)
         b = lens.numel()
-        self._same_device(dst.data)
-        kept = torch.empty(b, self.heads, max(keep, 0), dtype=torch.int32, device=self.device)
-        lens_out = torch.empty(b, dtype=torch.int32, device=self.device)
-        stream = _raw_stream(self.device.index)
-        _check(lib.l2pd_kv4_evict(stream, self._ref, dst._ref, self._per_key(weights, torch.float32, "weights"),
+        kept = torch.empty((b, self.heads, max(keep, 0)), dtype=torch.int32, device=self.device)
+        lens_out = torch.empty((b,), dtype=torch.int32, device=self.device)
+        _check(lib.l2pd_kv4_evict(self._stream(), self._ref, dst._ref, self._per_key(weights, torch.float32, "weights"),
                                   None if weights_into is None else dst._per_key(weights_into, torch.float32, "weights_into"),
                                   None if positions is None else self._per_key(positions, torch.int32, "positions"),
                                   None if positions_into is None else dst._per_key(positions_into, torch.int32, "positions_into"),
@@ -665,31 +674,39 @@ class KvCache4:
         return kept, lens_out
 
 
-@_on_device
 def qk_norm_rope(q: torch.Tensor, k: torch.Tensor, q_gain=None, k_gain=None, positions=None, theta: float = 10000.0, eps: float = 1e-5,
                  q_out=None, k_out=None):
     """Head norms (gains fp32 [dh], None: none) and rotation of q [rows, Hq, dh] and k [rows, Hk, dh] (bf16 or fp32) by their
     positions (int32 [rows], None: the row's number).  Returns (q_out, k_out); the inputs themselves may be given for them."""
-    if q.dim() != 3 or k.dim() != 3 or q.shape[0] != k.shape[0] or q.shape[2] != k.shape[2] or q.dtype != k.dtype or q.dtype not in (torch.bfloat16, torch.float32):
+    device, dtype = q.device, q.dtype
+    if device.index is not None and _device_now() != device.index:
+        with torch.cuda.device(device):
+            return qk_norm_rope(q, k, q_gain, k_gain, positions, theta, eps, q_out, k_out)
+    qshape, kshape = q.shape, k.shape
+    if len(qshape) != 3 or len(kshape) != 3 or qshape[0] != kshape[0] or qshape[2] != kshape[2] or dtype not in (torch.bfloat16, torch.float32):
         raise ValueError("q [rows, Hq, dh] and k [rows, Hk, dh], both bf16 or both fp32")
-    t, hq, dh = q.shape
-    hk = k.shape[1]
+    t, hq, dh = qshape
+    hk = kshape[1]
+    qs, ks = _rows(q, hq, dh, "q", dtype), _rows(k, hk, dh, "k", dtype)
     if q_out is None:
-        q_out = torch.empty_like(q, memory_format=torch.contiguous_format)
+        q_out, qos = torch.empty(qshape, dtype=dtype, device=device), hq * dh
+    else:
+        qos = _rows(q_out, hq, dh, "q_out", dtype)
     if k_out is None:
-        k_out = torch.empty_like(k, memory_format=torch.contiguous_format)
-    if q_out.shape != q.shape or k_out.shape != k.shape:
-        raise ValueError("the outputs have their inputs' shapes")
-    strides = [_rows(x, x.shape[1], dh, n, q.dtype) for x, n in ((q, "q"), (k, "k"), (q_out, "q_out"), (k_out, "k_out"))]
-    for g, n in ((q_gain, "q_gain"), (k_gain, "k_gain")):
-        if g is not None and (g.dtype != torch.float32 or g.numel() != dh or not g.is_contiguous() or g.device != q.device):
-            raise ValueError("%s must be a contiguous fp32 tensor [dh] on %s" % (n, q.device))
-    if any(x.device != q.device for x in (k, q_out, k_out)):
-        raise ValueError("the tensors lie on different devices")
-    stream = _raw_stream(q.device.index)
-    _check(lib.l2pd_qk_norm_rope(stream, L2PD_BF16 if q.dtype == torch.bfloat16 else L2PD_F32, q.data_ptr(), k.data_ptr(), q_out.data_ptr(),
-                                 k_out.data_ptr(), None if q_gain is None else q_gain.data_ptr(), None if k_gain is None else k_gain.data_ptr(),
-                                 _ints(positions, t, "positions", q.device), t, hq, hk, dh, *strides, eps, theta))
+        k_out, kos = torch.empty(kshape, dtype=dtype, device=device), hk * dh
+    else:
+        kos = _rows(k_out, hk, dh, "k_out", dtype)
+    if q_out.shape != qshape or k_out.shape != kshape or k.device != device or q_out.device != device or k_out.device != device:
+        raise ValueError("k and the outputs must be on q's device, the outputs of their inputs' shapes")
+    gains = [None, None]
+    for i, g in enumerate((q_gain, k_gain)):
+        if g is not None:
+            if g.dtype is not torch.float32 or g.numel() != dh or not g.is_contiguous() or g.device != device:
+                raise ValueError("gains must be contiguous fp32 tensors [dh] on %s" % device)
+            gains[i] = g.data_ptr()
+    _check(lib.l2pd_qk_norm_rope(_raw_stream(device.index), L2PD_BF16 if dtype is torch.bfloat16 else L2PD_F32, q.data_ptr(), k.data_ptr(),
+                                 q_out.data_ptr(), k_out.data_ptr(), gains[0], gains[1], _ints(positions, t, "positions", device), t, hq, hk, dh,
+                                 qs, ks, qos, kos, eps, theta))
     return q_out, k_out
 
 
