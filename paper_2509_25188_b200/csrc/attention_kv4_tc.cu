@@ -23,8 +23,8 @@
 // What bounds it: shared memory.  128 keys of 128: 17 KB of codes in and out, 64 KB of operands out and in: 1300 cycles at 128 bytes; the
 // products 1090, the exponentials (128 columns) 1024.
 //
-// Warp roles (640 threads): 0-3 softmax and output, 4-7 softmax and the next piece's queries meanwhile, 8-11 K, 12-15 V, 16 copies of
-// codes, 17 MMA issuer (owns tensor memory), 18 and 19 none.  Tensor memory: S at 0 and 128, O at 256, Q at 384.
+// Warp roles (640 threads): 0-3 and 4-7 softmax and output, 4-7 the next piece's queries before that, 8-11 K, 12-15 V, 16 copies of codes,
+// 17 MMA issuer (owns tensor memory), 18 and 19 bring the next piece's queries near.  Tensor memory: S at 0 and 128, O at 256, Q at 384.
 #include <cuda_fp16.h>
 #include <math.h>
 
@@ -37,15 +37,15 @@ namespace {
 
 constexpr int RING = 3, NB = 2;                    // tiles of codes on their way; operand buffers
 constexpr uint32_t ATOM = TC_TILE * 128;           // 128 rows x 64 fp16
-constexpr int NONE = -1000;                        // no exponent
-constexpr int LDS_O = 36;                          // floats of a staged row of 32
+constexpr float NONE = -1000.f;                    // no exponent
+constexpr int LDS_O = 20;                          // floats of a staged row of 16
 constexpr int THREADS = 640;
 constexpr int REGS_SOFTMAX = 120, REGS_CODES = 88, REGS_LEAN = 56;   // 256 x 120 + 256 x 88 + 128 x 56 of 640 x 96
 
 template <int DH> struct Tc {
   static constexpr int ATOMS = DH / 64, TILE32 = KV4_TILE * (DH + 8), STAGE = 4 * TILE32;
   static constexpr uint32_t K = 0, AUG = NB * ATOMS * ATOM, V = AUG + ATOM, CODES = V + NB * ATOMS * ATOM,
-                            STAGING = CODES + RING * STAGE, BYTES = STAGING + 128 * LDS_O * 4;
+                            STAGING = CODES + RING * STAGE, BYTES = STAGING + 2 * 128 * LDS_O * 4;
 };
 
 enum { B_FULL = 0, B_EMPTY = B_FULL + RING, B_KRDY = B_EMPTY + RING, B_KFREE = B_KRDY + NB, B_VRDY = B_KFREE + NB, B_VFREE = B_VRDY + NB,
@@ -62,7 +62,7 @@ __device__ __forceinline__ uint32_t hfma2(uint32_t a, uint32_t b, uint32_t c) {
   return d;
 }
 __device__ __forceinline__ void softmax_sync() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
-__device__ __forceinline__ void output_sync() { asm volatile("bar.sync 2, 128;" ::: "memory"); }
+__device__ __forceinline__ void output_sync(int g) { asm volatile("bar.sync %0, 128;" ::"r"(2 + g) : "memory"); }   // one group
 // A row of codes, its quarters in an order that differs from row to row: eight lanes touch all banks, reading and writing.
 template <int DH> struct Row {
   uint4 w[DH / 32];
@@ -96,11 +96,11 @@ __global__ void __launch_bounds__(THREADS, 1) attention_kv4_tc_kernel(const Attn
   __shared__ uint32_t tmem_slot;
   __shared__ int abort_flag;
   // [tile % 4][group of 32 keys]: exponents.  Those of V are told ahead of the operands, those of K come with the scores
-  __shared__ int expo_k[4][4], expo_v[4][4];
+  __shared__ float expo_k[4][4], expo_v[4][4];
   __shared__ int lost;                             // a softmax warp's wait ran out
   __shared__ float2 hand[2][128];                  // [group][lane]: reference and E0 of the group's last tile
   __shared__ float2 sums[2][128];                  // [group][lane]: the reference its sum is against, the sum
-  __shared__ float2 ml[128];                       // a lane's reference and sum
+  __shared__ float2 ml[2][128];                    // [group][lane]: a lane's reference and sum
   __shared__ float q_factor[2][128];
   const int warp = ptx::warp_index(), lane = threadIdx.x & 31;
   const uint32_t base = (ptx::smem_u32(smem_raw) + 1023u) & ~1023u;
@@ -113,7 +113,7 @@ __global__ void __launch_bounds__(THREADS, 1) attention_kv4_tc_kernel(const Attn
       ptx::mbar_init(bar(B_VRDY + i), 4); ptx::mbar_init(bar(B_VFREE + i), 1);
     }
     for (int i = 0; i < 2; ++i) { ptx::mbar_init(bar(B_SFULL + i), 2); ptx::mbar_init(bar(B_PRDY + i), 4); }
-    ptx::mbar_init(bar(B_QRDY), 4); ptx::mbar_init(bar(B_OFREE), 4);
+    ptx::mbar_init(bar(B_QRDY), 4); ptx::mbar_init(bar(B_OFREE), 8);
     for (int i = 0; i < 8; ++i) ptx::mbar_init(bar(B_HAND + i), 1);
     for (int i = 0; i < 4; ++i) ptx::mbar_init(bar(B_EXPO + i), 4);
     abort_flag = 0; lost = 0;
@@ -219,6 +219,18 @@ __global__ void __launch_bounds__(THREADS, 1) attention_kv4_tc_kernel(const Attn
       pos += n;
     }
   } else if (warp >= 18) {
+    // ------------------------------------------------------------------ the next piece's query rows to this SM's cache
+    for (uint32_t pos = begin; pos < end;) {
+      const Piece w = piece_at(pos);
+      const int c = w.c0 + (warp - 18) * 32 + lane;
+      for (int x = c; x < w.c0 + w.cols; x += 64) {
+        const int rr = x / ln.group;
+        const bf16 *src = p.q + (int64_t)(w.row0 + rr) * p.q_stride + (int64_t)(w.h * ln.group + x - rr * ln.group) * DH;
+#pragma unroll
+        for (int i = 0; i < DH; i += 64) asm volatile("{\n\t.reg .b32 t;\n\tld.global.ca.b32 t, [%0];\n\t}" ::"l"(src + i) : "memory");
+      }
+      pos += w.t1 - w.t0;
+    }
   } else if (warp >= 8) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(REGS_CODES));
     // ------------------------------------------------------------------ codes to operands
@@ -254,7 +266,7 @@ __global__ void __launch_bounds__(THREADS, 1) attention_kv4_tc_kernel(const Attn
         if (lane == 0) {
           ptx::mbar_arrive(bar(B_EMPTY + slot));
           if (is_v) {
-            expo_v[tile & 3u][grp] = none ? NONE : e;
+            expo_v[tile & 3u][grp] = none ? NONE : (float)e;
             ptx::mbar_arrive(bar(B_EXPO + (tile & 3u)));
           }
         }
@@ -267,7 +279,7 @@ __global__ void __launch_bounds__(THREADS, 1) attention_kv4_tc_kernel(const Attn
           ptx::st_shared_v4(at, make_uint4(pair(hi, hi), pair((a - hi) * 2048.f, 0.f), 0u, 0u));
           ptx::st_shared_v4(at ^ 16u, make_uint4(0u, 0u, 0u, 0u));
         }
-        if (!is_v && lane == 0) expo_k[tile & 3u][grp] = e;
+        if (!is_v && lane == 0) expo_k[tile & 3u][grp] = pow2(e + 9 - 32);   // e reaches 128
         ptx::fence_proxy_async();
         __syncwarp();
         if (lane == 0) ptx::mbar_arrive(bar((is_v ? B_VRDY : B_KRDY) + b));
@@ -331,9 +343,88 @@ __global__ void __launch_bounds__(THREADS, 1) attention_kv4_tc_kernel(const Attn
       __syncwarp();
       if (lane == 0) ptx::mbar_arrive(bar(B_QRDY));
     };
-    for (uint32_t pos = begin; pos < end; ++piece) {
-      const Piece w = piece_at(pos);
-      if (g == 1) queries(w, piece & 1u);            // group 0 may still be at the output of the piece before
+    // Queries of a piece, then the output of the one before, then the piece's tiles
+    Piece w = {}, old = {};
+    float2 last = {}, x0 = {}, x1 = {};              // of the piece before: reference and E0, the groups' sums
+    for (uint32_t pos = begin; begin < end; ++piece) {
+      const bool more = pos < end;
+      if (more) {
+        w = piece_at(pos);
+        if (g == 1) queries(w, piece & 1u);
+      }
+      if (piece > 0) {
+        // the copies of a column meet.  Each group brings half of the dimensions, 16 at a time
+        const float m_ref = last.x, e0 = last.y;
+        const float l = x0.y * (x0.x == -INFINITY ? 0.f : ptx::ex2(x0.x - m_ref)) + x1.y * (x1.x == -INFINITY ? 0.f : ptx::ex2(x1.x - m_ref));
+        ml[g][row] = make_float2(m_ref, l);
+        ok = ok && ptx::mbar_wait_warp(bar(B_VFREE + ((tile - 1) & 1u)), ((tile - 1) >> 1) & 1u);
+        output_sync(g);
+        float m = -INFINITY, sum = 0.f;
+#pragma unroll
+        for (int i = 0; i < COPIES; ++i) m = fmaxf(m, ml[g][col + i * CHUNK].x);
+#pragma unroll
+        for (int i = 0; i < COPIES; ++i) {
+          const float2 x = ml[g][col + i * CHUNK];
+          sum = fmaf(x.y, x.x == -INFINITY ? 0.f : ptx::ex2(x.x - m), sum);
+        }
+        const bool whole = old.t0 == 0 && old.t1 == old.nt;
+        // the lane's own factor: to the common reference, to the values' unit 2^(E0 + 5), and the quotient where the item is whole
+        const float own_f = (m_ref == -INFINITY ? 0.f : ptx::ex2(m_ref - m)) * (whole ? 1.f / sum : 1.f);
+        const int unit = (int)fmaxf(e0, -200.f) + 5, unit_a = unit >> 1;
+        const float f_a = own_f * pow2(unit_a), f_b = pow2(unit - unit_a);
+        float *part = p.part + (int64_t)(2 * blockIdx.x + (old.t0 == 0 ? 1 : 0)) * part_floats(CHUNK, DH);
+        if (g == 0 && row < old.cols) {                  // of the first copy
+          const int c = old.c0 + row, rr = c / ln.group;
+          if (!whole) { part[row * (DH + 4) + DH] = m; part[row * (DH + 4) + DH + 1] = sum; }
+          else if (p.lse) p.lse[(int64_t)(old.row0 + rr) * p.Hq + old.h * ln.group + c - rr * ln.group] = (m + log2f(sum)) * 0.6931471805599453f;
+        }
+        ptx::tc_fence_after_sync();
+        const uint32_t staging = base + T::STAGING + g * (128 * LDS_O * 4);
+#pragma unroll 1
+        for (int i = g * (DH / 2); i < (g + 1) * (DH / 2); i += 16) {
+          uint32_t v[16];
+          ptx::tmem_ld_x16(tOr + i, v);
+          ptx::tmem_ld_wait();
+          if (i + 16 == (g + 1) * (DH / 2)) {
+            ptx::tc_fence_before_sync();
+            __syncwarp();
+            if (lane == 0) ptx::mbar_arrive(bar(B_OFREE));
+          }
+#pragma unroll
+          for (int j = 0; j < 16; j += 4) {
+            uint4 x;
+            uint32_t *xw = &x.x;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) xw[e] = __float_as_uint(__uint_as_float(v[j + e]) * f_a * f_b);
+            ptx::st_shared_v4(staging + row * (LDS_O * 4) + j * 4, x);
+          }
+          output_sync(g);
+          // eight dimensions of a column a thread: they lie in the order 0 4 1 5 2 6 3 7
+          for (int x = threadIdx.x & 127; x < old.cols * 2; x += 128) {
+            const int c = x >> 1, d = (x & 1) * 8;
+            float y[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int e = 0; e < COPIES; ++e) {
+              const uint32_t at = staging + (c + e * CHUNK) * (LDS_O * 4) + d * 4;
+              const uint4 lo = ptx::ld_shared_v4(at), hi = ptx::ld_shared_v4(at + 16);
+              y[0] += __uint_as_float(lo.x); y[4] += __uint_as_float(lo.y); y[1] += __uint_as_float(lo.z); y[5] += __uint_as_float(lo.w);
+              y[2] += __uint_as_float(hi.x); y[6] += __uint_as_float(hi.y); y[3] += __uint_as_float(hi.z); y[7] += __uint_as_float(hi.w);
+            }
+            if (whole) {
+              const int cc = old.c0 + c, rr = cc / ln.group;
+              Vec8<bf16> ov;
+#pragma unroll
+              for (int e = 0; e < 8; ++e) ov.set(e, y[e]);
+              ov.store(p.out + (int64_t)(old.row0 + rr) * p.out_stride + (int64_t)(old.h * ln.group + cc - rr * ln.group) * DH + i + d);
+            } else {
+              float4 *dst = reinterpret_cast<float4 *>(part + c * (DH + 4) + i + d);
+              dst[0] = make_float4(y[0], y[1], y[2], y[3]); dst[1] = make_float4(y[4], y[5], y[6], y[7]);
+            }
+          }
+          output_sync(g);
+        }
+      }
+      if (!more) break;
       float m_own = -INFINITY, l = 0.f, cf = 0.f;    // the reference l is against
       for (int t = w.t0; t < w.t1; ++t, ++tile) {
         if ((tile & 1u) != (uint32_t)g) continue;
@@ -344,13 +435,12 @@ __global__ void __launch_bounds__(THREADS, 1) attention_kv4_tc_kernel(const Attn
         ptx::tc_fence_after_sync();
         if (m_own == -INFINITY) cf = q_factor[piece & 1u][row];
         const uint32_t tSr = tS + lane_base + b * TC_TILE, tSk = tSr + copy * KEYS;
-        float k[NG];
-        int ev[NG], e_top = NONE;
+        float k[NG], ev[NG], e_top = NONE;
 #pragma unroll
         for (int i = 0; i < NG; ++i) {
           ev[i] = expo_v[tile & 3u][copy * NG + i];
-          k[i] = fmaxf(scaled(cf, expo_k[tile & 3u][copy * NG + i] + 9), 1.2e-38f);   // never 0: -inf times it stays -inf
-          e_top = max(e_top, ev[i]);
+          k[i] = fmaxf(cf * expo_k[tile & 3u][copy * NG + i] * 4294967296.f, 1.2e-38f);   // never 0: -inf times it stays -inf
+          e_top = fmaxf(e_top, ev[i]);
         }
         const int left = w.keys - t * TC_TILE - copy * KEYS;
         uint32_t s[HALF];
@@ -376,41 +466,37 @@ __global__ void __launch_bounds__(THREADS, 1) attention_kv4_tc_kernel(const Attn
           }
         }
         // reference and E0: those of the tile before, moved where need be
-        float m_was = -INFINITY;
-        int e_was = NONE;
+        float m_was = -INFINITY, e_was = NONE;
         if (t > w.t0) {
           ok = ptx::mbar_wait_warp(theirs, ((tile - 1) >> 1) & 1u);
           if (!ok) break;
           const float2 x = hand[g ^ 1][row];
-          m_was = x.x; e_was = __float_as_int(x.y);
+          m_was = x.x; e_was = x.y;
         }
-        const int e0 = e_top > e_was ? e_top + 2 : e_was;
-        float fac = e0 == e_was ? 1.f : pow2(max(e_was - e0, -126)), rise = -INFINITY, w_of[NG], o[NG];
+        const float e0 = e_top > e_was ? e_top + 2.f : e_was;
+        float rise = -INFINITY, o[NG];
 #pragma unroll
         for (int i = 0; i < NG; ++i) {               // keys whose values are all 0 have no exponent: they count as E0
-          const int e = ev[i] == NONE ? 0 : max(ev[i] - e0, -120);
-          rise = fmaxf(rise, top[i] + (float)e);
-          o[i] = (float)e; w_of[i] = pow2(-e);
+          o[i] = ev[i] == NONE ? 0.f : fmaxf(ev[i] - e0, -120.f);
+          rise = fmaxf(rise, top[i] + o[i]);
         }
         // a copy whose keys all lie behind the end keeps an open reference
-        float m_ref = m_was;
-        if (m_was == -INFINITY) { m_ref = rise; fac = 0.f; }
-        else if (rise - m_was > LAZY) { m_ref = rise; fac *= ptx::ex2(m_was - rise); }
-        hand[g][row] = make_float2(m_ref, __int_as_float(e0));
+        const bool open = m_was == -INFINITY;
+        const float m_ref = open || rise - m_was > LAZY ? rise : m_was;
+        hand[g][row] = make_float2(m_ref, e0);
         __syncwarp();
         if (lane == 0) ptx::mbar_arrive(mine);
+        const bool moved = t > w.t0 && (m_ref != m_was || e0 != e_was);
         if (m_own != m_ref) l *= m_own == -INFINITY ? 0.f : ptx::ex2(m_own - m_ref);
         m_own = m_ref;
         const float m_use = m_ref == -INFINITY ? 0.f : m_ref;
-#pragma unroll
-        for (int i = 0; i < NG; ++i) o[i] -= m_use;
         // probabilities, the second half first
 #pragma unroll
         for (int from = KEYS - HALF; from >= 0; from -= HALF) {
           if (from != KEYS - HALF) load(from);
 #pragma unroll
           for (int i = 0; i < HG; ++i) {
-            const float kk = k[from / 32 + i], oo = o[from / 32 + i];
+            const float kk = k[from / 32 + i], oo = o[from / 32 + i] - m_use;
             float sum[2] = {0.f, 0.f};
 #pragma unroll
             for (int j = 0; j < 32; j += 2) {
@@ -418,7 +504,7 @@ __global__ void __launch_bounds__(THREADS, 1) attention_kv4_tc_kernel(const Attn
               sum[(j >> 1) & 1] += p0 + p1;
               s[16 * i + (j >> 1)] = pair(p0, p1);
             }
-            l = fmaf(sum[0] + sum[1], w_of[from / 32 + i], l);
+            l = fmaf(sum[0] + sum[1], ptx::ex2(-o[from / 32 + i]), l);
           }
           const uint32_t at = tSr + 64 + (copy * KEYS + from) / 2;
           if (HALF == 64) ptx::tmem_st_x32(at, s); else ptx::tmem_st_x16(at, s);
@@ -430,7 +516,8 @@ __global__ void __launch_bounds__(THREADS, 1) attention_kv4_tc_kernel(const Attn
 #pragma unroll
           for (int c = 0; c < 64; c += 16) if (c / (KEYS / 2) != copy) ptx::tmem_st_x16(tSr + 64 + c, z);
         }
-        if (t > w.t0 && __any_sync(0xffffffffu, fac != 1.f)) {
+        if (__any_sync(0xffffffffu, moved)) {
+          const float fac = open ? 0.f : ptx::ex2(m_was - m_ref + fmaxf(e_was - e0, -126.f));
           // once the product of the tile before is complete
           ok = ptx::mbar_wait_warp(bar(B_VFREE + (b ^ 1u)), ((tile - 1) >> 1) & 1u);
           ptx::tc_fence_after_sync();
@@ -455,77 +542,9 @@ __global__ void __launch_bounds__(THREADS, 1) attention_kv4_tc_kernel(const Attn
       if (!ok) lost = 1;
       softmax_sync();
       if (lost) break;                               // all eight warps or none: they meet at barriers
-      const float2 last = hand[(tile - 1) & 1u][row], x0 = sums[0][row], x1 = sums[1][row];
+      last = hand[(tile - 1) & 1u][row]; x0 = sums[0][row]; x1 = sums[1][row];
+      old = w;
       softmax_sync();                                // the next piece may write them again
-      if (g == 1) continue;
-      // group 0: the copies of a column meet, 32 dimensions at a time
-      const float m_ref = last.x;
-      const int e0 = __float_as_int(last.y);
-      l = x0.y * (x0.x == -INFINITY ? 0.f : ptx::ex2(x0.x - m_ref)) + x1.y * (x1.x == -INFINITY ? 0.f : ptx::ex2(x1.x - m_ref));
-      ml[row] = make_float2(m_ref, l);
-      ok = ok && ptx::mbar_wait_warp(bar(B_VFREE + ((tile - 1) & 1u)), ((tile - 1) >> 1) & 1u);
-      output_sync();
-      float m = -INFINITY, sum = 0.f;
-#pragma unroll
-      for (int i = 0; i < COPIES; ++i) m = fmaxf(m, ml[col + i * CHUNK].x);
-#pragma unroll
-      for (int i = 0; i < COPIES; ++i) {
-        const float2 x = ml[col + i * CHUNK];
-        sum = fmaf(x.y, x.x == -INFINITY ? 0.f : ptx::ex2(x.x - m), sum);
-      }
-      const bool whole = w.t0 == 0 && w.t1 == w.nt;
-      // the lane's own factor: to the common reference, and the quotient where the item is whole
-      const float own_f = (m_ref == -INFINITY ? 0.f : ptx::ex2(m_ref - m)) * (whole ? 1.f / sum : 1.f);
-      float *part = p.part + (int64_t)(2 * blockIdx.x + (w.t0 == 0 ? 1 : 0)) * part_floats(CHUNK, DH);
-      if (row < w.cols) {                            // of the first copy
-        const int c = w.c0 + row, rr = c / ln.group;
-        if (!whole) { part[row * (DH + 4) + DH] = m; part[row * (DH + 4) + DH + 1] = sum; }
-        else if (p.lse) p.lse[(int64_t)(w.row0 + rr) * p.Hq + w.h * ln.group + c - rr * ln.group] = (m + log2f(sum)) * 0.6931471805599453f;
-      }
-      ptx::tc_fence_after_sync();
-      const uint32_t staging = base + T::STAGING;
-      for (int i = 0; i < DH; i += 32) {
-        uint32_t v[32];
-        ptx::tmem_ld_x32(tOr + i, v);
-        ptx::tmem_ld_wait();
-        if (i + 32 == DH) {
-          ptx::tc_fence_before_sync();
-          __syncwarp();
-          if (lane == 0) ptx::mbar_arrive(bar(B_OFREE));
-        }
-#pragma unroll
-        for (int j = 0; j < 32; j += 4) {
-          uint4 x;
-          uint32_t *xw = &x.x;
-#pragma unroll
-          for (int e = 0; e < 4; ++e) xw[e] = __float_as_uint(scaled(__uint_as_float(v[j + e]), max(e0, -200) + 5) * own_f);
-          ptx::st_shared_v4(staging + row * (LDS_O * 4) + j * 4, x);
-        }
-        output_sync();
-        // eight dimensions of a column a thread: they lie in the order 0 4 1 5 2 6 3 7
-        for (int x = threadIdx.x; x < w.cols * 4; x += 128) {
-          const int c = x >> 2, d = (x & 3) * 8;
-          float y[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-          for (int e = 0; e < COPIES; ++e) {
-            const uint32_t at = staging + (c + e * CHUNK) * (LDS_O * 4) + d * 4;
-            const uint4 lo = ptx::ld_shared_v4(at), hi = ptx::ld_shared_v4(at + 16);
-            y[0] += __uint_as_float(lo.x); y[4] += __uint_as_float(lo.y); y[1] += __uint_as_float(lo.z); y[5] += __uint_as_float(lo.w);
-            y[2] += __uint_as_float(hi.x); y[6] += __uint_as_float(hi.y); y[3] += __uint_as_float(hi.z); y[7] += __uint_as_float(hi.w);
-          }
-          if (whole) {
-            const int cc = w.c0 + c, rr = cc / ln.group;
-            Vec8<bf16> ov;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) ov.set(e, y[e]);
-            ov.store(p.out + (int64_t)(w.row0 + rr) * p.out_stride + (int64_t)(w.h * ln.group + cc - rr * ln.group) * DH + i + d);
-          } else {
-            float4 *dst = reinterpret_cast<float4 *>(part + c * (DH + 4) + i + d);
-            dst[0] = make_float4(y[0], y[1], y[2], y[3]); dst[1] = make_float4(y[4], y[5], y[6], y[7]);
-          }
-        }
-        output_sync();
-      }
     }
     if (!ok || lost) { fail(status, DEV_TIMEOUT_EPILOGUE); abort_flag = 1; }
   }
