@@ -89,8 +89,9 @@ __device__ __forceinline__ float query_factor(float scale_log2, int u) {
 }
 
 template <int DH, int NT> struct AttnShape {
-  static constexpr int CH = 8 * NT, TILE = KV4_TILE * (DH + 8), STAGES = 3, RING = STAGES * TILE;
-  static constexpr int CTAS = NT == 1 ? 4 : 3;     // an SM's, as registers allow
+  static constexpr int CH = 8 * NT, TILE = KV4_TILE * (DH + 8), STAGES = NT == 4 ? 4 : 3, RING = STAGES * TILE;
+  static constexpr int CTAS = NT == 1 ? 4 : NT == 2 ? 3 : 2;   // an SM's, as registers allow
+  static constexpr bool Q_REGS = NT < 4;           // queries in registers; with 32 columns they are read from shared memory where they are used
   static constexpr int META = KV4_TILE * 24, QBYTES = NT * DH * 16;
   static constexpr int OFF_META = WARPS * RING, OFF_Q = OFF_META + WARPS * META, SMEM = OFF_Q + QBYTES;
 };
@@ -98,7 +99,7 @@ template <int DH, int NT> struct AttnShape {
 template <int DH, int NT>
 __global__ void __launch_bounds__(WARPS * 32, AttnShape<DH, NT>::CTAS) attention_kv4_kernel(const AttnParams p) {
   using Sh = AttnShape<DH, NT>;
-  constexpr int W = DH / 32, MT = DH / 16, CH = Sh::CH, MS = NT == 1 ? 2 : 1;   // MS: groups of 16 keys taken together
+  constexpr int W = DH / 32, MT = DH / 16, CH = Sh::CH, MS = NT == 2 ? 1 : 2;   // MS: groups of 16 keys taken together
   constexpr int TILE = Sh::TILE, RING = Sh::RING, STAGES = Sh::STAGES, LDO = DH + 4;
   static_assert(KV4_TILE == 32 && CH * LDO * 4 <= RING, "a warp's output goes to its ring");
   extern __shared__ __align__(128) uint8_t smem[];
@@ -171,14 +172,14 @@ __global__ void __launch_bounds__(WARPS * 32, AttnShape<DH, NT>::CTAS) attention
       for (int j = 0; j < W; ++j) qs[(warp * W + j) * 32 + lane] = make_uint4(f[4 * j], f[4 * j + 1], f[4 * j + 2], f[4 * j + 3]);
     }
     __syncthreads();
-    uint32_t qf[NT][DH / 8];
+    uint32_t qf[Sh::Q_REGS ? NT : 1][DH / 8];
     F2 cs[NT];                                     // columns 2t and 2t + 1 of each eight
     F2 neg_m[NT], l[NT], wm[NT];                   // minus the reference, sum of probabilities, sum of probability times m
     float o[MT][NT][4];
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
 #pragma unroll
-      for (int j = 0; j < W; ++j) *reinterpret_cast<uint4 *>(&qf[n][4 * j]) = qs[(n * W + j) * 32 + lane];
+      for (int j = 0; Sh::Q_REGS && j < W; ++j) *reinterpret_cast<uint4 *>(&qf[Sh::Q_REGS ? n : 0][4 * j]) = qs[(n * W + j) * 32 + lane];
       cs[n] = ptx::f2(qsum[8 * n + 2 * t], qsum[8 * n + 2 * t + 1]);
       neg_m[n] = l[n] = wm[n] = ptx::f2(0.f, 0.f);
 #pragma unroll
@@ -238,19 +239,24 @@ __global__ void __launch_bounds__(WARPS * 32, AttnShape<DH, NT>::CTAS) attention
           uint32_t x[MS][4], y[MS][4];
 #pragma unroll
           for (int u = 0; u < MS; ++u) { spread(ka[u][j], x[u]); spread(kb[u][j], y[u]); }
+          uint4 q4[NT];
+#pragma unroll
+          for (int n = 0; n < NT; ++n)
+            q4[n] = Sh::Q_REGS ? make_uint4(qf[Sh::Q_REGS ? n : 0][4 * j], qf[Sh::Q_REGS ? n : 0][4 * j + 1], qf[Sh::Q_REGS ? n : 0][4 * j + 2], qf[Sh::Q_REGS ? n : 0][4 * j + 3])
+                               : qs[(n * W + j) * 32 + lane];
           // one step of all sums, then the next: a sum's steps depend on one another
 #pragma unroll
           for (int u = 0; u < MS; ++u)
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
-              if (j == 0) ptx::mma_f16_16x8x16_first(acc[u][n], x[u][0], y[u][0], x[u][1], y[u][1], qf[n][0], qf[n][1]);
-              else ptx::mma_f16_16x8x16(acc[u][n], x[u][0], y[u][0], x[u][1], y[u][1], qf[n][4 * j], qf[n][4 * j + 1]);
+              if (j == 0) ptx::mma_f16_16x8x16_first(acc[u][n], x[u][0], y[u][0], x[u][1], y[u][1], q4[n].x, q4[n].y);
+              else ptx::mma_f16_16x8x16(acc[u][n], x[u][0], y[u][0], x[u][1], y[u][1], q4[n].x, q4[n].y);
             }
 #pragma unroll
           for (int u = 0; u < MS; ++u)
 #pragma unroll
             for (int n = 0; n < NT; ++n)
-              ptx::mma_f16_16x8x16(acc[u][n], x[u][2], y[u][2], x[u][3], y[u][3], qf[n][4 * j + 2], qf[n][4 * j + 3]);
+              ptx::mma_f16_16x8x16(acc[u][n], x[u][2], y[u][2], x[u][3], y[u][3], q4[n].z, q4[n].w);
         }
         // scores against the reference
         float top = -INFINITY;
@@ -473,18 +479,20 @@ __global__ void __launch_bounds__(128) kv4_join_kernel(const AttnParams p, int n
   if (lane == 0 && lse) *lse = (m + log2f(l)) * 0.6931471805599453f;
 }
 
-// Up to 8 columns: the warp-level kernel, whose operands never leave registers.  More: tcgen05 with 32, 64 or 128 lanes.
+// Up to 32 columns: the warp-level kernel, whose operands never leave registers.  More: tcgen05 with 64 or 128 lanes.  (8 sequences of
+// 32 heads, us at 128 / 2048 / 8192 keys: 16 columns 13 / 42 / 83 against 20 / 45 / 124 on tcgen05, 32 columns 16 / 44 / 130 against 21 / 47 / 128;
+// heads of 64: 10 / 31 / 56 against 15 / 36 / 103, 12 / 29 / 83 against 17 / 37 / 103.)
 struct AttnPlan { int chunk, ctas, tc; };
 
 AttnPlan plan_attention(int heads, int B, int rows, int Hq, int max_len, int sms) {
   AttnPlan pl;
   const int cols = rows * (Hq / heads);
-  pl.tc = cols > 8;
-  pl.chunk = cols <= 8 ? 8 : cols <= 32 ? 32 : cols <= 64 ? 64 : 128;
+  pl.tc = cols > 32;
+  pl.chunk = cols <= 8 ? 8 : cols <= 16 ? 16 : cols <= 32 ? 32 : cols <= 64 ? 64 : 128;
   // no more CTAs than there are tiles for each, or for each warp of them
   const int64_t items = (int64_t)B * heads * ceil_div(cols, pl.chunk);
   const int64_t want = pl.tc ? items * ceil_div(max_len, TC_TILE) : ceil_div64(items * ceil_div(max_len, KV4_TILE), WARPS);
-  const int most = pl.tc ? sms : sms * 4;
+  const int most = pl.tc ? sms : sms * (pl.chunk == 8 ? 4 : pl.chunk == 16 ? 3 : 2);
   pl.ctas = (int)(want < 1 ? 1 : want < most ? want : most);
   return pl;
 }
@@ -524,10 +532,12 @@ cudaError_t launch_attention_kv4(cudaStream_t st, const Kv4AttnArgs &a, int sms)
   Line &ln = p.line;
   ln.B = a.b.B; ln.H = a.c.heads; ln.chunk = pl.chunk; ln.group = a.Hq / a.c.heads; ln.slots = a.c.slots;
   ln.max_keys = a.max_len < a.c.cap ? a.max_len : a.c.cap; ln.tile_keys = pl.tc ? TC_TILE : KV4_TILE; ln.min_chunks = 0; ln.b = a.b;
+  ln.sms = sms; ln.piece = pl.tc ? 7 : 512 / pl.chunk;
   const int cols = a.b.rows * ln.group;
   cudaError_t e;
   if (pl.tc) e = launch_attention_kv4_tc(st, p, a.c.dh, pl.ctas);
-  else e = a.c.dh == 128 ? launch_attn<128, 1>(st, p, pl.ctas) : launch_attn<64, 1>(st, p, pl.ctas);
+  else if (a.c.dh == 128) e = pl.chunk == 8 ? launch_attn<128, 1>(st, p, pl.ctas) : pl.chunk == 16 ? launch_attn<128, 2>(st, p, pl.ctas) : launch_attn<128, 4>(st, p, pl.ctas);
+  else e = pl.chunk == 8 ? launch_attn<64, 1>(st, p, pl.ctas) : pl.chunk == 16 ? launch_attn<64, 2>(st, p, pl.ctas) : launch_attn<64, 4>(st, p, pl.ctas);
   if (e != cudaSuccess) return e;
   return a.c.dh == 128 ? launch_join<128>(st, p, pl.ctas, cols) : launch_join<64>(st, p, pl.ctas, cols);
 }
@@ -729,7 +739,7 @@ cudaError_t launch_kv4_weights(cudaStream_t st, const Kv4WeighArgs &a, int sms) 
   Line &ln = p.line;
   // one item a head, whatever its columns: a key's weight is written by one thread.  Sequences without rows too: their weights are copied
   ln.B = a.b.B; ln.H = a.c.heads; ln.chunk = 0x7fffffff; ln.min_chunks = 1; ln.group = a.Hq / a.c.heads; ln.slots = a.c.slots;
-  ln.max_keys = a.max_len < a.c.cap ? a.max_len : a.c.cap; ln.tile_keys = KV4_TILE; ln.b = a.b;
+  ln.max_keys = a.max_len < a.c.cap ? a.max_len : a.c.cap; ln.tile_keys = KV4_TILE; ln.b = a.b; ln.sms = sms; ln.piece = 32;
   const int64_t want = ceil_div64((int64_t)a.b.B * a.c.heads * ceil_div(ln.max_keys, KV4_TILE), WARPS);
   const int ctas = (int)(want < 1 ? 1 : want < sms * 4 ? want : sms * 4);
   return a.c.dh == 128 ? launch_weigh<128>(st, p, ctas) : launch_weigh<64>(st, p, ctas);

@@ -14,7 +14,7 @@ constexpr float LAZY = 6.0f;         // log2 units the running maximum may pass 
 // sequences are one round of loads.
 struct Seq { int keys, rows, row0, slot, tiles, chunks; uint32_t count; };
 struct Line {
-  int B, H, chunk, group, slots, max_keys, tile_keys, min_chunks;
+  int B, H, chunk, group, slots, max_keys, tile_keys, min_chunks, sms, piece;   // piece: see survey
   Kv4Batch b;
   __device__ __forceinline__ Seq seq(int s) const {
     Seq q = {0, 0, 0, -1, 0, 0, 0u};
@@ -28,8 +28,9 @@ struct Line {
     return q;
   }
   // Tiles of the line and of a CTA's run; *before: tiles of the sequences ahead of `upto`.  `own` is seq(lane).  (Whole warp.)
-  // Sequences of one length: whole items where that costs the longest run no more than a fifth, since a split item's halves go
-  // through memory.
+  // Equal runs split items, and every piece of one costs a CTA its queries, its output and, split, a way through memory: about what
+  // an SM takes for `piece` tiles.  Sequences of one length: whole items where the SM with most of them is done sooner (8 x 16 rows of
+  // 32 heads on 512 keys: 22 us split, 16 whole; on 8192 keys 83 split).  An SM with fewer CTAs than fit takes longer for a tile.
   __device__ uint32_t survey(const Seq &own, uint32_t ctas, int upto, uint32_t *share, uint32_t *before) const {
     const int lane = threadIdx.x & 31;
     uint32_t total = 0, ahead = 0, lo = 0xffffffffu, hi = 0;
@@ -44,8 +45,9 @@ struct Line {
     }
     uint32_t even = (total + ctas - 1) / ctas;
     if (lo == hi && hi) {
-      const uint32_t whole = (total / hi + ctas - 1) / ctas * hi;
-      if (whole <= even + even / 5) even = whole;
+      const uint32_t items = total / hi, rounds = (items + ctas - 1) / ctas;
+      const float most = items <= ctas ? 1.15f * ((items + sms - 1) / sms) * hi : (float)rounds * hi * ctas / sms;
+      if (most + (float)piece * rounds <= (float)total / sms + (float)piece * (1.f + (float)even / hi)) even = rounds * hi;
     }
     *share = even;
     if (before) *before = ahead;

@@ -1,4 +1,4 @@
-// Attention over a key/value cache in 4 bits on the 5th-generation tensor cores, for 9 to 128 columns (query rows times query heads
+// Attention over a key/value cache in 4 bits on the 5th-generation tensor cores, for 33 to 128 columns (query rows times query heads
 // that share a key head) of a sequence and key head at once.
 //
 // S = Q K^T and O += P V, the columns on the M side (128 lanes of tensor memory), tiles of 128 keys.  Eight warps turn codes into
@@ -16,8 +16,7 @@
 // of its lane before its exponentials.  128 keys of a lane are worked on in two halves, the second first: its probabilities go
 // over its own scores while the first half still stands.
 //
-// Fewer columns than lanes: chunks of 32 (64) columns stand four times (twice) in the lanes, and each copy takes its quarter (half) of a
-// tile's keys, its probabilities of the others being 0.  The tensor pipe and shared memory do the same work as for 128 columns, but the
+// Fewer columns than lanes: chunks of 64 columns stand twice in the lanes, and each copy takes its half of a tile's keys, its probabilities of the others being 0.  The tensor pipe and shared memory do the same work as for 128 columns, but the
 // exponentials are spread over all warps; the copies are added at the end.
 //
 // What bounds it: shared memory.  128 keys of 128: 17 KB of codes in and out, 64 KB of operands out and in: 1300 cycles at 128 bytes; the
@@ -573,7 +572,6 @@ template <int DH, int COPIES> cudaError_t launch(cudaStream_t st, const AttnPara
 
 template <int DH> cudaError_t launch_chunk(cudaStream_t st, const AttnParams &p, int ctas) {
   switch (p.line.chunk) {
-    case 32: return launch<DH, 4>(st, p, ctas);
     case 64: return launch<DH, 2>(st, p, ctas);
     default: return launch<DH, 1>(st, p, ctas);
   }
