@@ -512,7 +512,8 @@ int64_t attention_kv4_scratch_floats(const Kv4View &c, int B, int rows, int Hq, 
 template <int DH, int NT>
 static cudaError_t launch_attn(cudaStream_t st, const AttnParams &p, int ctas) {
   constexpr int smem = AttnShape<DH, NT>::SMEM;
-  cudaError_t e = cudaFuncSetAttribute(attention_kv4_kernel<DH, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  static std::atomic<uint64_t> done{0};
+  const cudaError_t e = allow_shared((const void *)attention_kv4_kernel<DH, NT>, smem, done);
   if (e != cudaSuccess) return e;
   return launch_kernel(attention_kv4_kernel<DH, NT>, dim3(ctas), dim3(WARPS * 32), (size_t)smem, st, p);
 }
@@ -725,7 +726,8 @@ __global__ void __launch_bounds__(WARPS * 32, 4) kv4_weights_kernel(const WeighP
 
 template <int DH> cudaError_t launch_weigh(cudaStream_t st, const WeighParams &p, int ctas) {
   constexpr int smem = WeighShape<DH>::SMEM;
-  cudaError_t e = cudaFuncSetAttribute(kv4_weights_kernel<DH>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  static std::atomic<uint64_t> done{0};
+  const cudaError_t e = allow_shared((const void *)kv4_weights_kernel<DH>, smem, done);
   if (e != cudaSuccess) return e;
   return launch_kernel(kv4_weights_kernel<DH>, dim3(ctas), dim3(WARPS * 32), (size_t)smem, st, p);
 }

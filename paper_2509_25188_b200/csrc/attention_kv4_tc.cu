@@ -565,7 +565,8 @@ __global__ void __launch_bounds__(THREADS, 1) attention_kv4_tc_kernel(const Attn
 
 template <int DH, int COPIES> cudaError_t launch(cudaStream_t st, const AttnParams &p, int ctas) {
   constexpr int smem = Tc<DH>::BYTES + 1024;
-  cudaError_t e = cudaFuncSetAttribute(attention_kv4_tc_kernel<DH, COPIES>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  static std::atomic<uint64_t> done{0};
+  const cudaError_t e = allow_shared((const void *)attention_kv4_tc_kernel<DH, COPIES>, smem, done);
   if (e != cudaSuccess) return e;
   return launch_kernel(attention_kv4_tc_kernel<DH, COPIES>, dim3(ctas), dim3(THREADS), (size_t)smem, st, p);
 }

@@ -463,7 +463,8 @@ cudaError_t launch_kv4_evict(cudaStream_t st, const Kv4EvictArgs &a) {
   const int slice = ceil_div(ceil_div(a.max_len > 1 ? a.max_len : 1, cluster), 32) * 32;
   const size_t smem = (size_t)slice / 32 * 8 + (slice <= SELECT_CACHE ? (size_t)slice * 4 : 0);
   cudaError_t e = cudaSuccess;
-  if (smem > 32 * 1024) e = cudaFuncSetAttribute(kv4_select_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, SELECT_CACHE * 4 + KV4_MAX_EVICT / 8 / 4);
+  static std::atomic<uint64_t> done{0};
+  if (smem > 32 * 1024) e = allow_shared((const void *)kv4_select_kernel, SELECT_CACHE * 4 + KV4_MAX_EVICT / 8 / 4, done);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(a.src.heads * cluster, a.b.B); cfg.blockDim = dim3(SELECT_THREADS); cfg.dynamicSmemBytes = smem; cfg.stream = st;

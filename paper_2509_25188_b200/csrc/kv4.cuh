@@ -11,6 +11,8 @@
 // half.  Head size 128: in V rows of keys 4..7 of every eight, the two halves of a row change places, so that the four keys whose
 // rows a warp reads at once (4 keys x 32 bytes) lie in different banks.
 #pragma once
+#include <atomic>
+
 #include "common.cuh"
 
 namespace l2pd {
@@ -24,6 +26,16 @@ __host__ __device__ __forceinline__ int kv4_off_vmeta(int dh) { return KV4_TILE 
 __host__ __device__ __forceinline__ int kv4_off_v(int dh) { return KV4_TILE * dh / 2 + KV4_TILE * 8; }
 // byte b of the V row of tile row r lies at byte b ^ kv4_v_swizzle
 __host__ __device__ __forceinline__ int kv4_v_swizzle(int r, int dh) { return dh == 128 ? ((r >> 2) & 1) << 5 : 0; }
+
+// Raises a kernel's shared-memory limit once a device; `done` has a bit a device.
+inline cudaError_t allow_shared(const void *kernel, int bytes, std::atomic<uint64_t> &done) {
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess || (dev < 64 && (done.load(std::memory_order_relaxed) >> dev & 1u))) return e;
+  e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  if (e == cudaSuccess && dev < 64) done.fetch_or(1ull << dev, std::memory_order_relaxed);
+  return e;
+}
 
 struct Kv4View {
   uint8_t *data;

@@ -225,6 +225,25 @@ def test_rising_scores_move_the_reference(rows):
     _check_attention(q, k, v, out, lse, 0.7)
 
 
+@pytest.mark.parametrize("dh", [64, 128])
+@pytest.mark.parametrize("scale", [0.0, -0.1, 3.0])
+@pytest.mark.parametrize("rows", [2, 12, 20, 40, 130])
+def test_any_scale_and_ragged_last_tiles(rows, scale, dh):
+    b = _b()
+    c = b.KvCache4(2, 1, dh, 300)
+    k, v = _rand(41, 2, 300, 1, dh), _rand(42, 2, 300, 1, dh)
+    k[:, 200:], v[:, 200:] = float("nan"), float("nan")
+    k[0, 64:96] = 0                                                     # a group of keys, and one of values, without magnitude
+    v[0, 32:64] = 0
+    v[1, :33] = 0
+    q = _rand(43, 2, rows, 1, dh)
+    c.store(k, v)
+    lens = [131, 33]
+    out, lse = c.attention(q, _i32(lens), 300, scale=scale)
+    for i, n in enumerate(lens):
+        _check_attention(q[i], k[i, :n], v[i, :n], out[i], lse[i], scale)
+
+
 @pytest.mark.parametrize("rows", [2, 40])
 def test_nan_stays_where_it_belongs(rows):
     b = _b()
@@ -413,6 +432,19 @@ def test_evict(into, kind, heads, dh, lens, keep, first, guard):
             else:
                 assert torch.equal(po[s, h, m:], p0[s, h, m:])
                 _same(gk[s, m:, h], ak[s, m:, h])
+
+
+def test_evict_longer_than_a_cluster_keeps_at_hand():
+    b = _b()
+    n, keep = 300000, 5000
+    c, into = b.KvCache4(1, 1, 64, n), b.KvCache4(1, 1, 64, keep)
+    k = _rand(44, 1, n, 1, 64)
+    c.store(k, k)
+    w = torch.round(torch.rand(1, 1, n, device=DEV) * 64) / 64          # thousands of equal weights at the border
+    kept, new = c.evict(w, _i32([n]), n, keep, into=into)
+    want = plain.keep(_np(w)[0, 0], range(n), n, keep, 0, 2 ** 31 - 1)
+    assert kept[0, 0].tolist() == want and new.tolist() == [keep]
+    _same(into.load(keep, dtype=torch.float32)[0][0, :, 0], plain.values32(_np(k[0, want, 0])))
 
 
 def test_evict_without_positions_and_twice():
