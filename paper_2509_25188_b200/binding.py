@@ -484,29 +484,37 @@ def attention_bf16(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, H: int, dh
 
 # ---- operators around a key/value cache in 4 bits --------------------------------------------------------------------
 
-def _rows(x: torch.Tensor, heads: int, dh: int, what: str, dtype=torch.bfloat16) -> int:
-    """Row stride of a packed batch [N, heads, dh] or [B, rows, heads, dh], after the checks the library cannot make."""
+# A call costs the host more than a small batch costs the GPU: the checks read a tensor's attributes once each, and fresh results
+# are made the way torch makes them fastest (empty_like of a contiguous tensor, or one flat size).
+
+def _rows(x: torch.Tensor, heads: int, dh: int, what: str, index: int, dtype=torch.bfloat16) -> int:
+    """Row stride of a packed batch [N, heads, dh] or [B, rows, heads, dh] on GPU `index`, after the checks the library cannot make."""
     shape = x.shape
-    if x.dtype is not dtype or not x.is_cuda:
-        raise ValueError("%s must be a %s tensor on a GPU" % (what, dtype))
-    if len(shape) not in (3, 4) or shape[-2] != heads or shape[-1] != dh:
+    n = len(shape)
+    if x.dtype is not dtype or x.get_device() != index:
+        raise ValueError("%s must be a %s tensor on cuda:%d" % (what, dtype, index))
+    if not 3 <= n <= 4 or shape[n - 2] != heads or shape[n - 1] != dh:
         raise ValueError("%s must be [rows, %d, %d] or [sequences, rows, %d, %d]" % (what, heads, dh, heads, dh))
     if x.is_contiguous():
         return heads * dh
     st = x.stride()
-    four = len(shape) == 4 and shape[0] > 1
+    four = n == 4 and shape[0] > 1
     if st[-1] != 1 or (heads > 1 and st[-2] != dh) or (four and shape[1] > 1 and st[0] != shape[1] * st[1]):
         raise ValueError("%s: heads and their numbers must be contiguous, sequences one row stride apart" % what)
     return st[-3] if shape[-3] > 1 else st[0] if four else heads * dh
 
 
-def _ints(x: Optional[torch.Tensor], n: int, what: str, device):
+def _ints(x: Optional[torch.Tensor], n: int, what: str, index: int):
     """Address of an int32 array of at least n entries, or None."""
     if x is None:
         return None
-    if x.dtype is not torch.int32 or x.device != device or not x.is_contiguous() or x.numel() < n:
-        raise ValueError("%s must be a contiguous int32 tensor of at least %d entries on %s" % (what, n, device))
+    if x.dtype is not torch.int32 or x.get_device() != index or x.numel() < n or not x.is_contiguous():
+        raise ValueError("%s must be a contiguous int32 tensor of at least %d entries on cuda:%d" % (what, n, index))
     return x.data_ptr()
+
+
+def _fresh(like: torch.Tensor) -> torch.Tensor:
+    return torch.empty_like(like) if like.is_contiguous() else torch.empty_like(like, memory_format=torch.contiguous_format)
 
 
 _device_now, _raw_stream = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
@@ -525,66 +533,57 @@ class KvCache4:
         self.slots, self.heads, self.head_dim, self.capacity = slots, heads, head_dim, capacity
         self.data = torch.zeros(n, dtype=torch.uint8, device="cuda:%d" % device)
         self.device = self.data.device
-        self._index = self.device.index
+        self._index = self.data.get_device()
+        self._scale = 1.0 / head_dim ** 0.5
         self._c = Kv4(self.data.data_ptr(), slots, heads, head_dim, capacity)
         self._ref = C.addressof(self._c)
         self._scratch = {}
 
-    def _stream(self) -> int:
-        return _raw_stream(self._index)
-
-    def _elsewhere(self) -> bool:
-        """The cache's device is not the current one: the call runs again with it as the current one."""
-        return _device_now() != self._index
-
     def _batch(self, x: torch.Tensor, row_start: Optional[torch.Tensor], max_rows: Optional[int]):
         """(sequences, most rows of one, address of row_start) of a packed batch."""
-        if x.device != self.device:
-            raise ValueError("a tensor is not on the cache's device %s" % self.device)
-        if x.dim() == 4:
-            if row_start is not None:
-                raise ValueError("row_start goes with packed rows [N, heads, head_dim]")
-            return x.shape[0], x.shape[1], None
-        if row_start is None:
-            return 1, x.shape[0], None
-        if max_rows is None:
-            raise ValueError("row_start needs max_rows, the most rows of a sequence")
-        return row_start.numel() - 1, max_rows, _ints(row_start, 1, "row_start", self.device)
+        if row_start is not None:
+            if max_rows is None or x.dim() != 3:
+                raise ValueError("row_start goes with packed rows [N, heads, head_dim] and max_rows, the most rows of a sequence")
+            return row_start.numel() - 1, max_rows, _ints(row_start, 1, "row_start", self._index)
+        shape = x.shape
+        return (shape[0], shape[1], None) if len(shape) == 4 else (1, shape[0], None)
 
     def store(self, k: torch.Tensor, v: torch.Tensor, key_start=None, slots=None, row_start=None, max_rows=None):
         """Row r of sequence i becomes key key_start[i] + r (key_start None: r) of slot slots[i] (None: i)."""
-        if self._elsewhere():
-            with torch.cuda.device(self._index):
+        index = self._index
+        if _device_now() != index:                  # runs again with the cache's device as the current one
+            with torch.cuda.device(index):
                 return self.store(k, v, key_start, slots, row_start, max_rows)
-        ks, vs = _rows(k, self.heads, self.head_dim, "k"), _rows(v, self.heads, self.head_dim, "v")
-        if k.shape != v.shape or v.device != self.device:
-            raise ValueError("k and v differ in shape or device")
+        ks, vs = _rows(k, self.heads, self.head_dim, "k", index), _rows(v, self.heads, self.head_dim, "v", index)
+        if k.shape != v.shape:
+            raise ValueError("k and v differ in shape")
         b, rows, rs = self._batch(k, row_start, max_rows)
-        _check(lib.l2pd_kv4_store(self._stream(), self._ref, k.data_ptr(), v.data_ptr(), b, rows, rs, _ints(slots, b, "slots", self.device),
-                                  _ints(key_start, b, "key_start", self.device), ks, vs))
+        _check(lib.l2pd_kv4_store(_raw_stream(index), self._ref, k.data_ptr(), v.data_ptr(), b, rows, rs, _ints(slots, b, "slots", index),
+                                  _ints(key_start, b, "key_start", index), ks, vs))
 
     def load(self, rows: int, key_start=None, slots=None, row_start=None, total_rows=None, dtype=torch.bfloat16):
         """The values of `rows` keys of each sequence, from key_start[i] on: (k, v), [sequences, rows, heads, head_dim].  With
         row_start: packed [total_rows, heads, head_dim], at most `rows` of a sequence."""
-        if self._elsewhere():
-            with torch.cuda.device(self._index):
+        index = self._index
+        if _device_now() != index:                  # runs again with the cache's device as the current one
+            with torch.cuda.device(index):
                 return self.load(rows, key_start, slots, row_start, total_rows, dtype)
         if dtype not in (torch.bfloat16, torch.float32):
             raise ValueError("dtype is torch.bfloat16 or torch.float32")
+        heads, dh = self.heads, self.head_dim
         if row_start is not None:
             if total_rows is None:
                 raise ValueError("row_start needs total_rows, the rows of the packed result")
-            b, shape = row_start.numel() - 1, (total_rows, self.heads, self.head_dim)
+            b, n, shape = row_start.numel() - 1, total_rows, (total_rows, heads, dh)
         else:
             given = slots if slots is not None else key_start
             b = self.slots if given is None else given.numel()
-            shape = (b, rows, self.heads, self.head_dim)
-        k = torch.empty(shape, dtype=dtype, device=self.device)
+            n, shape = b * rows, (b, rows, heads, dh)
+        k = torch.empty(n * heads * dh, dtype=dtype, device=self.device).view(shape)
         v = torch.empty_like(k)
-        st = self.heads * self.head_dim
-        _check(lib.l2pd_kv4_load(self._stream(), self._ref, L2PD_BF16 if dtype is torch.bfloat16 else L2PD_F32, k.data_ptr(), v.data_ptr(), b, rows,
-                                 _ints(row_start, b + 1, "row_start", self.device), _ints(slots, b, "slots", self.device),
-                                 _ints(key_start, b, "key_start", self.device), st, st))
+        _check(lib.l2pd_kv4_load(_raw_stream(index), self._ref, L2PD_BF16 if dtype is torch.bfloat16 else L2PD_F32, k.data_ptr(), v.data_ptr(), b, rows,
+                                 _ints(row_start, b + 1, "row_start", index), _ints(slots, b, "slots", index),
+                                 _ints(key_start, b, "key_start", index), heads * dh, heads * dh))
         return k, v
 
     def _scratch_bytes(self, b: int, rows: int, hq: int, max_len: int) -> int:
@@ -601,32 +600,33 @@ class KvCache4:
                   scale: Optional[float] = None, out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None, check: bool = False):
         """Softmax attention of q [.., Hq, head_dim] over the first lens[i] keys of each sequence, lens[i] <= max_len; scale None:
         1 / sqrt(head_dim).  Returns (out, lse), q's shape in bf16 and [.., Hq] in fp32."""
-        if self._elsewhere():
-            with torch.cuda.device(self._index):
+        index = self._index
+        if _device_now() != index:                  # runs again with the cache's device as the current one
+            with torch.cuda.device(index):
                 return self.attention(q, lens, max_len, row_start, max_rows, slots, scale, out, lse, check)
-        shape, device, dh = q.shape, self.device, self.head_dim
+        shape, dh = q.shape, self.head_dim
         hq = shape[-2]
-        qs = _rows(q, hq, dh, "q")
+        qs = _rows(q, hq, dh, "q", index)
         b, rows, rs = self._batch(q, row_start, max_rows)
         if out is None:
-            out, os = torch.empty(shape, dtype=torch.bfloat16, device=device), hq * dh
+            out, os = _fresh(q), hq * dh
         else:
-            os = _rows(out, hq, dh, "out")
+            os = _rows(out, hq, dh, "out", index)
+            if out.shape != shape:
+                raise ValueError("out must have q's shape")
         if lse is None:
-            lse = torch.empty(shape[:-1], dtype=torch.float32, device=device)
-        elif lse.shape != shape[:-1] or lse.dtype is not torch.float32 or lse.device != device or not lse.is_contiguous():
-            raise ValueError("lse must be [.., Hq] in contiguous fp32 on %s" % device)
-        if out.shape != shape or out.device != device:
-            raise ValueError("out must have q's shape and device")
+            lse = torch.empty(q.numel() // dh, dtype=torch.float32, device=self.device).view(shape[:-1])
+        elif lse.shape != shape[:-1] or lse.dtype is not torch.float32 or lse.get_device() != index or not lse.is_contiguous():
+            raise ValueError("lse must be [.., Hq] in contiguous fp32 on cuda:%d" % index)
         n = self._scratch_bytes(b, rows, hq, max_len)
-        scratch = torch.empty(n, dtype=torch.uint8, device=device)
-        _check(lib.l2pd_attention_kv4(self._stream(), self._ref, q.data_ptr(), out.data_ptr(), lse.data_ptr(), b, rows, rs,
-                                      _ints(slots, b, "slots", device), _ints(lens, b, "lens", device), max_len, hq, qs, os,
-                                      1.0 / dh ** 0.5 if scale is None else scale, scratch.data_ptr(), n, check))
+        scratch = torch.empty(n, dtype=torch.uint8, device=self.device)
+        _check(lib.l2pd_attention_kv4(_raw_stream(index), self._ref, q.data_ptr(), out.data_ptr(), lse.data_ptr(), b, rows, rs,
+                                      _ints(slots, b, "slots", index), _ints(lens, b, "lens", index), max_len, hq, qs, os,
+                                      self._scale if scale is None else scale, scratch.data_ptr(), n, check))
         return out, lse
 
     def _per_key(self, x: torch.Tensor, dtype, what: str):
-        if x.shape != (self.slots, self.heads, self.capacity) or x.dtype is not dtype or x.device != self.device or not x.is_contiguous():
+        if x.shape != (self.slots, self.heads, self.capacity) or x.dtype is not dtype or x.get_device() != self._index or not x.is_contiguous():
             raise ValueError("%s must be a contiguous %s tensor [slots, heads, capacity] of its cache" % (what, dtype))
         return x.data_ptr()
 
@@ -634,43 +634,44 @@ class KvCache4:
                           out: Optional[torch.Tensor] = None, row_start=None, max_rows=None, slots=None, scale: Optional[float] = None):
         """out = weights + what every key receives from these rows, weights [slots, heads, capacity] in fp32 (out None: in place).
         lse is attention()'s.  Returns out; keys at and behind a sequence's length are not written."""
-        if self._elsewhere():
-            with torch.cuda.device(self._index):
+        index = self._index
+        if _device_now() != index:                  # runs again with the cache's device as the current one
+            with torch.cuda.device(index):
                 return self.attention_weights(q, lse, lens, max_len, weights, out, row_start, max_rows, slots, scale)
         hq = q.shape[-2]
-        qs = _rows(q, hq, self.head_dim, "q")
+        qs = _rows(q, hq, self.head_dim, "q", index)
         b, rows, rs = self._batch(q, row_start, max_rows)
         out = weights if out is None else out
-        if lse.shape != q.shape[:-1] or lse.dtype is not torch.float32 or lse.device != self.device or not lse.is_contiguous():
-            raise ValueError("lse must be [.., Hq] in contiguous fp32 on %s" % self.device)
-        _check(lib.l2pd_kv4_weights(self._stream(), self._ref, q.data_ptr(), lse.data_ptr(), self._per_key(weights, torch.float32, "weights"),
-                                    self._per_key(out, torch.float32, "out"), b, rows, rs, _ints(slots, b, "slots", self.device),
-                                    _ints(lens, b, "lens", self.device), max_len, hq, qs,
-                                    1.0 / self.head_dim ** 0.5 if scale is None else scale))
+        if lse.shape != q.shape[:-1] or lse.dtype is not torch.float32 or lse.get_device() != index or not lse.is_contiguous():
+            raise ValueError("lse must be [.., Hq] in contiguous fp32 on cuda:%d" % index)
+        _check(lib.l2pd_kv4_weights(_raw_stream(index), self._ref, q.data_ptr(), lse.data_ptr(), self._per_key(weights, torch.float32, "weights"),
+                                    self._per_key(out, torch.float32, "out"), b, rows, rs, _ints(slots, b, "slots", index),
+                                    _ints(lens, b, "lens", index), max_len, hq, qs, self._scale if scale is None else scale))
         return out
 
     def evict(self, weights: torch.Tensor, lens: torch.Tensor, max_len: int, keep: int, positions=None, first: int = 0, protect_from=None,
               slots=None, into: Optional["KvCache4"] = None, weights_into=None, positions_into=None):
         """Keeps the `keep` heaviest keys of every head (see l2pd_kv4_evict) in `into`, or in place, where weights and positions
         follow in place too unless arrays for them are given.  Returns (kept [sequences, heads, keep], the new lengths)."""
-        if self._elsewhere():
-            with torch.cuda.device(self._index):
+        index = self._index
+        if _device_now() != index:                  # runs again with the cache's device as the current one
+            with torch.cuda.device(index):
                 return self.evict(weights, lens, max_len, keep, positions, first, protect_from, slots, into, weights_into, positions_into)
         dst = self if into is None else into
         if dst is self:
             weights_into = weights if weights_into is None else weights_into
             positions_into = positions if positions_into is None else positions_into
-        elif dst.device != self.device:
+        elif dst._index != index:
             raise ValueError("the destination is not on the cache's device %s" % self.device)
         b = lens.numel()
-        kept = torch.empty((b, self.heads, max(keep, 0)), dtype=torch.int32, device=self.device)
-        lens_out = torch.empty((b,), dtype=torch.int32, device=self.device)
-        _check(lib.l2pd_kv4_evict(self._stream(), self._ref, dst._ref, self._per_key(weights, torch.float32, "weights"),
+        kept = torch.empty(b * self.heads * max(keep, 0), dtype=torch.int32, device=self.device).view(b, self.heads, max(keep, 0))
+        lens_out = torch.empty(b, dtype=torch.int32, device=self.device)
+        _check(lib.l2pd_kv4_evict(_raw_stream(index), self._ref, dst._ref, self._per_key(weights, torch.float32, "weights"),
                                   None if weights_into is None else dst._per_key(weights_into, torch.float32, "weights_into"),
                                   None if positions is None else self._per_key(positions, torch.int32, "positions"),
                                   None if positions_into is None else dst._per_key(positions_into, torch.int32, "positions_into"),
-                                  b, _ints(slots, b, "slots", self.device), _ints(lens, b, "lens", self.device), max_len, keep, first,
-                                  _ints(protect_from, b, "protect_from", self.device), kept.data_ptr(), lens_out.data_ptr()))
+                                  b, _ints(slots, b, "slots", index), _ints(lens, b, "lens", index), max_len, keep, first,
+                                  _ints(protect_from, b, "protect_from", index), kept.data_ptr(), lens_out.data_ptr()))
         return kept, lens_out
 
 
@@ -678,36 +679,41 @@ def qk_norm_rope(q: torch.Tensor, k: torch.Tensor, q_gain=None, k_gain=None, pos
                  q_out=None, k_out=None):
     """Head norms (gains fp32 [dh], None: none) and rotation of q [rows, Hq, dh] and k [rows, Hk, dh] (bf16 or fp32) by their
     positions (int32 [rows], None: the row's number).  Returns (q_out, k_out); the inputs themselves may be given for them."""
-    device, dtype = q.device, q.dtype
-    if device.index is not None and _device_now() != device.index:
-        with torch.cuda.device(device):
+    index, dtype = q.get_device(), q.dtype
+    if index >= 0 and _device_now() != index:
+        with torch.cuda.device(index):
             return qk_norm_rope(q, k, q_gain, k_gain, positions, theta, eps, q_out, k_out)
     qshape, kshape = q.shape, k.shape
-    if len(qshape) != 3 or len(kshape) != 3 or qshape[0] != kshape[0] or qshape[2] != kshape[2] or dtype not in (torch.bfloat16, torch.float32):
-        raise ValueError("q [rows, Hq, dh] and k [rows, Hk, dh], both bf16 or both fp32")
+    if len(qshape) != 3 or len(kshape) != 3 or qshape[0] != kshape[0] or not (dtype is torch.bfloat16 or dtype is torch.float32) or index < 0:
+        raise ValueError("q [rows, Hq, dh] and k [rows, Hk, dh] on a GPU, both bf16 or both fp32")
     t, hq, dh = qshape
     hk = kshape[1]
-    qs, ks = _rows(q, hq, dh, "q", dtype), _rows(k, hk, dh, "k", dtype)
+    qs, ks = _rows(q, hq, dh, "q", index, dtype), _rows(k, hk, dh, "k", index, dtype)
     if q_out is None:
-        q_out, qos = torch.empty(qshape, dtype=dtype, device=device), hq * dh
+        q_out, qos = _fresh(q), hq * dh
     else:
-        qos = _rows(q_out, hq, dh, "q_out", dtype)
+        qos = _rows(q_out, hq, dh, "q_out", index, dtype)
     if k_out is None:
-        k_out, kos = torch.empty(kshape, dtype=dtype, device=device), hk * dh
+        k_out, kos = _fresh(k), hk * dh
     else:
-        kos = _rows(k_out, hk, dh, "k_out", dtype)
-    if q_out.shape != qshape or k_out.shape != kshape or k.device != device or q_out.device != device or k_out.device != device:
-        raise ValueError("k and the outputs must be on q's device, the outputs of their inputs' shapes")
-    gains = [None, None]
-    for i, g in enumerate((q_gain, k_gain)):
-        if g is not None:
-            if g.dtype is not torch.float32 or g.numel() != dh or not g.is_contiguous() or g.device != device:
-                raise ValueError("gains must be contiguous fp32 tensors [dh] on %s" % device)
-            gains[i] = g.data_ptr()
-    _check(lib.l2pd_qk_norm_rope(_raw_stream(device.index), L2PD_BF16 if dtype is torch.bfloat16 else L2PD_F32, q.data_ptr(), k.data_ptr(),
-                                 q_out.data_ptr(), k_out.data_ptr(), gains[0], gains[1], _ints(positions, t, "positions", device), t, hq, hk, dh,
+        kos = _rows(k_out, hk, dh, "k_out", index, dtype)
+    if q_out.shape != qshape or k_out.shape != kshape:
+        raise ValueError("the outputs must have their inputs' shapes")
+    gq = gk = None
+    if q_gain is not None:
+        gq = _gain(q_gain, dh, index)
+    if k_gain is not None:
+        gk = _gain(k_gain, dh, index)
+    _check(lib.l2pd_qk_norm_rope(_raw_stream(index), L2PD_BF16 if dtype is torch.bfloat16 else L2PD_F32, q.data_ptr(), k.data_ptr(),
+                                 q_out.data_ptr(), k_out.data_ptr(), gq, gk, _ints(positions, t, "positions", index), t, hq, hk, dh,
                                  qs, ks, qos, kos, eps, theta))
     return q_out, k_out
+
+
+def _gain(g: torch.Tensor, dh: int, index: int) -> int:
+    if g.dtype is not torch.float32 or g.get_device() != index or g.numel() != dh or not g.is_contiguous():
+        raise ValueError("gains must be contiguous fp32 tensors [%d] on cuda:%d" % (dh, index))
+    return g.data_ptr()
 
 
 def _flat_params(arrays, dev):
