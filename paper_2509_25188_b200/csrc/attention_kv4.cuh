@@ -97,7 +97,7 @@ __host__ __device__ constexpr int part_floats(int chunk, int dh) { return chunk 
 
 __device__ __forceinline__ void fail(int32_t *status, int code) { if (status) atomicCAS(status, 0, code); }
 
-// attention_kv4_tc.cu: chunks of 32, 64 or 128 columns on tcgen05 (chunk: line.chunk; ctas: at most an SM each)
+// attention_kv4_tc.cu: chunks of 64 or 128 columns on tcgen05 (chunk: line.chunk; ctas: at most an SM each)
 cudaError_t launch_attention_kv4_tc(cudaStream_t st, const AttnParams &p, int dh, int ctas);
 constexpr int TC_TILE = 128;         // its key tiles
 

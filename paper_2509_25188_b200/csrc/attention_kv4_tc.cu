@@ -3,27 +3,34 @@
 //
 // S = Q K^T and O += P V, the columns on the M side (128 lanes of tensor memory), tiles of 128 keys.  Eight warps turn codes into
 // fp16 operands in shared memory, in the 128-byte swizzle:
-//     K: (c - 8) s 2^-E    exact: c - 8 has three significant bits (or is 8), s has eight.  The rest of the value, a = m + 8 s, reaches the scores
-//        through sixteen further products of depth: (a_hi, a_hi, a_lo) against (sum q_hi, sum q_lo, sum q_hi): no number of a key's
-//        own is left for the softmax
+//     K: (c - 8) s 2^-E    exact: c - 8 has three significant bits (or is 8), s has eight.  The rest of the value, a = m + 8 s,
+//        reaches the scores through sixteen further products of depth, (a_hi, a_hi, a_lo) against (sum q_hi, sum q_lo, sum q_hi):
+//        no number of a key's own is left for the softmax
 //     V: c s 2^-E + m 2^-E in one fused operation, rounded once (2^-11 relative)
 // E belongs to 32 keys (a warp).  A code reaches fp16 as it lies, as the subnormal c 2^-24 (or 16 c 2^-24 from bits 4..7), and the
-// multiplication by s 2^24 (2^20) lifts it.  Eight codes of a word come out in the order 0 4 1 5 2 6 3 7: queries are written in that order, and
-// outputs read in it.
-// Two groups of four softmax warps take the tiles alternately, a thread a lane: t = cf 2^E acc + (E_V - E0) - M, P = 2^t as fp16 over the
-// second half of the scores, as the A operand of the second product.  M is a reference that follows the running maximum lazily, E0 the
-// largest E_V so far; O is rescaled when one moves.  The thread that has fixed them for a tile hands them to the other group's thread
-// of its lane before its exponentials.  128 keys of a lane are worked on in two halves, the second first: its probabilities go
-// over its own scores while the first half still stands.
+// multiplication by s 2^24 (2^20) lifts it.  Eight codes of a word come out in the order 0 4 1 5 2 6 3 7: queries are written in
+// that order, and outputs read in it.
+// Two groups of four softmax warps take the tiles alternately, a thread a lane: t = cf 2^E acc + (E_V - E0) - M, P = 2^t as fp16,
+// the A operand of the second product.  M is a reference that follows the running maximum lazily, E0 the largest E_V so far; O is
+// rescaled when one moves.  The thread that has fixed them for a tile hands them to the other group's thread of its lane before its
+// exponentials.  128 keys of a lane are read twice, 64 at a time (registers): the maximum first, then the second half, at hand
+// still, then the first.  From that last read on S belongs to the tile after next, whose product runs under the exponentials (P
+// over S instead: 64 numbers a head 14 % slower, 128 numbers 1 % faster).
 //
-// Fewer columns than lanes: chunks of 64 columns stand twice in the lanes, and each copy takes its half of a tile's keys, its probabilities of the others being 0.  The tensor pipe and shared memory do the same work as for 128 columns, but the
-// exponentials are spread over all warps; the copies are added at the end.
+// 33 to 64 columns stand twice in the lanes, and each copy takes its half of a tile's keys, its probabilities of the others being
+// 0: the products are those of 128 columns, but the exponentials are spread over all warps; the copies are added at the end.
 //
-// What bounds it: shared memory.  128 keys of 128: 17 KB of codes in and out, 64 KB of operands out and in: 1300 cycles at 128 bytes; the
-// products 1090, the exponentials (128 columns) 1024.
+// What bounds it.  A tile of 128 keys of 128 numbers needs, in cycles: shared memory 1300 (17 KB of codes in and out, 64 KB of
+// operands out and in, at 128 bytes), products 1090, exponentials of 128 columns 1024, issue slots 1400 of each scheduler.  It
+// takes 2270 with 64 columns and 2850 with 128, no unit more than half busy: with five warps a scheduler, dependent instructions,
+// instruction fetches and waits on barriers (100 each, ready or not) add up.  With exponentials, operand stores and products all
+// left out the rest alone took 70 % of the time.  8 x 64 rows of 32/32 heads of 128 on 8192 keys: 148 us; 4 x 32 rows of 32/8 heads
+// on 65000 keys: 174 us of 128 numbers a head, 143 of 64.  No gain: a second issuing warp, P V in two halves, rolled loops,
+// waits that read no clock, packed f32x2 arithmetic, other register splits.
 //
-// Warp roles (640 threads): 0-3 and 4-7 softmax and output, 4-7 the next piece's queries before that, 8-11 K, 12-15 V, 16 copies of codes,
-// 17 MMA issuer (owns tensor memory), 18 and 19 bring the next piece's queries near.  Tensor memory: S at 0 and 128, O at 256, Q at 384.
+// Warp roles (640 threads): 0-3 and 4-7 softmax and output, 4-7 the next piece's queries before that, 8-11 K, 12-15 V, 16 copies of
+// codes, 17 MMA issuer (owns tensor memory), 18 and 19 bring the next piece's queries near.  Tensor memory: S at 0 and 128, O at
+// 256, Q at 384, P at 448.
 #include <cuda_fp16.h>
 #include <math.h>
 
@@ -43,12 +50,13 @@ constexpr int REGS_SOFTMAX = 120, REGS_CODES = 88, REGS_LEAN = 56;   // 256 x 12
 
 template <int DH> struct Tc {
   static constexpr int ATOMS = DH / 64, TILE32 = KV4_TILE * (DH + 8), STAGE = 4 * TILE32;
+  // AUG: in one atom the further depth of both K buffers (32 bytes of a row each) and, at byte 64, that of the queries
   static constexpr uint32_t K = 0, AUG = NB * ATOMS * ATOM, V = AUG + ATOM, CODES = V + NB * ATOMS * ATOM,
                             STAGING = CODES + RING * STAGE, BYTES = STAGING + 2 * 128 * LDS_O * 4;
 };
 
 enum { B_FULL = 0, B_EMPTY = B_FULL + RING, B_KRDY = B_EMPTY + RING, B_KFREE = B_KRDY + NB, B_VRDY = B_KFREE + NB, B_VFREE = B_VRDY + NB,
-       B_SFULL = B_VFREE + NB, B_PRDY = B_SFULL + 2, B_QRDY = B_PRDY + 2, B_OFREE = B_QRDY + 1, B_HAND = B_OFREE + 1, B_EXPO = B_HAND + 8, B_COUNT = B_EXPO + 4 };
+       B_SFULL = B_VFREE + NB, B_PRDY = B_SFULL + 2, B_QRDY = B_PRDY + 2, B_OFREE = B_QRDY + 1, B_HAND = B_OFREE + 1, B_EXPO = B_HAND + 8, B_SREAD = B_EXPO + 4, B_COUNT = B_SREAD + 2 };
 
 __device__ __forceinline__ float pow2(int n) { return __uint_as_float((uint32_t)(127 + n) << 23); }   // -126 <= n <= 127
 // x 2^n for n beyond one exponent's range
@@ -111,7 +119,7 @@ __global__ void __launch_bounds__(THREADS, 1) attention_kv4_tc_kernel(const Attn
       ptx::mbar_init(bar(B_KRDY + i), 4); ptx::mbar_init(bar(B_KFREE + i), 1);
       ptx::mbar_init(bar(B_VRDY + i), 4); ptx::mbar_init(bar(B_VFREE + i), 1);
     }
-    for (int i = 0; i < 2; ++i) { ptx::mbar_init(bar(B_SFULL + i), 2); ptx::mbar_init(bar(B_PRDY + i), 4); }
+    for (int i = 0; i < 2; ++i) { ptx::mbar_init(bar(B_SFULL + i), 2); ptx::mbar_init(bar(B_SREAD + i), 4); ptx::mbar_init(bar(B_PRDY + i), 4); }
     ptx::mbar_init(bar(B_QRDY), 4); ptx::mbar_init(bar(B_OFREE), 8);
     for (int i = 0; i < 8; ++i) ptx::mbar_init(bar(B_HAND + i), 1);
     for (int i = 0; i < 4; ++i) ptx::mbar_init(bar(B_EXPO + i), 4);
@@ -123,7 +131,7 @@ __global__ void __launch_bounds__(THREADS, 1) attention_kv4_tc_kernel(const Attn
   ptx::tc_fence_before_sync();
   __syncthreads();
   ptx::tc_fence_after_sync();
-  const uint32_t tS = tmem_slot, tO = tS + 256, tQ = tS + 384;
+  const uint32_t tS = tmem_slot, tO = tS + 256, tQ = tS + 384, tP = tS + 448;
   int32_t *const status = p.status;
   grid_dep_launch();
   grid_dep_wait();
@@ -167,20 +175,21 @@ __global__ void __launch_bounds__(THREADS, 1) attention_kv4_tc_kernel(const Attn
       pos += w.t1 - w.t0;
     }
   } else if (warp == 17) {
-    // ------------------------------------------------------------------ MMA issuer: S(0) S(1) PV(0) S(2) PV(1) ...
+    // ------------------------------------------------------------------ MMA issuer: S(0) S(1) S(2) PV(0) S(3) PV(1) ...
     constexpr uint32_t F32 = 1u << 4, M128 = (128u >> 4) << 24;
     const uint32_t idesc_s = F32 | M128 | ((TC_TILE >> 3) << 17), idesc_o = F32 | M128 | ((DH >> 3) << 17) | (1u << 16);
     uint32_t ts = 0, tp = 0, qpar = 0, opar = 1;     // tiles whose S, whose PV was issued
     auto scores = [&]() {
       const uint32_t b = ts & 1u;
-      const bool ok = ptx::mbar_wait_or_abort(bar(B_KRDY + b), (ts >> 1) & 1u, &abort_flag, status, DEV_TIMEOUT_MMA);
+      bool ok = ptx::mbar_wait_or_abort(bar(B_KRDY + b), (ts >> 1) & 1u, &abort_flag, status, DEV_TIMEOUT_MMA);
+      ok = ptx::mbar_wait_or_abort(bar(B_SREAD + b), ((ts >> 1) & 1u) ^ 1u, &abort_flag, status, DEV_TIMEOUT_MMA) && ok;
       ptx::tc_fence_after_sync();
-      const uint64_t kd = ptx::smem_desc_sw128(base + T::K + b * T::ATOMS * ATOM), ad = ptx::smem_desc_sw128(base + T::AUG) + 2u * b;
+      const uint64_t kd = ptx::smem_desc_sw128(base + T::K + b * T::ATOMS * ATOM), ad = ptx::smem_desc_sw128(base + T::AUG);
       if (ptx::elect_one() && ok) {
 #pragma unroll
         for (int k = 0; k < DH / 16; ++k)
           ptx::mma_bf16_ts(tS + b * TC_TILE, tQ + 8 * k, kd + (k >> 2) * (ATOM >> 4) + 2u * (k & 3), idesc_s, k ? 1u : 0u);
-        ptx::mma_bf16_ts(tS + b * TC_TILE, tQ + DH / 2, ad, idesc_s, 1u);
+        ptx::mma_bf16_ss(tS + b * TC_TILE, ad + 4u, ad + 2u * b, idesc_s, 1u);
         ptx::mma_commit(bar(B_KFREE + b));
         ptx::mma_commit(bar(B_SFULL + b));
         ptx::mbar_arrive(bar(B_SFULL + b));          // passes on what the K and the query warps wrote besides
@@ -200,7 +209,7 @@ __global__ void __launch_bounds__(THREADS, 1) attention_kv4_tc_kernel(const Attn
       if (ptx::elect_one() && ok) {
 #pragma unroll
         for (int k = 0; k < TC_TILE / 16; ++k)
-          ptx::mma_bf16_ts(tO, tS + b * TC_TILE + 64 + 8 * k, vd + k * (2048u >> 4), idesc_o, k ? 1u : first ? 0u : 1u);
+          ptx::mma_bf16_ts(tO, tP + 8 * k, vd + k * (2048u >> 4), idesc_o, k ? 1u : first ? 0u : 1u);
         ptx::mma_commit(bar(B_VFREE + b));
       }
       ++tp;
@@ -211,8 +220,9 @@ __global__ void __launch_bounds__(THREADS, 1) attention_kv4_tc_kernel(const Attn
       ptx::mbar_wait_or_abort(bar(B_QRDY), qpar, &abort_flag, status, DEV_TIMEOUT_MMA);
       qpar ^= 1u;
       scores();
+      if (n > 1) scores();
       for (int i = 0; i < n; ++i) {
-        if (i + 1 < n) scores();
+        if (i + 2 < n) scores();
         output(i == 0);
       }
       pos += n;
@@ -293,12 +303,19 @@ __global__ void __launch_bounds__(THREADS, 1) attention_kv4_tc_kernel(const Attn
     const int g = warp >> 2, q = warp & 3, row = 32 * q + lane;
     const int col = row & (CHUNK - 1);               // this lane's column of the chunk
     const int copy = q / (4 / COPIES);               // its first key of a tile: copy * KEYS
-    constexpr int NG = KEYS / 32, HALF = KEYS < 64 ? KEYS : 64, HG = HALF / 32;   // exponents of a copy's keys; keys taken at once
+    constexpr int NG = KEYS / 32, HALF = 64, HG = HALF / 32;      // exponents of a copy's keys; keys taken at once
     const uint32_t mine = bar(B_HAND + 4 * g + q), theirs = bar(B_HAND + 4 * (g ^ 1) + q);
-    const uint32_t lane_base = (uint32_t)(32 * q) << 16, tOr = tO + lane_base;
+    const uint32_t lane_base = (uint32_t)(32 * q) << 16, tOr = tO + lane_base, tPr = tP + lane_base;
+    if (COPIES > 1 && g == 0) {                      // zeros where the other copy's keys are
+      uint32_t z[32];
+#pragma unroll
+      for (int j = 0; j < 32; ++j) z[j] = 0u;
+      ptx::tmem_st_x32(tPr + 32 * (copy ^ 1), z);
+      ptx::tmem_st_wait();
+    }
     uint32_t tile = 0, piece = 0;
     bool ok = true;
-    // Queries of a piece to tensor memory (group 1): the largest of a row becomes 2^7 .. 2^8
+    // Queries of a piece to tensor memory and AUG (group 1): the largest of a row becomes 2^7 .. 2^8
     auto queries = [&](const Piece &w, uint32_t parity) {
       const int c = w.c0 + col, rr = c / ln.group;
       const bool there = col < w.cols;
@@ -332,11 +349,11 @@ __global__ void __launch_bounds__(THREADS, 1) attention_kv4_tc_kernel(const Attn
 #pragma unroll
       for (int j = 0; j < DH / 2; j += 32) ptx::tmem_st_x32(tQ + lane_base + j, raw + j);
       const float hi = __half2float(__float2half_rn(sum));
-      raw[0] = finite ? pair(hi, sum - hi) : 0x7fff7fffu;            // a NaN here makes every score of the row NaN
-      raw[1] = pair(hi * (1.f / 2048.f), 0.f);
-#pragma unroll
-      for (int i = 2; i < 16; ++i) raw[i] = 0u;
-      ptx::tmem_st_x16(tQ + lane_base + DH / 2, raw);
+      const uint32_t at = base + T::AUG + row * 128 + ((4 ^ (row & 7)) << 4);
+      // a NaN here makes every score of the row NaN
+      ptx::st_shared_v4(at, make_uint4(finite ? pair(hi, sum - hi) : 0x7fff7fffu, pair(hi * (1.f / 2048.f), 0.f), 0u, 0u));
+      ptx::st_shared_v4(at ^ 16u, make_uint4(0u, 0u, 0u, 0u));
+      ptx::fence_proxy_async();
       ptx::tmem_st_wait();
       ptx::tc_fence_before_sync();
       __syncwarp();
@@ -452,10 +469,16 @@ __global__ void __launch_bounds__(THREADS, 1) attention_kv4_tc_kernel(const Attn
             for (int j = 0; j < HALF; ++j) if (j >= left - from) s[j] = 0xff800000u;
           }
         };
+        auto release = [&]() {                       // these scores were read for the last time
+          ptx::tc_fence_before_sync();
+          __syncwarp();
+          if (lane == 0) ptx::mbar_arrive(bar(B_SREAD + b));
+        };
         float top[NG];                               // largest scores of the groups
 #pragma unroll
         for (int from = 0; from < KEYS; from += HALF) {
           load(from);
+          if (KEYS == HALF) release();
 #pragma unroll
           for (int i = 0; i < HG; ++i) {
             float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
@@ -492,7 +515,10 @@ __global__ void __launch_bounds__(THREADS, 1) attention_kv4_tc_kernel(const Attn
         // probabilities, the second half first
 #pragma unroll
         for (int from = KEYS - HALF; from >= 0; from -= HALF) {
-          if (from != KEYS - HALF) load(from);
+          if (from != KEYS - HALF) {
+            load(from);
+            release();
+          }
 #pragma unroll
           for (int i = 0; i < HG; ++i) {
             const float kk = k[from / 32 + i], oo = o[from / 32 + i] - m_use;
@@ -505,21 +531,15 @@ __global__ void __launch_bounds__(THREADS, 1) attention_kv4_tc_kernel(const Attn
             }
             l = fmaf(sum[0] + sum[1], ptx::ex2(-o[from / 32 + i]), l);
           }
-          const uint32_t at = tSr + 64 + (copy * KEYS + from) / 2;
-          if (HALF == 64) ptx::tmem_st_x32(at, s); else ptx::tmem_st_x16(at, s);
+          if (from == KEYS - HALF && t > w.t0) {     // once the product of the tile before is complete
+            ok = ptx::mbar_wait_warp(bar(B_VFREE + (b ^ 1u)), ((tile - 1) >> 1) & 1u);
+            ptx::tc_fence_after_sync();
+          }
+          ptx::tmem_st_x32(tPr + (copy * KEYS + from) / 2, s);
         }
-        if (COPIES > 1) {                            // zeros where the other copies' keys are
-          uint32_t z[16];
-#pragma unroll
-          for (int j = 0; j < 16; ++j) z[j] = 0u;
-#pragma unroll
-          for (int c = 0; c < 64; c += 16) if (c / (KEYS / 2) != copy) ptx::tmem_st_x16(tSr + 64 + c, z);
-        }
+        if (!ok) break;
         if (__any_sync(0xffffffffu, moved)) {
           const float fac = open ? 0.f : ptx::ex2(m_was - m_ref + fmaxf(e_was - e0, -126.f));
-          // once the product of the tile before is complete
-          ok = ptx::mbar_wait_warp(bar(B_VFREE + (b ^ 1u)), ((tile - 1) >> 1) & 1u);
-          ptx::tc_fence_after_sync();
 #pragma unroll
           for (int i = 0; i < DH; i += 32) {
             uint32_t v[32];

@@ -90,7 +90,7 @@ struct Kv4AttnArgs {
   const bf16 *q; bf16 *out; float *lse;
   int64_t q_stride, out_stride;
   float scale;
-  float *scratch; int64_t scratch_floats;
+  float *scratch;
   int32_t *status;
 };
 bool attention_kv4_fits(const Kv4View &c, int B, int rows, int Hq, int max_len);   // fewer than 2^31 tiles of work
