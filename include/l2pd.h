@@ -423,8 +423,10 @@ l2pd_status l2pd_attention_bf16(void *stream, const void *q, const void *k, cons
  * [B], the slot of each sequence (NULL: i).  Rows that belong to no sequence are neither read nor written.  A slot outside the
  * cache holds nothing: it is not written and reads as a sequence without keys.  Row strides are in elements; [row][head][head_dim]
  * within a row is contiguous; rows start on 16 bytes (strides multiples of 8), else L2PD_ERR_SHAPE.  Every call follows stream order,
- * allocates nothing, runs on the current device and may be captured into a graph (attention: after one call outside a capture).
- * B = 0 or rows = 0 is L2PD_OK and does nothing.  All arithmetic is fp32 or wider and the order of every sum is fixed: a call
+ * allocates nothing, runs on the current device and may be captured into a graph (attention and weights: after a call of
+ * either outside a capture on that device).
+ * B = 0 or rows = 0 is L2PD_OK and does nothing.  2^31 tiles (of 32 keys, for each head and 8 of its query rows) in a call, or 2^37
+ * rows times heads, are L2PD_ERR_SHAPE.  All arithmetic is fp32 or wider and the order of every sum is fixed: a call
  * repeated on the same device gives the same bits.
  */
 typedef struct {

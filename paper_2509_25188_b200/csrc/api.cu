@@ -1534,6 +1534,11 @@ static l2pd_status kv4_batch(const char *call, int32_t B, int32_t rows, const in
   return L2PD_OK;
 }
 
+// Rows in pieces of 64 for each head: the launch grid counts in 32 bits, whatever `rows` promises.
+static l2pd_status kv4_rows_fit(const char *call, const Kv4View &c, int32_t rows) {
+  return ceil_div64(rows, 64) * c.heads <= 0x7fffffff ? L2PD_OK : refuse(L2PD_ERR_SHAPE, call, "2^37 rows times heads or more");
+}
+
 static l2pd_status kv4_launched(const char *call, cudaError_t e) {
   return e == cudaSuccess ? L2PD_OK : standalone_cuda_error(call, e);
 }
@@ -1550,6 +1555,7 @@ l2pd_status l2pd_kv4_store(void *stream, const l2pd_kv4 *cache, const void *k, c
   const int64_t w = (int64_t)c.heads * c.dh;
   if (k_stride < w || v_stride < w || k_stride % 8 || v_stride % 8 || !aligned16(k) || !aligned16(v))
     return refuse(L2PD_ERR_SHAPE, call, "row strides of at least heads * head_dim, rows on 16 bytes");
+  if ((r = kv4_rows_fit(call, c, rows)) != L2PD_OK) return r;
   return kv4_launched(call, launch_kv4_store((cudaStream_t)stream, c, (const bf16 *)k, (const bf16 *)v, b, k_stride, v_stride));
 }
 
@@ -1566,6 +1572,7 @@ l2pd_status l2pd_kv4_load(void *stream, const l2pd_kv4 *cache, int32_t dtype, vo
   const int64_t w = (int64_t)c.heads * c.dh;
   if (k_stride < w || v_stride < w || k_stride % 8 || v_stride % 8 || !aligned16(k) || !aligned16(v))
     return refuse(L2PD_ERR_SHAPE, call, "row strides of at least heads * head_dim, rows on 16 bytes");
+  if ((r = kv4_rows_fit(call, c, rows)) != L2PD_OK) return r;
   return kv4_launched(call, launch_kv4_load((cudaStream_t)stream, c, dtype, k, v, b, k_stride, v_stride));
 }
 
@@ -1627,6 +1634,8 @@ l2pd_status l2pd_kv4_weights(void *stream, const l2pd_kv4 *cache, const void *q,
   r = kv4_query_checks(call, a.c, q, d_lens, rows, max_len, Hq, q_stride);
   if (r != L2PD_OK) return r;
   if ((rows && !d_lse) || !d_in || !d_out) return refuse(L2PD_ERR_ARG, call, "null pointer");
+  const int64_t n = (int64_t)a.c.slots * a.c.heads * a.c.cap;
+  if (d_in != d_out && d_in < d_out + n && d_out < d_in + n) return refuse(L2PD_ERR_ARG, call, "the sums before and after are one array or two apart");
   a.max_len = max_len; a.Hq = Hq; a.q = (const bf16 *)q; a.lse = d_lse; a.q_stride = q_stride; a.scale = scale; a.w_in = d_in; a.w_out = d_out;
   if (!attention_kv4_fits(a.c, B, 1, a.c.heads, max_len)) return refuse(L2PD_ERR_SHAPE, call, "2^31 tiles of work or more");
   a.status = standalone_status();

@@ -13,8 +13,13 @@
 //
 // Work: the key tiles of all (sequence, head, chunk of columns) stand in one line and every CTA takes an equal run of it; a run
 // that starts or ends inside an item leaves a partial result, joined in the order of the tiles by a second kernel.  A warp takes
-// every fourth tile of its CTA's run, through a ring of its own; the CTA's second half of an SM computes while the first one
-// fetches queries or brings its warps' sums together.
+// every fourth tile of its CTA's run, through a ring of its own.  Two to four CTAs an SM: one computes while another fetches
+// queries or brings its warps' sums together.
+//
+// What bounds it.  One row of 32/8 heads on 4000 keys: the latency of a few dependent steps and of two launches, 11 us.  Up to 8
+// columns on many keys: memory (64 rows of 32/8 heads on 8192 keys each: 116 us, 4.9 TB/s).  32 columns (8 x 32 rows of 32 heads of
+// 128 on 2048 keys, 44 us): products 512 cycles of a scheduler and 453 instructions for 16 keys, which take 1250; registers leave two
+// warps a scheduler, and each goes through products, exponentials and products in turn.
 #include <cuda_fp16.h>
 #include <math.h>
 
@@ -122,8 +127,8 @@ __global__ void __launch_bounds__(WARPS * 32, AttnShape<DH, NT>::CTAS) attention
   }
   if (threadIdx.x == 0) abort_flag = 0;
   __syncthreads();
-  grid_dep_launch();
   grid_dep_wait();
+  grid_dep_launch();                               // behind the wait: see the joining kernel
 
   const Line &ln = p.line;
   const Seq own = ln.seq(lane);
@@ -417,6 +422,8 @@ __global__ void __launch_bounds__(WARPS * 32, AttnShape<DH, NT>::CTAS) attention
 
 // Joins the partial results of an item, in the order of its tiles.  WPC warps have a column (4: few columns of many pieces);
 // a block of four warps, 4 / WPC columns.  Sequences without keys: output 0, log-sum -inf.
+// The attention kernel lets it start only behind its own wait for what came before: the batch's arrays are then final, and the
+// survey runs beside the attention's end (one row on 4000 keys 13.3 -> 11.1 us, 3 x 27 rows 18.3 -> 15.2).
 template <int DH, int WPC>
 __global__ void __launch_bounds__(128) kv4_join_kernel(const AttnParams p, int n_ctas) {
   constexpr int LDO = DH + 4;
@@ -424,9 +431,11 @@ __global__ void __launch_bounds__(128) kv4_join_kernel(const AttnParams p, int n
   __shared__ float4 sm_o[4][32];
   const Line &ln = p.line;
   const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, b = blockIdx.y, h = blockIdx.z, col = blockIdx.x * (4 / WPC) + w / WPC;
+  const Seq own = ln.seq(lane), sq = ln.seq(b);
+  uint32_t share = 1, before = 0;
+  if (sq.tiles) ln.survey(own, n_ctas, b, &share, &before);
   grid_dep_launch();
   grid_dep_wait();
-  const Seq own = ln.seq(lane), sq = ln.seq(b);
   if (col >= sq.rows * ln.group) return;           // WPC 4: the whole block
   const int nt = sq.tiles, r = col / ln.group, hq = h * ln.group + col - r * ln.group;
   const int64_t row = (int64_t)sq.row0 + r;
@@ -438,8 +447,6 @@ __global__ void __launch_bounds__(128) kv4_join_kernel(const AttnParams p, int n
     if (lead && lane == 0 && lse) *lse = -INFINITY;
     return;
   }
-  uint32_t share, before;
-  ln.survey(own, n_ctas, b, &share, &before);
   const uint32_t start = before + ((uint32_t)h * sq.chunks + col / ln.chunk) * nt;
   const int i0 = (int)(start / share), i1 = (int)((start + nt - 1) / share);
   if (i0 == i1) return;                            // stored by its CTA
@@ -479,9 +486,9 @@ __global__ void __launch_bounds__(128) kv4_join_kernel(const AttnParams p, int n
   if (lane == 0 && lse) *lse = (m + log2f(l)) * 0.6931471805599453f;
 }
 
-// Up to 32 columns: the warp-level kernel, whose operands never leave registers.  More: tcgen05 with 64 or 128 lanes.  (8 sequences of
-// 32 heads, us at 128 / 2048 / 8192 keys: 16 columns 13 / 42 / 83 against 20 / 45 / 124 on tcgen05, 32 columns 16 / 44 / 130 against 21 / 47 / 128;
-// heads of 64: 10 / 31 / 56 against 15 / 36 / 103, 12 / 29 / 83 against 17 / 37 / 103.)
+// Up to 32 columns: the warp-level kernel, whose operands never leave registers.  More: tcgen05 with 64 or 128 lanes.  (8 sequences
+// of 32 heads, us at 128 / 2048 / 8192 keys: 16 columns 13 / 42 / 83 against 20 / 45 / 124 on tcgen05, 32 columns 16 / 44 / 130
+// against 21 / 47 / 128; heads of 64: 10 / 31 / 56 against 15 / 36 / 103, 12 / 29 / 83 against 17 / 37 / 103.)
 struct AttnPlan { int chunk, ctas, tc; };
 
 AttnPlan plan_attention(int heads, int B, int rows, int Hq, int max_len, int sms) {
@@ -548,7 +555,9 @@ cudaError_t launch_attention_kv4(cudaStream_t st, const Kv4AttnArgs &a, int sms)
 // of a cache tile, codes and (s, m) of K.  A warp keeps 32 keys as A fragments in registers and passes the columns by them, whose B
 // fragments lie in shared memory for all warps of the CTA; more than 64 columns in several passes over the CTA's run.
 //
-// Few columns: bound by memory.  Many: by the products, 16 MMAs of 8 cycles for 32 keys and 8 columns.
+// Few columns: bound by memory (16 x 1 token of 32/8 heads on 30000 keys: 50 us, 4.6 TB/s with the sums).  Many: by the products, 16
+// MMAs of 8 cycles for 32 keys and 8 columns (8 x 32 rows of 32 heads on 2048 keys: 23 us, the products alone 7.8), and by the
+// launch, the queries' conversion in every CTA and the exponentials beside them.
 namespace {
 
 struct WeighParams {

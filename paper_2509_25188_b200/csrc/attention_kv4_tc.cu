@@ -25,7 +25,7 @@
 // takes 2270 with 64 columns and 2850 with 128, no unit more than half busy: with five warps a scheduler, dependent instructions,
 // instruction fetches and waits on barriers (100 each, ready or not) add up.  With exponentials, operand stores and products all
 // left out the rest alone took 70 % of the time.  8 x 64 rows of 32/32 heads of 128 on 8192 keys: 148 us; 4 x 32 rows of 32/8 heads
-// on 65000 keys: 174 us of 128 numbers a head, 143 of 64.  No gain: a second issuing warp, P V in two halves, rolled loops,
+// on 65000 keys: 171 us of 128 numbers a head, 139 of 64.  No gain: a second issuing warp, P V in two halves, rolled loops,
 // waits that read no clock, packed f32x2 arithmetic, other register splits.
 //
 // Warp roles (640 threads): 0-3 and 4-7 softmax and output, 4-7 the next piece's queries before that, 8-11 K, 12-15 V, 16 copies of
@@ -133,8 +133,8 @@ __global__ void __launch_bounds__(THREADS, 1) attention_kv4_tc_kernel(const Attn
   ptx::tc_fence_after_sync();
   const uint32_t tS = tmem_slot, tO = tS + 256, tQ = tS + 384, tP = tS + 448;
   int32_t *const status = p.status;
-  grid_dep_launch();
   grid_dep_wait();
+  grid_dep_launch();                               // behind the wait: see the joining kernel
 
   // the run of tiles, the same in every warp
   const Line &ln = p.line;

@@ -137,3 +137,18 @@ def test_norm_rope_refusals(kw, status):
     a.update(kw)
     assert b.lib.l2pd_qk_norm_rope(None, a["dtype"], a["q"], a["k"], a["qo"], a["ko"], None, None, None, a["rows"], a["hq"], a["hk"], a["dh"], a["qs"],
                                    a["ks"], a["qos"], a["kos"], a["eps"], a["theta"]) == status
+
+
+def test_rows_that_a_launch_cannot_count_are_refused():
+    # `rows` is a promise, not an array: 2^31 - 1 of them for 65 heads pass the grid's 32 bits
+    b, c = _cache(heads=65)
+    w = 65 * 128
+    assert b.lib.l2pd_kv4_store(None, C.byref(c), P, P, 1, 2 ** 31 - 1, P, None, None, w, w) == SHAPE
+    assert b.lib.l2pd_kv4_load(None, C.byref(c), 1, P, P, 1, 2 ** 31 - 1, P, None, None, w, w) == SHAPE
+
+
+@pytest.mark.parametrize("off", [4, 4 * (2 * 4 * 100 - 1)])
+def test_weights_refuse_arrays_that_overlap(off):
+    b, c = _cache()
+    for i, o in ((P, P + off), (P + off, P)):
+        assert b.lib.l2pd_kv4_weights(None, C.byref(c), P, P, i, o, 1, 1, None, None, P, 100, 4, 512, 0.1) == ARG
