@@ -751,11 +751,13 @@ void set_standalone_error(const char *fmt, ...) {
   vsnprintf(g_standalone_err, sizeof(g_standalone_err), fmt, ap);
   va_end(ap);
 }
+void begin_standalone() { g_standalone_err[0] = 0; }
 }  // namespace l2pd
 
 extern "C" {
 
 l2pd_status l2pd_init(const l2pd_config *cfg, const l2pd_weights *w, int device, l2pd_ctx **out) {
+  begin_standalone();
   if (out) *out = nullptr;
   if (!cfg || !w || !out) return L2PD_ERR_ARG;
   std::string why;
@@ -1124,6 +1126,7 @@ struct TrainLimits { int64_t chunk; uint64_t wait_ns; int64_t short_launch; };
 static l2pd_status filter_train_impl(void *stream, int32_t s, int32_t L, int64_t N, const float *d_c, const uint8_t *d_y,
                                      float *const *w, float *const *b, const l2pd_train_config *t, float *h_losses,
                                      const TrainLimits &lim = {0, 2000000000ull, -1}) {
+  begin_standalone();
   if (!d_c || !d_y || !w || !b || !t) return L2PD_ERR_ARG;
   if (L < 1 || L > 4) return L2PD_ERR_ARG;
   for (int k = 0; k < L; ++k) if (!w[k] || !b[k]) return L2PD_ERR_ARG;
@@ -1342,6 +1345,7 @@ static l2pd_status gemm_common_wm(void *stream, int epi, const void *A, const vo
 
 static l2pd_status gemm_common(void *stream, int epi, const void *A, const void *W, const void *W2, void *out,
                                int M, int N, int K, int tile_n, int check) {
+  begin_standalone();
   if (!A || !W || !out || (epi == EPI_SWIGLU && !W2)) return L2PD_ERR_ARG;
   if (M < 1 || N < 8 || K < 8 || (N % 8) || (K % 8)) return L2PD_ERR_SHAPE;
   if (tile_n < 0) return L2PD_ERR_SHAPE;
@@ -1437,6 +1441,7 @@ int64_t l2pd_lm_head_scratch_elems(int32_t R, int32_t V) {
 l2pd_status l2pd_lm_head_bf16(void *stream, const void *A, const void *W, const float *bias, int32_t R, int32_t V,
                               int32_t K, float *d_scratch, int32_t *d_pred, float *d_conf, float *d_logits,
                               int32_t check) {
+  begin_standalone();
   if (!A || !W || !d_scratch || !d_pred || !d_conf) return L2PD_ERR_ARG;
   if (R < 1 || V < 2 || K < 8 || (K % 8)) return L2PD_ERR_SHAPE;
   const int sms = device_sms();
@@ -1466,6 +1471,7 @@ l2pd_status l2pd_lm_head_bf16(void *stream, const void *A, const void *W, const 
 l2pd_status l2pd_attention_bf16(void *stream, const void *q, const void *k, const void *v, void *out, int32_t Tq,
                                 int32_t Tk, int32_t H, int32_t dh, int64_t q_stride, int64_t kv_stride,
                                 int64_t out_stride, int32_t impl, int32_t check) {
+  begin_standalone();
   if (!q || !k || !v || !out) return L2PD_ERR_ARG;
   if (Tq < 1 || Tk < 1 || H < 1 || (dh != 64 && dh != 128) || (q_stride % 8) || (kv_stride % 8) || (out_stride % 2))
     return L2PD_ERR_SHAPE;
@@ -1516,6 +1522,7 @@ int64_t l2pd_kv4_bytes(int32_t slots, int32_t heads, int32_t head_dim, int32_t c
 
 // The device's view of a cache, after the checks that every call makes.
 static l2pd_status kv4_view(const char *call, const l2pd_kv4 *c, Kv4View *v) {
+  begin_standalone();
   if (!c || !c->data) return refuse(L2PD_ERR_ARG, call, "null cache");
   if (!l2pd_kv4_bytes(c->slots, c->heads, c->head_dim, c->capacity))
     return refuse(L2PD_ERR_SHAPE, call, "cache of slots >= 1, 1 to 65535 heads of 64 or 128, capacity >= 1");
@@ -1675,6 +1682,7 @@ l2pd_status l2pd_qk_norm_rope(void *stream, int32_t dtype, const void *q, const 
                               const float *k_gain, const int32_t *d_positions, int32_t rows, int32_t Hq, int32_t Hk, int32_t head_dim,
                               int64_t q_stride, int64_t k_stride, int64_t q_out_stride, int64_t k_out_stride, float eps, float theta) {
   const char *call = "l2pd_qk_norm_rope";
+  begin_standalone();
   if (dtype != L2PD_F32 && dtype != L2PD_BF16) return refuse(L2PD_ERR_ARG, call, "dtype is L2PD_F32 or L2PD_BF16");
   if (rows < 0 || Hq < 0 || Hk < 0 || Hq > 65535 || Hk > 65535 || head_dim < 2 || head_dim > 256 || head_dim % 2)
     return refuse(L2PD_ERR_SHAPE, call, "rows >= 0, heads in [0, 65535], an even head_dim of at most 256");

@@ -215,6 +215,7 @@ l2pd_status make_tma_out_tail(TmaDesc *out, void *ptr, bool fp32, int64_t rows, 
 int lm_head_tile_n(int R, int V, int K, int num_sms);   // tile width of the LM-head GEMM (single CTAs)
 // what failed in the calling thread's last context-free call: reported by l2pd_last_error(NULL) (api.cu)
 void set_standalone_error(const char *fmt, ...);
+void begin_standalone();             // nothing so far: every such call starts with it
 // How one GEMM is laid over the SMs: CTAs per tile (1, or 2 = a cta_group::2 pair on a 256-row tile),
 // tile width, K slices (residual epilogue only: slices add into X with vector reductions), and row
 // slabs per unit (2 = a unit covers two 128 * cta_group row slabs against one load of the weight

@@ -44,6 +44,7 @@ using namespace l2pd;
 extern "C" l2pd_status l2pd_lm_head_bf16_static(void *stream, const void *A, const void *W, const float *bias,
                                                 int32_t R, int32_t V, int32_t K, int32_t *d_pred, float *d_conf,
                                                 int32_t check) {
+  begin_standalone();
   auto bad = [](l2pd_status st, const char *what) { set_standalone_error("l2pd_lm_head_bf16_static: %s", what); return st; };
   if (!A || !W || !d_pred || !d_conf) return bad(L2PD_ERR_ARG, "null pointer");
   if (R < 1 || V < 2 || K < 8 || (K % 8)) return bad(L2PD_ERR_SHAPE, "R >= 1, V >= 2, K a positive multiple of 8");

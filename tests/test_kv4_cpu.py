@@ -152,3 +152,20 @@ def test_weights_refuse_arrays_that_overlap(off):
     b, c = _cache()
     for i, o in ((P, P + off), (P + off, P)):
         assert b.lib.l2pd_kv4_weights(None, C.byref(c), P, P, i, o, 1, 1, None, None, P, 100, 4, 512, 0.1) == ARG
+
+
+@pytest.mark.parametrize("then", ["nothing to do", "gemm", "attention", "lm_head", "init"])
+def test_a_refusal_is_reported_for_its_own_call_alone(then):
+    b, c = _cache()
+    assert _store(b, c, k=None) == ARG and b.lib.l2pd_last_error(None) != b""
+    if then == "nothing to do":
+        assert _store(b, c, B=0) == 0
+    elif then == "gemm":
+        assert b.lib.l2pd_gemm_bf16(None, None, None, None, 1, 8, 8, 0, 0) == ARG
+    elif then == "attention":
+        assert b.lib.l2pd_attention_bf16(None, None, None, None, None, 1, 1, 1, 64, 64, 64, 64, 0, 0) == ARG
+    elif then == "lm_head":
+        assert b.lib.l2pd_lm_head_bf16(None, None, None, None, 1, 8, 8, None, None, None, None, 0) == ARG
+    else:
+        assert b.lib.l2pd_init(None, None, 0, None) == ARG
+    assert b.lib.l2pd_last_error(None) == b""
