@@ -219,7 +219,7 @@ __device__ __forceinline__ int block_scan(int x, int *warp_sums, int *total) {
 // histograms of 256, added over the cluster); a bitmap of the kept keys with the running count before each word then answers both "how many
 // free places before j" and "which is the i-th kept key", in the slice of any CTA, so that no list is built.
 // Bound by the latency of its steps.  8 heads x 4 sequences of 65000 keys down to 8000: one CTA each 141 us, eight that deal the
-// places out 34 (the records' move behind it 19).
+// places out 34, all of a slice's weights in flight and four words of the search a step 29 (the records' move behind it 19).
 __device__ __forceinline__ uint32_t ld_cluster(const void *p, uint32_t rank) {
   uint32_t v;
   asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(ptx::mapa(ptx::smem_u32(p), rank)));
@@ -257,14 +257,27 @@ __global__ void __launch_bounds__(SELECT_THREADS) kv4_select_kernel(const Kv4Evi
   for (int i = tid; i < 1024; i += SELECT_THREADS) hist[i >> 8][i & 255] = 0;
   if (tid < 3) counts[tid] = 0;
   if (cached) {
-#pragma unroll 4
-    for (int j = tid; j < count; j += SELECT_THREADS) cache[j] = rank_of(j);
+    // sixteen keys a thread at once: a slice of 8192 is one round of loads
+    for (int j0 = tid; j0 < count; j0 += 16 * SELECT_THREADS) {
+      float w[16];
+      int pos[16];
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const int j = min(j0 + i * SELECT_THREADS, count - 1);
+        w[i] = a.weights[base + j];
+        pos[i] = a.positions ? a.positions[base + j] : lo + j;
+      }
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+        if (j0 + i * SELECT_THREADS < count) cache[j0 + i * SELECT_THREADS] = weight_rank(w[i], pos[i] < a.first || pos[i] >= from);
+    }
   }
   __syncthreads();
   uint32_t prefix = 0, mask = 0;
   int need = m;                                   // of the keys whose leading digits equal the prefix, this many are kept
   for (int pass = 0; pass < 4; ++pass) {
     const int shift = 24 - 8 * pass;
+#pragma unroll 8
     for (int j = tid; j < count; j += SELECT_THREADS) {
       const uint32_t r = rank(j);
       if ((r & mask) == prefix) atomicAdd(&hist[pass][(r >> shift) & 255u], 1);
@@ -364,9 +377,13 @@ __global__ void __launch_bounds__(SELECT_THREADS) kv4_select_kernel(const Kv4Evi
       for (int i = 0; i < 7; ++i)
         if (c == i && i < cluster - 1 && want >= held[i]) { want -= held[i]; ++c; }
       int x = 0, y = (min(slice, n - c * slice) + 31) / 32 - 1;   // its word: the last whose count does not pass `want`
-      while (x < y) {
-        const int mid = (x + y + 1) >> 1;
-        if ((int)peek(&before[mid], c) <= want) x = mid; else y = mid - 1;
+      while (x < y) {                               // a quarter of the words a step
+        const int step = (y - x + 4) >> 2, p1 = min(x + step, y), p2 = min(x + 2 * step, y), p3 = min(x + 3 * step, y);
+        const int b1 = (int)peek(&before[p1], c), b2 = (int)peek(&before[p2], c), b3 = (int)peek(&before[p3], c);
+        if (b3 <= want) x = p3;
+        else if (b2 <= want) { x = p2; y = p3 - 1; }
+        else if (b1 <= want) { x = p1; y = p2 - 1; }
+        else y = p1 - 1;
       }
       uint32_t u = peek(&bits[x], c);
       want -= (int)peek(&before[x], c);             // the bit with `want` set ones below it, halving
@@ -458,7 +475,8 @@ cudaError_t launch_kv4_load(cudaStream_t st, const Kv4View &c, int dtype, void *
 }
 
 cudaError_t launch_kv4_evict(cudaStream_t st, const Kv4EvictArgs &a) {
-  // CTAs of a cluster: a slice of 4096 keys each, eight at most
+  // CTAs of a cluster: a slice of 4096 keys each, eight at most (1 x 8 heads on 4000 keys in four: 14.1 us instead of 15.8, on 1500 in
+  // two: 12.7 instead of 11.7)
   int cluster = 1;
   while (cluster < 8 && a.max_len > 4096 * cluster) cluster *= 2;
   const int slice = ceil_div(ceil_div(a.max_len > 1 ? a.max_len : 1, cluster), 32) * 32;
