@@ -556,7 +556,7 @@ cudaError_t launch_attention_kv4(cudaStream_t st, const Kv4AttnArgs &a, int sms)
 // fragments lie in shared memory for all warps of the CTA; more than 64 columns in several passes over the CTA's run.
 //
 // Few columns: bound by memory (16 x 1 token of 32/8 heads on 30000 keys: 50 us, 4.6 TB/s with the sums).  Many: by the products, 16
-// MMAs of 8 cycles for 32 keys and 8 columns (8 x 32 rows of 32 heads on 2048 keys: 23 us, the products alone 7.8), and by the
+// MMAs of 8 cycles for 32 keys and 8 columns (8 x 32 rows of 32 heads on 2048 keys: 22 us, the products alone 7.8), and by the
 // launch, the queries' conversion in every CTA and the exponentials beside them.
 namespace {
 
@@ -629,18 +629,17 @@ __global__ void __launch_bounds__(WARPS * 32, 4) kv4_weights_kernel(const WeighP
       };
       for (int i = 0; i < STAGES; ++i) request(i);
       // queries: each warp converts every fourth eight of columns.  Two rounds: the largest of all, then the conversion
-      auto column = [&](int n, bool *there) {
+      struct Column { int row, head; bool there; };
+      auto column = [&](int n) {
         const int col = c0 + 8 * n + g, r = col / ln.group;
-        *there = 8 * n + g < here;
-        return (int64_t)(sq.row0 + r) * p.Hq + h * ln.group + col - r * ln.group;   // row and query head
+        return Column{sq.row0 + r, h * ln.group + col - r * ln.group, 8 * n + g < here};
       };
-      auto address = [&](int64_t x) { return p.q + x / p.Hq * p.q_stride + x % p.Hq * DH + t * (DH / 4); };
+      auto address = [&](const Column &x) { return p.q + (int64_t)x.row * p.q_stride + (int64_t)x.head * DH + t * (DH / 4); };
       uint32_t top = 0;
       for (int n = warp; n < nts; n += WARPS) {
-        bool there;
-        const int64_t x = column(n, &there);
+        const Column x = column(n);
         Queries<DH> qn;
-        qn.load(address(x), there);
+        qn.load(address(x), x.there);
         if (qn.finite()) top = max(top, qn.top);
       }
       top = __reduce_max_sync(0xffffffffu, top);
@@ -649,14 +648,13 @@ __global__ void __launch_bounds__(WARPS * 32, 4) kv4_weights_kernel(const WeighP
       const int u = query_exponent(max(max(qtop[0], qtop[1]), max(qtop[2], qtop[3])));
       const float cf = query_factor(p.scale_log2, u);
       for (int n = warp; n < nts; n += WARPS) {
-        bool there;
-        const int64_t x = column(n, &there);
+        const Column x = column(n);
         Queries<DH> qn;
-        qn.load(address(x), there);
+        qn.load(address(x), x.there);
         uint32_t f[DH / 8];
         const float cs = qn.convert(u, f);
         if (t == 0) {
-          float l = there ? p.lse[x] * 1.4426950408889634f : INFINITY;
+          float l = x.there ? p.lse[(int64_t)x.row * p.Hq + x.head] * 1.4426950408889634f : INFINITY;
           if (l == -INFINITY) l = INFINITY;        // a row without keys gives no weight
           of_col[8 * n + g] = make_float2(cs, -l);
         }
@@ -690,7 +688,7 @@ __global__ void __launch_bounds__(WARPS * 32, 4) kv4_weights_kernel(const WeighP
         for (int e = 0; e < 4; ++e)
 #pragma unroll
           for (int j = 0; j < W; ++j) spread(k[e][j], &x[e][4 * j]);
-#pragma unroll 1
+#pragma unroll 2                                     // four sums under way: heads of 64 18.0 -> 15.6 us, of 128 22.7 -> 22.3
         for (int n = 0; n < nts; ++n) {
           float acc[2][4];
 #pragma unroll
