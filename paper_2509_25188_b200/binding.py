@@ -558,6 +558,8 @@ class KvCache4:
         if k.shape != v.shape:
             raise ValueError("k and v differ in shape")
         b, rows, rs = self._batch(k, row_start, max_rows)
+        if not k.shape[0]:                          # no rows, and no address of any
+            rows = 0
         _check(lib.l2pd_kv4_store(_raw_stream(index), self._ref, k.data_ptr(), v.data_ptr(), b, rows, rs, _ints(slots, b, "slots", index),
                                   _ints(key_start, b, "key_start", index), ks, vs))
 
@@ -581,6 +583,8 @@ class KvCache4:
             n, shape = b * rows, (b, rows, heads, dh)
         k = torch.empty(n * heads * dh, dtype=dtype, device=self.device).view(shape)
         v = torch.empty_like(k)
+        if not n:                                   # no rows, and no address of any
+            rows = 0
         _check(lib.l2pd_kv4_load(_raw_stream(index), self._ref, L2PD_BF16 if dtype is torch.bfloat16 else L2PD_F32, k.data_ptr(), v.data_ptr(), b, rows,
                                  _ints(row_start, b + 1, "row_start", index), _ints(slots, b, "slots", index),
                                  _ints(key_start, b, "key_start", index), heads * dh, heads * dh))
@@ -608,6 +612,8 @@ class KvCache4:
         hq = shape[-2]
         qs = _rows(q, hq, dh, "q", index)
         b, rows, rs = self._batch(q, row_start, max_rows)
+        if not shape[0]:                            # no rows, and no address of any
+            rows = 0
         if out is None:
             out, os = _fresh(q), hq * dh
         else:
@@ -641,6 +647,8 @@ class KvCache4:
         hq = q.shape[-2]
         qs = _rows(q, hq, self.head_dim, "q", index)
         b, rows, rs = self._batch(q, row_start, max_rows)
+        if not q.shape[0]:                          # no rows, and no address of any
+            rows = 0
         out = weights if out is None else out
         if lse.shape != q.shape[:-1] or lse.dtype is not torch.float32 or lse.get_device() != index or not lse.is_contiguous():
             raise ValueError("lse must be [.., Hq] in contiguous fp32 on cuda:%d" % index)

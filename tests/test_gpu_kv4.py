@@ -321,6 +321,83 @@ def test_other_streams_captures_and_strides():
     assert torch.allclose(weights, 4 * once, rtol=2.0 ** -21, atol=0)   # four additions, a half-ulp each
 
 
+@pytest.mark.parametrize("rows", [1, 40])
+def test_lengths_written_just_before_the_call(rows):
+    """The lengths of a call are those the stream holds when it runs, for all of its kernels: they change from call to call, behind a
+    store and behind an eviction, with nothing waited for in between."""
+    b = _b()
+    B, heads, cap = 3, 2, 700
+    c, d = b.KvCache4(B, heads, 128, cap), b.KvCache4(B, heads, 128, cap)
+    k, v, q = _rand(61, B, cap, heads, 128), _rand(62, B, cap, heads, 128), _rand(63, B, rows, 2 * heads, 128)
+    c.store(k, v)
+    w = torch.rand(B, heads, cap, generator=torch.Generator().manual_seed(64)).to(DEV)
+    plan = [_i32([(131 * i * (j + 1)) % (cap + 1) for j in range(B)]) for i in range(24)]
+    lens, got = _i32([0] * B), []
+    for i, n in enumerate(plan):
+        lens.copy_(n)
+        c.store(k, v)
+        first = c.attention(q, lens, cap)
+        kept, left = c.evict(w, lens, cap, 200 + i, into=d)
+        got.append(first + d.attention(q, left, cap))
+    torch.cuda.synchronize()
+    for i, (n, have) in enumerate(zip(plan, got)):
+        one = c.attention(q, n, cap)
+        torch.cuda.synchronize()
+        _, left = c.evict(w, n, cap, 200 + i, into=d)
+        torch.cuda.synchronize()
+        want = one + d.attention(q, left, cap)
+        assert left.tolist() == [min(x, 200 + i) for x in n.tolist()]
+        for x, y in zip(have, want):
+            assert torch.equal(x, y), i
+
+
+def test_calls_at_once_on_two_streams():
+    """Attention of both kinds, weights and stores into another cache, on two streams with nothing between them: the bits are those of
+    the calls one after the other."""
+    b = _b()
+    c, other = b.KvCache4(2, 4, 128, 3000), [b.KvCache4(2, 4, 128, 3000) for _ in range(2)]
+    k, v = _rand(71, 2, 3000, 4, 128), _rand(72, 2, 3000, 4, 128)
+    c.store(k, v)
+    lens = _i32([3000, 1234])
+    qs = [_rand(73, 2, 5, 8, 128), _rand(74, 2, 50, 8, 128), _rand(75, 2, 16, 8, 128)]
+    want = [c.attention(q, lens, 3000) for q in qs]
+    sums = [c.attention_weights(q, l, lens, 3000, torch.zeros(2, 4, 3000, device=DEV)) for q, (_, l) in zip(qs, want)]
+    torch.cuda.synchronize()
+    streams, got = [torch.cuda.Stream() for _ in range(2)], [[], []]
+    for turn in range(10):
+        for i, s in enumerate(streams):
+            with torch.cuda.stream(s):
+                q = (turn + i) % 3
+                o, l = c.attention(qs[q], lens, 3000)
+                got[i].append((q, o, l, c.attention_weights(qs[q], l, lens, 3000, torch.zeros(2, 4, 3000, device=DEV))))
+                other[i].store(k, v)
+    for s in streams:
+        s.synchronize()
+    for q, o, l, w in got[0] + got[1]:
+        assert torch.equal(o, want[q][0]) and torch.equal(l, want[q][1]) and torch.equal(w, sums[q])
+    for x in other:
+        assert torch.equal(x.data, c.data)
+
+
+def test_batches_without_rows():
+    b = _b()
+    c = b.KvCache4(2, 2, 64, 50)
+    c.store(_rand(81, 2, 50, 2, 64), _rand(82, 2, 50, 2, 64))
+    before = c.data.clone()
+    none, q, lens, start = _rand(83, 0, 2, 64), _rand(84, 0, 4, 64), _i32([50, 9]), _i32([0, 0, 0])
+    c.store(none, none, row_start=start, max_rows=5)
+    k, v = c.load(5, row_start=start, total_rows=0)
+    out, lse = c.attention(q, lens, 50, row_start=start, max_rows=5)
+    assert k.shape == v.shape == (0, 2, 64) and out.shape == (0, 4, 64) and lse.shape == (0, 4)
+    w = torch.rand(2, 2, 50, device=DEV)
+    new = c.attention_weights(q, lse, lens, 50, w, out=torch.full_like(w, -1.0), row_start=start, max_rows=5)
+    for i, n in enumerate([50, 9]):
+        assert torch.equal(new[i, :, :n], w[i, :, :n]) and (new[i, :, n:] == -1).all()
+    assert c.attention(_rand(85, 0, 3, 4, 64), _i32([]), 50)[0].shape == (0, 3, 4, 64)
+    assert b.qk_norm_rope(_rand(86, 0, 4, 64), none)[0].shape == (0, 4, 64)
+    assert torch.equal(c.data, before)
+
+
 def test_binding_refuses_wrong_tensors():
     b = _b()
     c = b.KvCache4(1, 2, 128, 10)
