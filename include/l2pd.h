@@ -459,8 +459,8 @@ l2pd_status l2pd_attention_kv4(void *stream, const l2pd_kv4 *cache, const void *
 l2pd_status l2pd_kv4_weights(void *stream, const l2pd_kv4 *cache, const void *q, const float *d_lse, const float *d_in, float *d_out, int32_t B,
                              int32_t rows, const int32_t *d_row_start, const int32_t *d_slots, const int32_t *d_lens, int32_t max_len,
                              int32_t Hq, int64_t q_stride, float scale);
-/* Keeps min(d_lens[i], keep) keys of every head: protected keys first, then by weight, largest first (NaN last), equal ones
- * by index.  A key is protected if its position is below `first` or not below d_protect_from[i] (DEVICE int32 [B] or NULL).
+/* Keeps min(d_lens[i], keep) keys of every head: protected keys first, among themselves by index; then by weight, largest first
+ * (NaN last), equal ones by index.  A key is protected if its position is below `first` or not below d_protect_from[i] (DEVICE int32 [B] or NULL).
  * d_positions: DEVICE int32 [slots, heads, capacity], or NULL: a key's position is its index.  Kept keys of index below the new length
  * stay at their place; the others fill the free places, both in ascending order.  d_kept: DEVICE int32 [B, heads, keep], the index
  * that place j was filled from, -1 behind the new length.  d_lens_out: DEVICE int32 [B], not d_lens itself.
