@@ -6,7 +6,8 @@
 // Bound by memory: every value is read and written once.  A block takes R rows: their sines and cosines (R dh/2 of them, for all
 // heads) go to shared memory while the first rows are on their way.  A thread holds eight values of a head's first half and the
 // eight they are paired with, dh / 16 threads a head, so that the sum of squares needs log2(dh / 16) shuffles; the next such item is
-// loaded before one is worked on.  16384 rows of 40 heads of 128: four items in flight in 124 registers a thread 128 us, one ahead in 64: 67 us (floor 51).
+// loaded before one is worked on.  16384 rows of 40 heads of 128: four items in flight in 124 registers a thread 128 us, one ahead in 64: 63 us
+// (floor 51).
 #include "kv4.cuh"
 
 namespace l2pd {
@@ -149,11 +150,15 @@ cudaError_t launch_qk_norm_rope(cudaStream_t st, const NormRopeArgs &a, int sms)
   for (int i = 0; i < half; ++i, x *= step) f.f[i] = (double)x;
   const int L = a.dh / 16, heads = a.Hq + a.Hk;
   if (a.vec && (L & (L - 1)) == 0) {
-    // rows of a block: sixteen rounds, but no fewer than four blocks an SM
-    const int64_t fill = (int64_t)16 * 256 / ((int64_t)heads * L), share = a.rows / (4 * sms);
-    int64_t R = fill < share ? fill : share;
-    if (R > TABLE / half) R = TABLE / half;
-    if (R < 1) R = 1;
+    // rows of a block: at most sixteen rounds of its threads; below that the number with which blocks, four an SM at a time, are done
+    // soonest, a block counted as a row more than it has (16384 rows of 40 heads of 128: 12 rows 66 us, 7 rows
+    // 63; heads of 64: 16 rows 42.5 us, 14 rows 33)
+    int64_t most = (int64_t)16 * 256 / ((int64_t)heads * L), R = 1, best = INT64_MAX;
+    if (most > TABLE / half) most = TABLE / half;
+    for (int64_t r = most < 1 ? 1 : most; r >= 1; --r) {
+      const int64_t cost = ceil_div64(ceil_div64(a.rows, r), (int64_t)4 * sms) * (r + 1);   // a row's time for what a block takes besides
+      if (cost < best) { best = cost; R = r; }
+    }
     return launch_kernel(qk_norm_rope_vec_kernel<T>, dim3((unsigned)ceil_div64(a.rows, R)), dim3(256), 0, st, a, f, (int)R, L);
   }
   const int64_t blocks = ceil_div64((int64_t)a.rows * heads, 8);
