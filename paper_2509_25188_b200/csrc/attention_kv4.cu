@@ -540,7 +540,7 @@ cudaError_t launch_attention_kv4(cudaStream_t st, const Kv4AttnArgs &a, int sms)
   Line &ln = p.line;
   ln.B = a.b.B; ln.H = a.c.heads; ln.chunk = pl.chunk; ln.group = a.Hq / a.c.heads; ln.slots = a.c.slots;
   ln.max_keys = a.max_len < a.c.cap ? a.max_len : a.c.cap; ln.tile_keys = pl.tc ? TC_TILE : KV4_TILE; ln.min_chunks = 0; ln.b = a.b;
-  ln.sms = sms; ln.piece = pl.tc ? 7 : 512 / pl.chunk;
+  ln.sms = sms; ln.piece = pl.tc ? 10 : pl.chunk == 8 ? 64 : pl.chunk == 16 ? 32 : 24;
   const int cols = a.b.rows * ln.group;
   cudaError_t e;
   if (pl.tc) e = launch_attention_kv4_tc(st, p, a.c.dh, pl.ctas);
