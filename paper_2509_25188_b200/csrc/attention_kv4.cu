@@ -18,7 +18,7 @@
 //
 // What bounds it.  One row of 32/8 heads on 4000 keys: the latency of a few dependent steps and of two launches, 11 us.  Up to 8
 // columns on many keys: memory (64 rows of 32/8 heads on 8192 keys each: 116 us, 4.9 TB/s).  32 columns (8 x 32 rows of 32 heads of
-// 128 on 2048 keys, 44 us): products 512 cycles of a scheduler and 453 instructions for 16 keys, which take 1250; registers leave two
+// 128 on 2048 keys, 42 us): products 512 cycles of a scheduler and 453 instructions for 16 keys, which take 1250; registers leave two
 // warps a scheduler, and each goes through products, exponentials and products in turn.
 #include <cuda_fp16.h>
 #include <math.h>
