@@ -237,7 +237,7 @@ __global__ void __launch_bounds__(SELECT_THREADS) kv4_select_kernel(const Kv4Evi
   const int n = slot < 0 ? 0 : max(0, min(min(a.b.keys[seq], a.max_len), a.src.cap)), m = min(n, a.keep);
   int32_t *kept = a.kept + ((int64_t)seq * H + h) * a.keep;
   if (blockIdx.x == 0 && tid == 0) a.lens_out[seq] = m;
-  for (int j = m + me * SELECT_THREADS + tid; j < a.keep; j += cluster * SELECT_THREADS) kept[j] = -1;
+  for (uint32_t j = m + me * SELECT_THREADS + tid; j < (uint32_t)a.keep; j += cluster * SELECT_THREADS) kept[j] = -1;   // keep may end at 2^31 - 1
   if (n <= a.keep) {                              // the whole cluster
     for (int j = me * SELECT_THREADS + tid; j < n; j += cluster * SELECT_THREADS) kept[j] = j;
     return;
@@ -495,7 +495,9 @@ cudaError_t launch_kv4_evict(cudaStream_t st, const Kv4EvictArgs &a) {
   cfg.attrs = at; cfg.numAttrs = pdl_enabled() ? 2 : 1;
   e = cudaLaunchKernelEx(&cfg, kv4_select_kernel, a, cluster, slice);
   if (e != cudaSuccess) return e;
-  return launch_kernel(kv4_move_kernel, dim3((unsigned)(ceil_div(a.keep, MOVE_PLACES) * a.src.heads), a.b.B), dim3(256), 0, st, a);
+  const int places = a.keep < a.max_len ? a.keep : a.max_len;   // no place behind them is filled, whatever `keep` allows
+  if (places == 0) return cudaSuccess;
+  return launch_kernel(kv4_move_kernel, dim3((unsigned)(ceil_div(places, MOVE_PLACES) * a.src.heads), a.b.B), dim3(256), 0, st, a);
 }
 
 }  // namespace l2pd

@@ -543,6 +543,24 @@ def test_evict_without_positions_and_twice():
         _same(c.load(100, dtype=torch.float32)[0][0, :, h], plain.values32(_np(k))[0, p1[want], h])
 
 
+@pytest.mark.parametrize("keep", [2 ** 31 - 1, 2 ** 31 - 130])
+def test_evict_that_keeps_everything(keep):
+    """`keep` as "no limit": every key stays, and the places behind them say so to the last one."""
+    b = _b()
+    c = b.KvCache4(1, 1, 64, 9000)
+    k = _rand(45, 1, 9000, 1, 64)
+    c.store(k, k)
+    before, w = c.data.clone(), torch.rand(1, 1, 9000, device=DEV)
+    kept, new = c.evict(w, _i32([8999]), 9000, keep)                    # 8.6 GB of places
+    assert new.tolist() == [8999] and kept.shape == (1, 1, keep)
+    assert torch.equal(kept[0, 0, :8999], torch.arange(8999, dtype=torch.int32, device=DEV))
+    assert int(kept[0, 0, 8999:].max()) == -1 and int(kept[0, 0, 8999:].min()) == -1
+    assert torch.equal(c.data, before)
+    del kept
+    kept, new = c.evict(w, _i32([5]), 0, 7)                             # no key may be read
+    assert new.tolist() == [0] and (kept == -1).all()
+
+
 # ---- norms and rotation ------------------------------------------------------------------------------------------------------
 
 @pytest.mark.parametrize("norm", [True, False])
