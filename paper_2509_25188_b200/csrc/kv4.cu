@@ -117,7 +117,8 @@ __global__ void __launch_bounds__(256, 5) kv4_store_kernel(const Kv4View c, cons
     float inv;
     asm("rcp.approx.f32 %0, %1;" : "=f"(inv) : "f"(s));
     inv = fmaf(inv, -4.76837158203125e-7f, inv);
-    if (least && most - least > 15)
+    // a subnormal has the exponent field 0, as no value at all has: `near` tells them apart
+    if ((near & 0xffffu) != 0x8000u && most - least > 15)
       codes = make_uint4(kv4_codes<true>(wv, mn, s, inv), kv4_codes<true>(wv + 4, mn, s, inv), kv4_codes<true>(wv + 8, mn, s, inv), kv4_codes<true>(wv + 12, mn, s, inv));
     else
       codes = make_uint4(kv4_codes<false>(wv, mn, s, inv), kv4_codes<false>(wv + 4, mn, s, inv), kv4_codes<false>(wv + 8, mn, s, inv), kv4_codes<false>(wv + 12, mn, s, inv));

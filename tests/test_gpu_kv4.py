@@ -9,6 +9,8 @@ for the exponentials and sums.  Probabilities times s are rounded to fp16 (2^-11
 """
 from __future__ import annotations
 
+from fractions import Fraction
+
 import numpy as np
 import pytest
 import torch
@@ -86,6 +88,39 @@ def test_rows_at_the_ends_of_the_range(dh):
     gk, gv = c.load(12, dtype=torch.float32)
     _same(gk[0], plain.values32(_np(x)))
     _same(gv[0], plain.values32(_np(x)))
+
+
+def _exact_codes(row, m, s):
+    """Codes of one row in rational arithmetic."""
+    out = []
+    for x in row:
+        t = (Fraction(float(x)) - Fraction(float(m))) / Fraction(float(s))
+        low = t.__floor__()
+        up = t - low > Fraction(1, 2) or (t - low == Fraction(1, 2) and low % 2)
+        out.append(min(15, low + int(up)))
+    return out
+
+
+@pytest.mark.parametrize("tiny", [9.2e-41, 1e-39, 1.0e-38, 1.2e-38, 1e-30, 1e-9])
+@pytest.mark.parametrize("dh", [64, 128])
+def test_values_beside_a_border(dh, tiny):
+    """A subnormal moves a quotient off a border as any other number does: 64 bits lose it beside 8, rational numbers do not."""
+    b = _b()
+    rows = np.zeros((6, dh), np.float32)
+    for i, lo in enumerate((-7.5, -8.5, -6.5)):                         # 0 lies on the borders 7.5, 8.5 and 6.5 of step 1
+        rows[2 * i, :5] = [lo, lo + 15, tiny, -tiny, 0]
+        rows[2 * i + 1, -4:] = [lo + 15, -tiny, tiny, lo]               # the other end of the row, no zero in its quarter
+        rows[2 * i + 1, :dh // 2] = tiny
+    x = torch.from_numpy(rows).to(torch.bfloat16)
+    assert (x[0, 2] != 0) and (x[0, 3] != 0)
+    c = b.KvCache4(1, 1, dh, 6)
+    c.store(x.to(DEV)[:, None], x.to(DEV)[:, None])
+    gk, gv = c.load(6, dtype=torch.float32)
+    for i, row in enumerate(x.float().numpy()):
+        m = row.min()
+        want = np.array(_exact_codes(row, m, 1.0)) + np.float64(m)      # step 1, few bits: exact
+        _same(gk[0, i, 0], want)
+        _same(gv[0, i, 0], want)
 
 
 def test_ragged_batch_into_chosen_slots_and_places():
