@@ -4,7 +4,7 @@
 // S^T = K Q^T, keys on the M side of mma.sync.m16n8k16, so that one query row pads to 8 columns instead of 16 rows, and the
 // output as O^T = V^T P^T.  A code c in the low four bits of an fp16 is the subnormal number c 2^-24, exactly: the codes go to the
 // product as they lie, by a mask (those in bits 4..7 as 16 c 2^-24, against queries divided by 16).  With q' = q scaled by a power
-// of two into fp16's range (8 significant bits of 11):
+// of two of its own into fp16's range (8 significant bits of 11), and cf what undoes it:
 //     t_j = log2 of exp(scale q . k_j) + e_j = cf (s_j sum(c q') + m_j sum(q')) + e_j - E
 // 2^e_j bounds the value row's s_j and |m_j| / 16, E the largest e_j.  Probabilities are taken as p'_j = 2^(t_j - M), M a reference at
 // most 2^6 below the running maximum of t, so that p'_j s_j 2^-e_j, what multiplies the codes of V, stays within fp16 whatever the
@@ -63,6 +63,9 @@ template <int DH> struct Queries {
     top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
   }
   __device__ __forceinline__ bool finite() const { return top < 0x7f800000u; }
+  // Power of two that takes the column's largest to 2^14 .. 2^15: what is less than 2^-35 of it is lost (odd dimensions go in divided by 16).
+  // Columns have powers of their own: rows of a block may differ without limit.
+  __device__ __forceinline__ int exponent() const { return finite() ? min(14 - ((int)(top >> 23) - 127), 126) : 0; }
   // Scaled by 2^u to fp16.  Returns the column's sum in the scale of the products with codes; NaN: a column that holds an
   // infinity or NaN, whose scores are all NaN.
   __device__ __forceinline__ float convert(int u, uint32_t (&f)[DH / 8]) const {
@@ -86,12 +89,10 @@ template <int DH> struct Queries {
     return finite() ? sum * __uint_as_float((127 - 24) << 23) : __uint_as_float(0x7fc00000u);
   }
 };
-// Power of two that takes the largest of all columns to 2^14 .. 2^15.  (A column 2^20 below the largest still has 2^-19 of its own
-// magnitude, and scores a millionth of the other's.)  What then turns the products into log2 scores: scale 2^(24 - u).
-__device__ __forceinline__ int query_exponent(uint32_t top) { return min(14 - ((int)(top >> 23) - 127), 126); }
-__device__ __forceinline__ float query_factor(float scale_log2, int u) {
-  return scale_log2 * 1024.f * __uint_as_float((uint32_t)(127 + 14 - u) << 23);
-}
+// What turns a column's products, with K's s and m times 2^12, into log2 scores: scale 2^(12 - u).  (2^24 in one place would pass fp32 for
+// queries near 2^127.)
+constexpr float K_UNIT = 4096.f;
+__device__ __forceinline__ float query_factor(float scale_log2, int u) { return scale_log2 * __uint_as_float((uint32_t)(127 + 12 - u) << 23); }
 
 template <int DH, int NT> struct AttnShape {
   static constexpr int CH = 8 * NT, TILE = KV4_TILE * (DH + 8), STAGES = NT == 4 ? 4 : 3, RING = STAGES * TILE;
@@ -110,14 +111,13 @@ __global__ void __launch_bounds__(WARPS * 32, AttnShape<DH, NT>::CTAS) attention
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ __align__(8) uint64_t bars[WARPS * STAGES];
   __shared__ float fin[WARPS][2][CH];              // reference and sum of probabilities
-  __shared__ float qsum[CH];
-  __shared__ uint32_t qtop[WARPS];
+  __shared__ float4 qcol[CH / 2];                  // of two columns: sums of q' times cf, and cf
   __shared__ int abort_flag;
   const int warp = ptx::warp_index(), lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   const uint32_t bar0 = ptx::smem_u32(&bars[warp * STAGES]);
   uint8_t *const ring = smem + warp * RING;
   const uint32_t ring_u = ptx::smem_u32(ring);
-  float4 *const meta_a = reinterpret_cast<float4 *>(smem + Sh::OFF_META + warp * Sh::META);   // by key: cf s, cf m of K, e - E, 2^(E - e)
+  float4 *const meta_a = reinterpret_cast<float4 *>(smem + Sh::OFF_META + warp * Sh::META);   // by key: s, m of K, e - E, 2^(E - e)
   float2 *const meta_b = reinterpret_cast<float2 *>(meta_a + KV4_TILE);                        // s 2^-e, m 2^-e of V
   uint4 *const qs = reinterpret_cast<uint4 *>(smem + Sh::OFF_Q);
   if (lane == 0) {
@@ -158,34 +158,34 @@ __global__ void __launch_bounds__(WARPS * 32, AttnShape<DH, NT>::CTAS) attention
     for (int i = 0; i < STAGES; ++i) request(i);
 
     // queries: warp n converts the columns 8 n .. 8 n + 7 for all
-    Queries<DH> qn;
-    qn.top = 0;
     if (warp < NT) {
       const int col = c0 + 8 * warp + g, r = col / ln.group;
+      Queries<DH> qn;
       qn.load(p.q + (int64_t)(row0 + r) * p.q_stride + (int64_t)(h * ln.group + col - r * ln.group) * DH + t * (DH / 4), 8 * warp + g < cols);
-    }
-    const uint32_t top = __reduce_max_sync(0xffffffffu, qn.finite() ? qn.top : 0u);
-    if (lane == 0) qtop[warp] = top;
-    __syncthreads();
-    const int u = query_exponent(max(max(qtop[0], qtop[1]), max(qtop[2], qtop[3])));
-    const float cf = query_factor(p.scale_log2, u);
-    if (warp < NT) {
       uint32_t f[DH / 8];
-      const float cs = qn.convert(u, f);
-      if (t == 0) qsum[8 * warp + g] = cs;
+      const int u = qn.exponent();
+      const float sum = qn.convert(u, f), cf = query_factor(p.scale_log2, u);
+      if (t == 0) {
+        float *of = reinterpret_cast<float *>(&qcol[4 * warp + (g >> 1)]) + (g & 1);
+        of[0] = sum * cf; of[2] = cf;
+      }
 #pragma unroll
       for (int j = 0; j < W; ++j) qs[(warp * W + j) * 32 + lane] = make_uint4(f[4 * j], f[4 * j + 1], f[4 * j + 2], f[4 * j + 3]);
     }
     __syncthreads();
     uint32_t qf[Sh::Q_REGS ? NT : 1][DH / 8];
-    F2 cs[NT];                                     // columns 2t and 2t + 1 of each eight
+    F2 cs[Sh::Q_REGS ? NT : 1], cf[Sh::Q_REGS ? NT : 1];   // columns 2t and 2t + 1 of each eight
+    auto column_factors = [&](int n, F2 &sum, F2 &factor) {
+      const float4 x = qcol[4 * n + t];
+      sum = ptx::f2(x.x, x.y); factor = ptx::f2(x.z, x.w);
+    };
     F2 neg_m[NT], l[NT], wm[NT];                   // minus the reference, sum of probabilities, sum of probability times m
     float o[MT][NT][4];
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
 #pragma unroll
       for (int j = 0; Sh::Q_REGS && j < W; ++j) *reinterpret_cast<uint4 *>(&qf[Sh::Q_REGS ? n : 0][4 * j]) = qs[(n * W + j) * 32 + lane];
-      cs[n] = ptx::f2(qsum[8 * n + 2 * t], qsum[8 * n + 2 * t + 1]);
+      if (Sh::Q_REGS) column_factors(n, cs[Sh::Q_REGS ? n : 0], cf[Sh::Q_REGS ? n : 0]);
       neg_m[n] = l[n] = wm[n] = ptx::f2(0.f, 0.f);
 #pragma unroll
       for (int m = 0; m < MT; ++m) o[m][n][0] = o[m][n][1] = o[m][n][2] = o[m][n][3] = 0.f;
@@ -218,7 +218,7 @@ __global__ void __launch_bounds__(WARPS * 32, AttnShape<DH, NT>::CTAS) attention
         }
         const int e = max(ex, e0 - 60);
         const float w = __uint_as_float((uint32_t)(127 - e) << 23);
-        meta_a[lane] = make_float4(kv4_scale(km) * cf, kv4_min(km) * cf, real ? (float)(e - e0) : -INFINITY,
+        meta_a[lane] = make_float4(kv4_scale(km) * K_UNIT, kv4_min(km) * K_UNIT, real ? (float)(e - e0) : -INFINITY,
                                    __uint_as_float((uint32_t)(127 - e + e0) << 23));
         meta_b[lane] = make_float2(kv4_scale(vm) * w, kv4_min(vm) * w);
         __syncwarp();
@@ -274,7 +274,9 @@ __global__ void __launch_bounds__(WARPS * 32, AttnShape<DH, NT>::CTAS) attention
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
               float *x = &acc[u][n][2 * e];
-              const F2 y = ptx::fma2(ptx::f2(x[0], x[1]), ks, ptx::add2(ptx::fma2(km, cs[n], bias), neg_m[n]));
+              F2 sum = cs[Sh::Q_REGS ? n : 0], factor = cf[Sh::Q_REGS ? n : 0];
+              if (!Sh::Q_REGS) column_factors(n, sum, factor);
+              const F2 y = ptx::fma2(ptx::mul2(ptx::f2(x[0], x[1]), factor), ks, ptx::add2(ptx::fma2(km, sum, bias), neg_m[n]));
               x[0] = ptx::f2_lo(y); x[1] = ptx::f2_hi(y);
               top = fmaxf(top, fmaxf(x[0], x[1]));
             }
@@ -584,8 +586,8 @@ __global__ void __launch_bounds__(WARPS * 32, 4) kv4_weights_kernel(const WeighP
   constexpr int W = DH / 32, STAGES = Sh::STAGES;
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ __align__(8) uint64_t bars[WARPS * STAGES];
-  __shared__ float2 of_col[WEIGH_COLS];            // sum of the scaled queries, minus the log-sum
-  __shared__ uint32_t qtop[WARPS];
+  __shared__ __align__(16) float2 of_col[WEIGH_COLS];            // sum of the scaled queries times cf, minus the log-sum
+  __shared__ __align__(16) float cf_col[WEIGH_COLS];             // cf
   __shared__ int abort_flag;
   const int warp = ptx::warp_index(), lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   const uint32_t bar0 = ptx::smem_u32(&bars[warp * STAGES]);
@@ -628,35 +630,20 @@ __global__ void __launch_bounds__(WARPS * 32, 4) kv4_weights_kernel(const WeighP
         }
       };
       for (int i = 0; i < STAGES; ++i) request(i);
-      // queries: each warp converts every fourth eight of columns.  Two rounds: the largest of all, then the conversion
-      struct Column { int row, head; bool there; };
-      auto column = [&](int n) {
-        const int col = c0 + 8 * n + g, r = col / ln.group;
-        return Column{sq.row0 + r, h * ln.group + col - r * ln.group, 8 * n + g < here};
-      };
-      auto address = [&](const Column &x) { return p.q + (int64_t)x.row * p.q_stride + (int64_t)x.head * DH + t * (DH / 4); };
-      uint32_t top = 0;
+      // queries: each warp converts every fourth eight of columns
       for (int n = warp; n < nts; n += WARPS) {
-        const Column x = column(n);
+        const int col = c0 + 8 * n + g, r = col / ln.group, row = sq.row0 + r, head = h * ln.group + col - r * ln.group;
+        const bool there = 8 * n + g < here;
         Queries<DH> qn;
-        qn.load(address(x), x.there);
-        if (qn.finite()) top = max(top, qn.top);
-      }
-      top = __reduce_max_sync(0xffffffffu, top);
-      if (lane == 0) qtop[warp] = top;
-      __syncthreads();
-      const int u = query_exponent(max(max(qtop[0], qtop[1]), max(qtop[2], qtop[3])));
-      const float cf = query_factor(p.scale_log2, u);
-      for (int n = warp; n < nts; n += WARPS) {
-        const Column x = column(n);
-        Queries<DH> qn;
-        qn.load(address(x), x.there);
+        qn.load(p.q + (int64_t)row * p.q_stride + (int64_t)head * DH + t * (DH / 4), there);
         uint32_t f[DH / 8];
-        const float cs = qn.convert(u, f);
+        const int u = qn.exponent();
+        const float sum = qn.convert(u, f), cf = query_factor(p.scale_log2, u);
         if (t == 0) {
-          float l = x.there ? p.lse[(int64_t)x.row * p.Hq + x.head] * 1.4426950408889634f : INFINITY;
+          float l = there ? p.lse[(int64_t)row * p.Hq + head] * 1.4426950408889634f : INFINITY;
           if (l == -INFINITY) l = INFINITY;        // a row without keys gives no weight
-          of_col[8 * n + g] = make_float2(cs, -l);
+          of_col[8 * n + g] = make_float2(sum * cf, -l);
+          cf_col[8 * n + g] = cf;
         }
 #pragma unroll
         for (int j = 0; j < W; ++j) qs[(n * W + j) * 32 + lane] = make_uint4(f[4 * j], f[4 * j + 1], f[4 * j + 2], f[4 * j + 3]);
@@ -679,7 +666,7 @@ __global__ void __launch_bounds__(WARPS * 32, 4) kv4_weights_kernel(const WeighP
           if (DH == 128) *reinterpret_cast<uint4 *>(k[e]) = *reinterpret_cast<const uint4 *>(a);
           else *reinterpret_cast<uint2 *>(k[e]) = *reinterpret_cast<const uint2 *>(a);
           const uint32_t m = *reinterpret_cast<const uint32_t *>(tile + kv4_off_kmeta(DH) + 4 * (g + 8 * e));
-          ks[e] = kv4_scale(m) * cf; km[e] = kv4_min(m) * cf;
+          ks[e] = kv4_scale(m) * K_UNIT; km[e] = kv4_min(m) * K_UNIT;
         }
         __syncwarp();
         request(i + STAGES);
@@ -704,10 +691,13 @@ __global__ void __launch_bounds__(WARPS * 32, 4) kv4_weights_kernel(const WeighP
               ptx::mma_f16_16x8x16(acc[m], x[2 * m][4 * j + 2], x[2 * m + 1][4 * j + 2], x[2 * m][4 * j + 3], x[2 * m + 1][4 * j + 3], f.z, f.w);
           }
           const float4 of = *reinterpret_cast<const float4 *>(&of_col[8 * n + 2 * t]);   // columns 2t and 2t + 1
+          const float2 cf2 = *reinterpret_cast<const float2 *>(&cf_col[8 * n + 2 * t]);
+          const F2 cf = ptx::f2(cf2.x, cf2.y);
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             const float *a = &acc[e >> 1][2 * (e & 1)];
-            w[e] += ptx::ex2(fmaf(a[0], ks[e], fmaf(km[e], of.x, of.y))) + ptx::ex2(fmaf(a[1], ks[e], fmaf(km[e], of.z, of.w)));
+            const F2 x = ptx::mul2(ptx::f2(a[0], a[1]), cf);
+            w[e] += ptx::ex2(fmaf(ptx::f2_lo(x), ks[e], fmaf(km[e], of.x, of.y))) + ptx::ex2(fmaf(ptx::f2_hi(x), ks[e], fmaf(km[e], of.z, of.w)));
           }
         }
 #pragma unroll

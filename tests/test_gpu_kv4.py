@@ -279,6 +279,36 @@ def test_any_scale_and_ragged_last_tiles(rows, scale, dh):
         _check_attention(q[i], k[i, :n], v[i, :n], out[i], lse[i], scale)
 
 
+def _uneven_queries(rows, dh):
+    """Keys without negative numbers, 0 in dimension 0 of every one (kept exactly), and a block of queries whose row 1 is 2^60 in that dimension
+    alone: its scores are 0, and the other rows' are what they would be without it."""
+    b = _b()
+    c = b.KvCache4(1, 1, dh, 500)
+    k, v = _rand(91, 500, 1, dh).abs(), _rand(92, 500, 1, dh)
+    k[..., 0] = 0
+    q = _rand(93, rows, 1, dh, scale=3)
+    q[1] = 0
+    q[1, 0, 0] = 2.0 ** 60
+    q[rows // 2 + 1 if rows > 2 else 0] *= 2.0 ** -10
+    c.store(k, v)
+    return b, c, k, v, q
+
+
+@pytest.mark.parametrize("dh", [64, 128])
+@pytest.mark.parametrize("rows", [2, 3, 12, 20, 40, 130])
+def test_a_row_does_not_decide_the_precision_of_others(rows, dh):
+    b, c, k, v, q = _uneven_queries(rows, dh)
+    n = _i32([500])
+    out, lse = c.attention(q, n, 500)
+    _check_attention(q, k, v, out, lse, dh ** -0.5)
+    w = c.attention_weights(q, lse, n, 500, torch.zeros(1, 1, 500, device=DEV))
+    kk, qn = plain.values(_np(k)), _np(q)
+    _, _, want = plain.attention(qn, kk, kk, dh ** -0.5)
+    code, s, m = plain.quantise(_np(k))
+    d = (np.abs(qn[:, 0]) @ (code * s + np.abs(m))[:, 0].T).max() * dh ** -0.5 * (dh / 16 + 8) * 2.0 ** -23     # as in test_weights
+    assert (np.abs(_np(w)[0] - want) <= (2 * d + 2.0 ** -19 + rows * 2.0 ** -24) * want + 2.0 ** -23 * want).all()
+
+
 @pytest.mark.parametrize("rows", [2, 40])
 def test_nan_stays_where_it_belongs(rows):
     b = _b()
