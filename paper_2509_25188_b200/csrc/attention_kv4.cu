@@ -5,11 +5,10 @@
 // output as O^T = V^T P^T.  A code c in the low four bits of an fp16 is the subnormal number c 2^-24, exactly: the codes go to the
 // product as they lie, by a mask (those in bits 4..7 as 16 c 2^-24, against queries divided by 16).  With q' = q scaled by a power
 // of two of its own into fp16's range (8 significant bits of 11), and cf what undoes it:
-//     t_j = log2 of exp(scale q . k_j) + e_j = cf (s_j sum(c q') + m_j sum(q')) + e_j - E
-// 2^e_j bounds the value row's s_j and |m_j| / 16, E the largest e_j.  Probabilities are taken as p'_j = 2^(t_j - M), M a reference at
+//     t_j = log2 of exp(scale q . k_j) + e_j - E = cf (s_j sum(c q') + m_j sum(q')) + e_j - E
+// 2^e_j bounds the value row's s_j and |m_j| / 16, E is above all e_j so far.  Probabilities are taken as p'_j = 2^(t_j - M), M a reference at
 // most 2^6 below the running maximum of t, so that p'_j s_j 2^-e_j, what multiplies the codes of V, stays within fp16 whatever the
-// values' magnitude.  (e_j is at least E - 60, so that a row of zeros keeps its part of the sum of probabilities p'_j 2^(E - e_j).)
-// Rounding it to fp16 is the only step to less than 32 bits between the queries and the output.
+// values' magnitude (attention_kv4.cuh has what becomes of M and the sums where E rises).  Rounding it to fp16 is the only step to less than 32 bits between the queries and the output.
 //
 // Work: the key tiles of all (sequence, head, chunk of columns) stand in one line and every CTA takes an equal run of it; a run
 // that starts or ends inside an item leaves a partial result, joined in the order of the tiles by a second kernel.  A warp takes
@@ -110,14 +109,14 @@ __global__ void __launch_bounds__(WARPS * 32, AttnShape<DH, NT>::CTAS) attention
   static_assert(KV4_TILE == 32 && CH * LDO * 4 <= RING, "a warp's output goes to its ring");
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ __align__(8) uint64_t bars[WARPS * STAGES];
-  __shared__ float fin[WARPS][2][CH];              // reference and sum of probabilities
+  __shared__ float fin[WARPS][2][CH];              // reference and sum of weights
   __shared__ float4 qcol[CH / 2];                  // of two columns: sums of q' times cf, and cf
   __shared__ int abort_flag;
   const int warp = ptx::warp_index(), lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   const uint32_t bar0 = ptx::smem_u32(&bars[warp * STAGES]);
   uint8_t *const ring = smem + warp * RING;
   const uint32_t ring_u = ptx::smem_u32(ring);
-  float4 *const meta_a = reinterpret_cast<float4 *>(smem + Sh::OFF_META + warp * Sh::META);   // by key: s, m of K, e - E, 2^(E - e)
+  float4 *const meta_a = reinterpret_cast<float4 *>(smem + Sh::OFF_META + warp * Sh::META);   // by key: s, m of K, e - E, 2^(E - e - LOG_L)
   float2 *const meta_b = reinterpret_cast<float2 *>(meta_a + KV4_TILE);                        // s 2^-e, m 2^-e of V
   uint4 *const qs = reinterpret_cast<uint4 *>(smem + Sh::OFF_Q);
   if (lane == 0) {
@@ -205,21 +204,27 @@ __global__ void __launch_bounds__(WARPS * 32, AttnShape<DH, NT>::CTAS) attention
         const uint32_t vm = real ? *reinterpret_cast<const uint32_t *>(tile + kv4_off_vmeta(DH) + 4 * lane) : 0u;
         const int ex = min(max((int)((vm >> 7) & 255u), (int)((vm >> 23) & 255u) - 4) - 126, 100);
         const int ex_top = __reduce_max_sync(0xffffffffu, ex);
-        if (ex_top > e0) {                         // rare: what came before is in units of 2^e0
-          const int was = e0;
+        if (ex_top > e0) {                         // rare
+          const float d = e0 == -1000 ? 0.f : (float)(max(ex_top, -100) + 2 - e0);
           e0 = max(ex_top, -100) + 2;
-          const float f = __uint_as_float((uint32_t)max(127 - (e0 - was), 0) << 23);
 #pragma unroll
           for (int n = 0; n < NT; ++n) {
-            wm[n] = ptx::mul2(wm[n], ptx::f2(f, f));
+            const F2 was = neg_m[n];
+            neg_m[n] = ptx::add2(was, ptx::f2(d, d));
+            const float da = ptx::f2_lo(neg_m[n]) - ptx::f2_lo(was), db = ptx::f2_hi(neg_m[n]) - ptx::f2_hi(was);
+            l[n] = ptx::f2(ex2_scaled(ptx::f2_lo(l[n]), da), ex2_scaled(ptx::f2_hi(l[n]), db));
+            if (__any_sync(0xffffffffu, da != d || db != d)) {   // references beyond 2^24 do not move by d exactly
+              const float fa = ptx::ex2(da - d), fb = ptx::ex2(db - d);
+              wm[n] = ptx::mul2(wm[n], ptx::f2(fa, fb));
 #pragma unroll
-            for (int m = 0; m < MT; ++m) { o[m][n][0] *= f; o[m][n][1] *= f; o[m][n][2] *= f; o[m][n][3] *= f; }
+              for (int m = 0; m < MT; ++m) { o[m][n][0] *= fa; o[m][n][2] *= fa; o[m][n][1] *= fb; o[m][n][3] *= fb; }
+            }
           }
         }
-        const int e = max(ex, e0 - 60);
+        const int e = max(ex, e0 + (int)FLOOR);
         const float w = __uint_as_float((uint32_t)(127 - e) << 23);
         meta_a[lane] = make_float4(kv4_scale(km) * K_UNIT, kv4_min(km) * K_UNIT, real ? (float)(e - e0) : -INFINITY,
-                                   __uint_as_float((uint32_t)(127 - e + e0) << 23));
+                                   pow2(e0 - e - LOG_L));
         meta_b[lane] = make_float2(kv4_scale(vm) * w, kv4_min(vm) * w);
         __syncwarp();
       }
@@ -300,7 +305,8 @@ __global__ void __launch_bounds__(WARPS * 32, AttnShape<DH, NT>::CTAS) attention
             const float sa = first ? 0.f : ptx::ex2(-da), sb = first ? 0.f : ptx::ex2(-db);
             const F2 d = ptx::f2(-da, -db), sc = ptx::f2(sa, sb);
             neg_m[n] = ptx::add2(neg_m[n], d);
-            l[n] = ptx::mul2(l[n], sc); wm[n] = ptx::mul2(wm[n], sc);
+            l[n] = ptx::f2(ex2_scaled(ptx::f2_lo(l[n]), -da), ex2_scaled(ptx::f2_hi(l[n]), -db));
+            wm[n] = ptx::mul2(wm[n], sc);
 #pragma unroll
             for (int m = 0; m < MT; ++m) { o[m][n][0] *= sa; o[m][n][2] *= sa; o[m][n][1] *= sb; o[m][n][3] *= sb; }
 #pragma unroll
@@ -367,20 +373,20 @@ __global__ void __launch_bounds__(WARPS * 32, AttnShape<DH, NT>::CTAS) attention
         la += __shfl_xor_sync(0xffffffffu, la, x); lb += __shfl_xor_sync(0xffffffffu, lb, x);
         wa += __shfl_xor_sync(0xffffffffu, wa, x); wb += __shfl_xor_sync(0xffffffffu, wb, x);
       }
+      const Normal na = normalised(la, -ptx::f2_lo(neg_m[n]), max(e0, -100)), nb = normalised(lb, -ptx::f2_hi(neg_m[n]), max(e0, -100));
       if (g == 0) {
-        fin[warp][0][8 * n + 2 * t] = mine > 0 ? -ptx::f2_lo(neg_m[n]) : -INFINITY;
-        fin[warp][0][8 * n + 2 * t + 1] = mine > 0 ? -ptx::f2_hi(neg_m[n]) : -INFINITY;
-        fin[warp][1][8 * n + 2 * t] = la; fin[warp][1][8 * n + 2 * t + 1] = lb;
+        fin[warp][0][8 * n + 2 * t] = na.ref; fin[warp][0][8 * n + 2 * t + 1] = nb.ref;      // no tiles: -inf
+        fin[warp][1][8 * n + 2 * t] = na.x; fin[warp][1][8 * n + 2 * t + 1] = nb.x;
       }
       float *oa = reinterpret_cast<float *>(ring) + (8 * n + 2 * t) * LDO + g * (DH / 8), *ob = oa + LDO;
       constexpr float EVEN = 16777216.f, ODD = 1048576.f;             // the codes' 2^24, and 2^20 where they came 16 times
-      const float unit = __uint_as_float((uint32_t)(127 + max(e0, -126)) << 23);
+      auto in_unit = [](float x, float unit, float w, const Normal &f) { return fmaf(x, unit, w) * f.up_a * f.up_b; };
 #pragma unroll
       for (int m = 0; m < MT; m += 2) {
-        *reinterpret_cast<float4 *>(oa + 2 * m) = make_float4(fmaf(o[m][n][0], EVEN, wa) * unit, fmaf(o[m][n][2], ODD, wa) * unit,
-                                                              fmaf(o[m + 1][n][0], EVEN, wa) * unit, fmaf(o[m + 1][n][2], ODD, wa) * unit);
-        *reinterpret_cast<float4 *>(ob + 2 * m) = make_float4(fmaf(o[m][n][1], EVEN, wb) * unit, fmaf(o[m][n][3], ODD, wb) * unit,
-                                                              fmaf(o[m + 1][n][1], EVEN, wb) * unit, fmaf(o[m + 1][n][3], ODD, wb) * unit);
+        *reinterpret_cast<float4 *>(oa + 2 * m) = make_float4(in_unit(o[m][n][0], EVEN, wa, na), in_unit(o[m][n][2], ODD, wa, na),
+                                                              in_unit(o[m + 1][n][0], EVEN, wa, na), in_unit(o[m + 1][n][2], ODD, wa, na));
+        *reinterpret_cast<float4 *>(ob + 2 * m) = make_float4(in_unit(o[m][n][1], EVEN, wb, nb), in_unit(o[m][n][3], ODD, wb, nb),
+                                                              in_unit(o[m + 1][n][1], EVEN, wb, nb), in_unit(o[m + 1][n][3], ODD, wb, nb));
       }
     }
     __syncthreads();

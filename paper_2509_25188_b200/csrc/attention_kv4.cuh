@@ -8,6 +8,31 @@ namespace kv4 {
 
 constexpr float LAZY = 6.0f;         // log2 units the running maximum may pass the reference
 
+// ---- one unit for values of any size -----------------------------------------------------------------------------------
+// A key's probability goes to the product as p' = 2^(t - M), t = log2 w + b: w its weight, b = (the exponent of its values) - E, E one that
+// no value has passed so far.  Two sums then stand for the output: O = sum p' v 2^-(E + b) = sum w v 2^(-E - M), and l = sum p' 2^-b = sum w 2^-M.
+// Where E rises by d, M is lowered by d: what is in O stays, the keys to come keep their bits whatever the size of the row that raised E
+// (which may have no weight at all), and l alone grows by 2^d.  l lies between 1 and 2^227 times the keys, and is kept as l 2^-LOG_L.
+// FLOOR: the least b, so that p' is no zero where w counts; values 2^100 below the largest seen so far lose their size, rows of zeros take it.
+constexpr int LOG_L = 120;
+constexpr float FLOOR = -100.f;
+
+__device__ __forceinline__ float pow2(int n) { return __uint_as_float((uint32_t)(127 + n) << 23); }   // -126 <= n <= 127
+// x 2^d for d beyond one exponent's range
+__device__ __forceinline__ float ex2_scaled(float x, float d) { const float h = ptx::ex2(0.5f * d); return x * h * h; }
+// A sum l 2^-LOG_L against the reference M, as x 2^ref with x in [1, 2): sums against references far apart can then be added, and so can the
+// outputs that stand in the unit x 2^ref.  They come from O in the unit 2^unit by the two powers.  0: a sum of nothing; NaN stays.
+struct Normal { float x, ref, up_a, up_b; };
+__device__ __forceinline__ Normal normalised(float l, float m, int unit) {
+  const uint32_t u = __float_as_uint(l) & 0x7fffffffu;
+  const int e = (int)(u >> 23), k = e - 127 + LOG_L, n = max(unit - k, -250), h = n >> 1;
+  Normal r;
+  r.x = e == 255 ? l : e ? __uint_as_float((u & 0x7fffffu) | 0x3f800000u) : 0.f;
+  r.ref = e ? m + (float)k : -INFINITY;
+  r.up_a = e ? pow2(h) : 0.f; r.up_b = pow2(n - h);
+  return r;
+}
+
 // ---- the line of work --------------------------------------------------------------------------------------------------
 // Items: for sequence b, key heads times chunks of `chunk` columns (those that have rows), tiles_b key tiles each.  Fewer than 2^31
 // tiles in all (the host sees to it).  Every warp surveys the line for itself, a lane a sequence: the lengths and rows of 32
@@ -90,7 +115,7 @@ struct AttnParams {
   const bf16 *q; bf16 *out; float *lse;
   int64_t q_stride, out_stride;
   float scale_log2;
-  float *part;             // [2 * CTAs][chunk][dh + 4]: O, M, L of a partial item
+  float *part;             // [2 * CTAs][chunk][dh + 4]: of a partial item O, reference, sum of weights
   int32_t *status;
 };
 

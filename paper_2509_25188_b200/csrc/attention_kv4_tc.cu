@@ -11,8 +11,8 @@
 // multiplication by s 2^24 (2^20) lifts it.  Eight codes of a word come out in the order 0 4 1 5 2 6 3 7: queries are written in
 // that order, and outputs read in it.
 // Two groups of four softmax warps take the tiles alternately, a thread a lane: t = cf 2^E acc + (E_V - E0) - M, P = 2^t as fp16,
-// the A operand of the second product.  M is a reference that follows the running maximum lazily, E0 the largest E_V so far; O is
-// rescaled when one moves.  The thread that has fixed them for a tile hands them to the other group's thread of its lane before its
+// the A operand of the second product.  M is a reference that follows the running maximum lazily, E0 above the largest E_V so far
+// (attention_kv4.cuh has what becomes of M and the sums where it rises); O is rescaled when M moves against the scores.  The thread that has fixed them for a tile hands them to the other group's thread of its lane before its
 // exponentials.  128 keys of a lane are read twice, 64 at a time (registers): the maximum first, then the second half, at hand
 // still, then the first.  From that last read on S belongs to the tile after next, whose product runs under the exponentials (P
 // over S instead: 64 numbers a head 14 % slower, 128 numbers 1 % faster).
@@ -58,7 +58,6 @@ template <int DH> struct Tc {
 enum { B_FULL = 0, B_EMPTY = B_FULL + RING, B_KRDY = B_EMPTY + RING, B_KFREE = B_KRDY + NB, B_VRDY = B_KFREE + NB, B_VFREE = B_VRDY + NB,
        B_SFULL = B_VFREE + NB, B_PRDY = B_SFULL + 2, B_QRDY = B_PRDY + 2, B_OFREE = B_QRDY + 1, B_HAND = B_OFREE + 1, B_EXPO = B_HAND + 8, B_SREAD = B_EXPO + 4, B_COUNT = B_SREAD + 2 };
 
-__device__ __forceinline__ float pow2(int n) { return __uint_as_float((uint32_t)(127 + n) << 23); }   // -126 <= n <= 127
 // x 2^n for n beyond one exponent's range
 __device__ __forceinline__ float scaled(float x, int n) { const int h = n >> 1; return x * pow2(h) * pow2(n - h); }
 __device__ __forceinline__ uint32_t dup(float x) { __half2 h = __float2half2_rn(x); return *reinterpret_cast<uint32_t *>(&h); }
@@ -371,8 +370,10 @@ __global__ void __launch_bounds__(THREADS, 1) attention_kv4_tc_kernel(const Attn
       if (piece > 0) {
         // the copies of a column meet.  Each group brings half of the dimensions, 16 at a time
         const float m_ref = last.x, e0 = last.y;
-        const float l = x0.y * (x0.x == -INFINITY ? 0.f : ptx::ex2(x0.x - m_ref)) + x1.y * (x1.x == -INFINITY ? 0.f : ptx::ex2(x1.x - m_ref));
-        ml[g][row] = make_float2(m_ref, l);
+        // without a reference: no keys, or NaN alone
+        auto against = [&](float2 x) { return x.x == -INFINITY ? 0.f * x.y : ex2_scaled(x.y, x.x - m_ref); };
+        const Normal own = normalised(against(x0) + against(x1), m_ref, (int)fmaxf(e0, -100.f) + 5);   // values in the unit 2^(E0 + 5)
+        ml[g][row] = make_float2(own.ref, own.x);
         ok = ok && ptx::mbar_wait_warp(bar(B_VFREE + ((tile - 1) & 1u)), ((tile - 1) >> 1) & 1u);
         output_sync(g);
         float m = -INFINITY, sum = 0.f;
@@ -384,10 +385,8 @@ __global__ void __launch_bounds__(THREADS, 1) attention_kv4_tc_kernel(const Attn
           sum = fmaf(x.y, x.x == -INFINITY ? 0.f : ptx::ex2(x.x - m), sum);
         }
         const bool whole = old.t0 == 0 && old.t1 == old.nt;
-        // the lane's own factor: to the common reference, to the values' unit 2^(E0 + 5), and the quotient where the item is whole
-        const float own_f = (m_ref == -INFINITY ? 0.f : ptx::ex2(m_ref - m)) * (whole ? 1.f / sum : 1.f);
-        const int unit = (int)fmaxf(e0, -200.f) + 5, unit_a = unit >> 1;
-        const float f_a = own_f * pow2(unit_a), f_b = pow2(unit - unit_a);
+        // the lane's own factor: to the common reference, and the quotient where the item is whole
+        const float f_a = (own.ref == -INFINITY ? 0.f : ptx::ex2(own.ref - m)) * (whole ? 1.f / sum : 1.f) * own.up_a, f_b = own.up_b;
         float *part = p.part + (int64_t)(2 * blockIdx.x + (old.t0 == 0 ? 1 : 0)) * part_floats(CHUNK, DH);
         if (g == 0 && row < old.cols) {                  // of the first copy
           const int c = old.c0 + row, rr = c / ln.group;
@@ -495,21 +494,21 @@ __global__ void __launch_bounds__(THREADS, 1) attention_kv4_tc_kernel(const Attn
           const float2 x = hand[g ^ 1][row];
           m_was = x.x; e_was = x.y;
         }
-        const float e0 = e_top > e_was ? e_top + 2.f : e_was;
+        const float e0 = e_top > e_was ? e_top + 2.f : e_was, d = e_was == NONE ? 0.f : e0 - e_was, m_low = m_was - d;
         float rise = -INFINITY, o[NG];
 #pragma unroll
-        for (int i = 0; i < NG; ++i) {               // keys whose values are all 0 have no exponent: they count as E0
-          o[i] = ev[i] == NONE ? 0.f : fmaxf(ev[i] - e0, -120.f);
+        for (int i = 0; i < NG; ++i) {               // keys whose values are all 0 have no exponent
+          o[i] = ev[i] == NONE ? FLOOR : fmaxf(ev[i] - e0, FLOOR);
           rise = fmaxf(rise, top[i] + o[i]);
         }
         // a copy whose keys all lie behind the end keeps an open reference
         const bool open = m_was == -INFINITY;
-        const float m_ref = open || rise - m_was > LAZY ? rise : m_was;
+        const float m_ref = open || rise - m_low > LAZY ? rise : m_low;
         hand[g][row] = make_float2(m_ref, e0);
         __syncwarp();
         if (lane == 0) ptx::mbar_arrive(mine);
-        const bool moved = t > w.t0 && (m_ref != m_was || e0 != e_was);
-        if (m_own != m_ref) l *= m_own == -INFINITY ? 0.f : ptx::ex2(m_own - m_ref);
+        const bool moved = t > w.t0 && m_was - m_ref != d;     // NaN where both are open; not m_low: beyond 2^24 it is no exact difference
+        if (m_own != m_ref) l = m_own == -INFINITY ? 0.f * l : ex2_scaled(l, m_own - m_ref);
         m_own = m_ref;
         const float m_use = m_ref == -INFINITY ? 0.f : m_ref;
         // probabilities, the second half first
@@ -529,7 +528,7 @@ __global__ void __launch_bounds__(THREADS, 1) attention_kv4_tc_kernel(const Attn
               sum[(j >> 1) & 1] += p0 + p1;
               s[16 * i + (j >> 1)] = pair(p0, p1);
             }
-            l = fmaf(sum[0] + sum[1], ptx::ex2(-o[from / 32 + i]), l);
+            l = fmaf(sum[0] + sum[1], ptx::ex2(-o[from / 32 + i] - LOG_L), l);
           }
           if (from == KEYS - HALF && t > w.t0) {     // once the product of the tile before is complete
             ok = ptx::mbar_wait_warp(bar(B_VFREE + (b ^ 1u)), ((tile - 1) >> 1) & 1u);
@@ -539,7 +538,7 @@ __global__ void __launch_bounds__(THREADS, 1) attention_kv4_tc_kernel(const Attn
         }
         if (!ok) break;
         if (__any_sync(0xffffffffu, moved)) {
-          const float fac = open ? 0.f : ptx::ex2(m_was - m_ref + fmaxf(e_was - e0, -126.f));
+          const float fac = open ? 0.f : ptx::ex2(m_was - m_ref - d);
 #pragma unroll
           for (int i = 0; i < DH; i += 32) {
             uint32_t v[32];
