@@ -344,7 +344,7 @@ def test_scores_beyond_24_bits_beside_growing_values(rows):
 
 @pytest.mark.parametrize("dh", [64, 128])
 @pytest.mark.parametrize("scale", [0.0, -0.1, 3.0])
-@pytest.mark.parametrize("rows", [2, 12, 20])
+@pytest.mark.parametrize("rows", [2, 12, 20, 40, 130])
 def test_any_scale_and_ragged_last_tiles(rows, scale, dh):
     b = _b()
     c = b.KvCache4(2, 1, dh, 300)
