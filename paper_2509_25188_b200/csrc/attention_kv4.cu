@@ -358,6 +358,7 @@ __global__ void __launch_bounds__(WARPS * 32, AttnShape<DH, NT>::CTAS) attention
             }
         }
       }
+      ptx::fence_proxy_async();                    // the next copy overwrites what was read: no read is put off behind it
       __syncwarp();
       request(i + STAGES);
     }
@@ -674,6 +675,7 @@ __global__ void __launch_bounds__(WARPS * 32, 4) kv4_weights_kernel(const WeighP
           const uint32_t m = *reinterpret_cast<const uint32_t *>(tile + kv4_off_kmeta(DH) + 4 * (g + 8 * e));
           ks[e] = kv4_scale(m) * K_UNIT; km[e] = kv4_min(m) * K_UNIT;
         }
+        ptx::fence_proxy_async();                  // the next copy overwrites what was read: no read is put off behind it
         __syncwarp();
         request(i + STAGES);
         uint32_t x[4][4 * W];

@@ -270,6 +270,9 @@ __global__ void __launch_bounds__(THREADS, 1) attention_kv4_tc_kernel(const Attn
         // V: |value| < 2^e, as fp16 times 2^-(e + 5); K: s < 2^e, times 2^-(e + 9)
         const int down = -(e + (is_v ? 5 : 9));
         const float s1 = scaled(s, down), m1 = scaled(m, down), o = is_v ? m1 : -8.f * s1, a = m1 + 8.f * s1;
+        // the next copy overwrites what was read: reads come before it only by a fence between the two ways to shared memory (without one
+        // the compiler may put them off to where the values are used, behind the wait below)
+        ptx::fence_proxy_async();
         __syncwarp();
         if (lane == 0) {
           ptx::mbar_arrive(bar(B_EMPTY + slot));

@@ -526,6 +526,25 @@ def test_calls_at_once_on_two_streams():
         assert torch.equal(x.data, c.data)
 
 
+@pytest.mark.parametrize("rows,heads,dh", [(130, 32, 128), (130, 32, 64), (128, 8, 128), (64, 32, 128), (40, 32, 128), (32, 32, 128), (9, 32, 64), (1, 32, 128)])
+def test_many_calls_give_the_same_bits(rows, heads, dh):
+    """Every CTA goes through several pieces and tiles, whose buffers follow one another as fast as they can: 200 calls, all heads alike."""
+    b = _b()
+    B, n = 8, 1010
+    c = b.KvCache4(B, heads, dh, n)
+    alike = lambda x: x[None, :, None].expand(B, -1, heads, -1).contiguous()
+    c.store(alike(_rand(121, n, dh)), alike(_rand(122, n, dh)))
+    q, lens = alike(_rand(123, rows, dh)), _i32([n] * B)
+    w = torch.zeros(B, heads, n, device=DEV)
+    out, lse = c.attention(q, lens, n)
+    once = c.attention_weights(q, lse, lens, n, w, out=torch.empty_like(w))
+    differ = torch.zeros(3, dtype=torch.int64, device=DEV)
+    for _ in range(200):
+        o, l = c.attention(q, lens, n)
+        differ += torch.stack([(o != out).sum(), (l != lse).sum(), (c.attention_weights(q, lse, lens, n, w, out=torch.empty_like(w)) != once).sum()])
+    assert differ.tolist() == [0, 0, 0]
+
+
 def test_batches_without_rows():
     b = _b()
     c = b.KvCache4(2, 2, 64, 50)
