@@ -9,12 +9,13 @@ namespace kv4 {
 constexpr float LAZY = 6.0f;         // log2 units the running maximum may pass the reference
 
 // ---- one unit for values of any size -----------------------------------------------------------------------------------
-// A key's probability goes to the product as p' = 2^(t - M), t = log2 w + b: w its weight, b = (the exponent of its values) - E, E one that
-// no value has passed so far.  Two sums then stand for the output: O = sum p' v 2^-(E + b) = sum w v 2^(-E - M), and l = sum p' 2^-b = sum w 2^-M.
+// A key's probability goes to the product as p' = 2^(log2 w - M + b), w its weight, b = the exponent of its values - E, E one that no value
+// has passed so far.  Two sums then stand for the output: O = sum p' v 2^-(E + b) = sum w v 2^(-E - M), and l = sum p' 2^-b = sum w 2^-M.
 // Where E rises by d, M is lowered by d: what is in O stays, the keys to come keep their bits whatever the size of the row that raised E
-// (which may have no weight at all), and l alone grows by 2^d.  l lies between 1 and 2^227 times the keys, and is kept as l 2^-LOG_L.
-// FLOOR: the least b, so that p' is no zero where w counts; values 2^100 below the largest seen so far lose their size, rows of zeros take it.
-constexpr int LOG_L = 120;
+// (which may have no weight at all), and l alone grows by 2^d.  l is at least 1, and as large as the values that have the weight are
+// smaller than E: it is kept as l 2^-LOG_L, which bears 2^180.  FLOOR: the least b, so that p' is no zero where w counts; values 2^100
+// below the largest so far lose their size, rows of zeros take it.
+constexpr int LOG_L = 80;
 constexpr float FLOOR = -100.f;
 
 __device__ __forceinline__ float pow2(int n) { return __uint_as_float((uint32_t)(127 + n) << 23); }   // -126 <= n <= 127

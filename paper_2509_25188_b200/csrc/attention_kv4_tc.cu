@@ -6,13 +6,15 @@
 //     K: (c - 8) s 2^-E    exact: c - 8 has three significant bits (or is 8), s has eight.  The rest of the value, a = m + 8 s,
 //        reaches the scores through sixteen further products of depth, (a_hi, a_hi, a_lo) against (sum q_hi, sum q_lo, sum q_hi):
 //        no number of a key's own is left for the softmax
-//     V: c s 2^-E + m 2^-E in one fused operation, rounded once (2^-11 relative)
-// E belongs to 32 keys (a warp).  A code reaches fp16 as it lies, as the subnormal c 2^-24 (or 16 c 2^-24 from bits 4..7), and the
-// multiplication by s 2^24 (2^20) lifts it.  Eight codes of a word come out in the order 0 4 1 5 2 6 3 7: queries are written in
-// that order, and outputs read in it.
+//     V: c s 2^-E + m 2^-E in one fused operation, rounded once (2^-12 relative, or 2^-20 of 2^E)
+// E belongs to 32 keys (a warp), unless one of them is 2^8 and more below the largest: then each has its own, and the softmax takes the
+// tile key by key (below), so that a key's bits do not hang on its neighbours' size.  A code reaches fp16 as it lies, as the subnormal
+// c 2^-24 (or 16 c 2^-24 from bits 4..7), and the multiplication by s 2^24 (2^20) lifts it.  Eight codes of a word come out in the order
+// 0 4 1 5 2 6 3 7: queries are written in that order, and outputs read in it.
 // Two groups of four softmax warps take the tiles alternately, a thread a lane: t = cf 2^E acc + (E_V - E0) - M, P = 2^t as fp16,
 // the A operand of the second product.  M is a reference that follows the running maximum lazily, E0 above the largest E_V so far
-// (attention_kv4.cuh has what becomes of M and the sums where it rises); O is rescaled when M moves against the scores.  The thread that has fixed them for a tile hands them to the other group's thread of its lane before its
+// (attention_kv4.cuh has what becomes of M and the sums where it rises); O is rescaled when M moves against the scores.  The thread that has
+// fixed them for a tile hands them to the other group's thread of its lane before its
 // exponentials.  128 keys of a lane are read twice, 64 at a time (registers): the maximum first, then the second half, at hand
 // still, then the first.  From that last read on S belongs to the tile after next, whose product runs under the exponentials (P
 // over S instead: 64 numbers a head 14 % slower, 128 numbers 1 % faster).
@@ -44,6 +46,7 @@ namespace {
 constexpr int RING = 3, NB = 2;                    // tiles of codes on their way; operand buffers
 constexpr uint32_t ATOM = TC_TILE * 128;           // 128 rows x 64 fp16
 constexpr float NONE = -1000.f;                    // no exponent
+constexpr int SPREAD = 8;                          // 2^8 below the largest of 32, (c - 8) s is still exact and values are within 2^-11 of their row's largest
 constexpr int LDS_O = 20;                          // floats of a staged row of 16
 constexpr int THREADS = 640;
 constexpr int REGS_SOFTMAX = 120, REGS_CODES = 88, REGS_LEAN = 56;   // 256 x 120 + 256 x 88 + 128 x 56 of 640 x 96
@@ -67,6 +70,7 @@ __device__ __forceinline__ uint32_t hfma2(uint32_t a, uint32_t b, uint32_t c) {
   asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(d) : "r"(a), "r"(b), "r"(c));
   return d;
 }
+__device__ __forceinline__ float key_factor(float cf, float expo_k) { return fmaxf(cf * expo_k * 4294967296.f, 1.2e-38f); }   // never 0: -inf times it stays -inf
 __device__ __forceinline__ void softmax_sync() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
 __device__ __forceinline__ void output_sync(int g) { asm volatile("bar.sync %0, 128;" ::"r"(2 + g) : "memory"); }   // one group
 // A row of codes, its quarters in an order that differs from row to row: eight lanes touch all banks, reading and writing.
@@ -93,16 +97,25 @@ template <int DH> struct Row {
   }
 };
 
+// Exponents of a tile, by group of 32 keys; those of V are told ahead of the operands, those of K come with the scores
+struct Exponents {
+  float k[4], v[4];                                // negative, and larger by APART: the group's keys have exponents of their own,
+  int16_t below_k[TC_TILE], below_v[TC_TILE];      // that lie below it by this
+};
+constexpr int APART = 1024;
+
 template <int DH, int COPIES>
 __global__ void __launch_bounds__(THREADS, 1) attention_kv4_tc_kernel(const AttnParams p) {
   using T = Tc<DH>;
   constexpr int CHUNK = 128 / COPIES, KEYS = TC_TILE / COPIES;   // columns; keys of a tile that a copy takes
+  // Halves of a copy's keys whose exponentials are written out: the code of the tile loop is fetched again and again by eight warps at
+  // different places in it (128 columns, 65000 keys, us, one / two: heads of 64 154 / 157, of 128 189 / 185)
+  constexpr int TURNS = DH == 64 ? 1 : 2;
   extern __shared__ uint8_t smem_raw[];
   __shared__ __align__(8) uint64_t bars[B_COUNT];
   __shared__ uint32_t tmem_slot;
   __shared__ int abort_flag;
-  // [tile % 4][group of 32 keys]: exponents.  Those of V are told ahead of the operands, those of K come with the scores
-  __shared__ float expo_k[4][4], expo_v[4][4];
+  __shared__ __align__(16) Exponents expo[4];      // of tile % 4
   __shared__ int lost;                             // a softmax warp's wait ran out
   __shared__ float2 hand[2][128];                  // [group][lane]: reference and E0 of the group's last tile
   __shared__ float2 sums[2][128];                  // [group][lane]: the reference its sum is against, the sum
@@ -265,21 +278,32 @@ __global__ void __launch_bounds__(THREADS, 1) attention_kv4_tc_kernel(const Attn
         // the group's exponent; keys that are not finite stay outside it
         const int es = (int)((meta >> 7) & 255u), em = (int)((meta >> 23) & 255u);
         int e = es == 255 || em == 255 ? 0 : is_v ? max(es + 4, em) : max(es, em - 11);
-        const bool none = is_v && __all_sync(0xffffffffu, (meta & 0x7fff7fffu) == 0u);   // values that are all 0 have no exponent
-        e = max((int)__reduce_max_sync(0xffffffffu, (uint32_t)max(e, 0)) - 126, -100) + (is_v ? 1 : 0);
+        const bool zero = (meta & 0x7fff7fffu) == 0u, none = is_v && __all_sync(0xffffffffu, zero);   // values that are all 0 have no exponent
+        const bool real = !zero && es != 255 && em != 255;
+        e = max(e, 0);
+        const int most = max((int)__reduce_max_sync(0xffffffffu, (uint32_t)e), 26), least = max((int)__reduce_min_sync(0xffffffffu, real ? (uint32_t)e : 255u), 26);
+        const int group_e = most - 126 + (is_v ? 1 : 0);
         // V: |value| < 2^e, as fp16 times 2^-(e + 5); K: s < 2^e, times 2^-(e + 9)
-        const int down = -(e + (is_v ? 5 : 9));
-        const float s1 = scaled(s, down), m1 = scaled(m, down), o = is_v ? m1 : -8.f * s1, a = m1 + 8.f * s1;
+        const int down = -(group_e + (is_v ? 5 : 9));
+        float s1 = scaled(s, down), m1 = scaled(m, down);
+        int below_k = 0;
+        const bool apart = most - least > SPREAD;
+        if (apart) {
+          // rows further below the group's largest than fp16 bears keep exponents of their own; rows of zeros go with the smallest
+          const int below = real ? max(e, 26) - most : zero ? least - most : 0;
+          if (is_v) expo[tile & 3u].below_v[r] = (int16_t)below;
+          else below_k = below;
+          s1 = scaled(s, down - below); m1 = scaled(m, down - below);
+        }
+        if (is_v && lane == 0) expo[tile & 3u].v[grp] = none ? NONE : (float)(apart ? group_e + APART : group_e);
+        const float o = is_v ? m1 : -8.f * s1, a = m1 + 8.f * s1;
         // the next copy overwrites what was read: reads come before it only by a fence between the two ways to shared memory (without one
         // the compiler may put them off to where the values are used, behind the wait below)
         ptx::fence_proxy_async();
         __syncwarp();
         if (lane == 0) {
           ptx::mbar_arrive(bar(B_EMPTY + slot));
-          if (is_v) {
-            expo_v[tile & 3u][grp] = none ? NONE : (float)e;
-            ptx::mbar_arrive(bar(B_EXPO + (tile & 3u)));
-          }
+          if (is_v) ptx::mbar_arrive(bar(B_EXPO + (tile & 3u)));
         }
         ok = ptx::mbar_wait_warp(bar((is_v ? B_VFREE : B_KFREE) + b), ((tile >> 1) & 1u) ^ 1u);
         if (!ok) break;
@@ -290,7 +314,8 @@ __global__ void __launch_bounds__(THREADS, 1) attention_kv4_tc_kernel(const Attn
           ptx::st_shared_v4(at, make_uint4(pair(hi, hi), pair((a - hi) * 2048.f, 0.f), 0u, 0u));
           ptx::st_shared_v4(at ^ 16u, make_uint4(0u, 0u, 0u, 0u));
         }
-        if (!is_v && lane == 0) expo_k[tile & 3u][grp] = pow2(e + 9 - 32);   // e reaches 128
+        if (!is_v && apart) expo[tile & 3u].below_k[r] = (int16_t)below_k;
+        if (!is_v && lane == 0) expo[tile & 3u].k[grp] = apart ? -pow2(group_e + 9 - 32) : pow2(group_e + 9 - 32);   // group_e reaches 128
         ptx::fence_proxy_async();
         __syncwarp();
         if (lane == 0) ptx::mbar_arrive(bar((is_v ? B_VRDY : B_KRDY) + b));
@@ -363,7 +388,7 @@ __global__ void __launch_bounds__(THREADS, 1) attention_kv4_tc_kernel(const Attn
     };
     // Queries of a piece, then the output of the one before, then the piece's tiles
     Piece w = {}, old = {};
-    float2 last = {}, x0 = {}, x1 = {};              // of the piece before: reference and E0, the groups' sums
+    float2 last = {}, x0 = {}, x1 = {};              // of the piece before: reference, the groups' sums
     for (uint32_t pos = begin; begin < end; ++piece) {
       const bool more = pos < end;
       if (more) {
@@ -372,10 +397,10 @@ __global__ void __launch_bounds__(THREADS, 1) attention_kv4_tc_kernel(const Attn
       }
       if (piece > 0) {
         // the copies of a column meet.  Each group brings half of the dimensions, 16 at a time
-        const float m_ref = last.x, e0 = last.y;
+        const float m_ref = last.x;
         // without a reference: no keys, or NaN alone
         auto against = [&](float2 x) { return x.x == -INFINITY ? 0.f * x.y : ex2_scaled(x.y, x.x - m_ref); };
-        const Normal own = normalised(against(x0) + against(x1), m_ref, (int)fmaxf(e0, -100.f) + 5);   // values in the unit 2^(E0 + 5)
+        const Normal own = normalised(against(x0) + against(x1), m_ref, (int)fmaxf(last.y, -100.f) + 5);   // values in the unit 2^(E0 + 5)
         ml[g][row] = make_float2(own.ref, own.x);
         ok = ok && ptx::mbar_wait_warp(bar(B_VFREE + ((tile - 1) & 1u)), ((tile - 1) >> 1) & 1u);
         output_sync(g);
@@ -453,12 +478,14 @@ __global__ void __launch_bounds__(THREADS, 1) attention_kv4_tc_kernel(const Attn
         ptx::tc_fence_after_sync();
         if (m_own == -INFINITY) cf = q_factor[piece & 1u][row];
         const uint32_t tSr = tS + lane_base + b * TC_TILE, tSk = tSr + copy * KEYS;
-        float k[NG], ev[NG], e_top = NONE;
+        const Exponents &ex = expo[tile & 3u];
+        float k[NG], ev[NG], e_top = NONE, k_least = 0.f;
 #pragma unroll
         for (int i = 0; i < NG; ++i) {
-          ev[i] = expo_v[tile & 3u][copy * NG + i];
-          k[i] = fmaxf(cf * expo_k[tile & 3u][copy * NG + i] * 4294967296.f, 1.2e-38f);   // never 0: -inf times it stays -inf
+          ev[i] = ex.v[copy * NG + i];
+          k[i] = key_factor(cf, ex.k[copy * NG + i]);
           e_top = fmaxf(e_top, ev[i]);
+          k_least = fminf(k_least, ex.k[copy * NG + i]);
         }
         const int left = w.keys - t * TC_TILE - copy * KEYS;
         uint32_t s[HALF];
@@ -466,83 +493,148 @@ __global__ void __launch_bounds__(THREADS, 1) attention_kv4_tc_kernel(const Attn
 #pragma unroll
           for (int i = 0; i < HALF; i += 32) ptx::tmem_ld_x32(tSk + from + i, s + i);
           ptx::tmem_ld_wait();
-          if (left - from < HALF) {
-#pragma unroll
-            for (int j = 0; j < HALF; ++j) if (j >= left - from) s[j] = 0xff800000u;
-          }
         };
+        // Scores behind the end.  In tensor memory and 16 at a time, as all that is rare here: the code of the tile loop is read again and again
+        // by eight warps at different places, and each KB of it beside the exponentials costs every tile
+        if (left < KEYS) {
+#pragma unroll 1
+          for (int c = max(left, 0) & ~15; c < KEYS; c += 16) {
+            uint32_t x[16];
+            ptx::tmem_ld_x16(tSk + c, x);
+            ptx::tmem_ld_wait();
+#pragma unroll
+            for (int j = 0; j < 16; ++j) if (c + j >= left) x[j] = 0xff800000u;
+            ptx::tmem_st_x16(tSk + c, x);
+          }
+          ptx::tmem_st_wait();
+        }
         auto release = [&]() {                       // these scores were read for the last time
           ptx::tc_fence_before_sync();
           __syncwarp();
           if (lane == 0) ptx::mbar_arrive(bar(B_SREAD + b));
         };
         float top[NG];                               // largest scores of the groups
-#pragma unroll
+#pragma unroll 1
         for (int from = 0; from < KEYS; from += HALF) {
           load(from);
-          if (KEYS == HALF) release();
 #pragma unroll
           for (int i = 0; i < HG; ++i) {
             float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
             for (int j = 0; j < 32; ++j) mx[j & 3] = fmaxf(mx[j & 3], __uint_as_float(s[32 * i + j]));
-            top[from / 32 + i] = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * k[from / 32 + i];
+            top[NG - HG + i] = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
+            if (KEYS > HALF && from == 0) top[i] = top[NG - HG + i];
           }
         }
-        // reference and E0: those of the tile before, moved where need be
-        float m_was = -INFINITY, e_was = NONE;
-        if (t > w.t0) {
+#pragma unroll
+        for (int i = 0; i < NG; ++i) top[i] *= k[i];
+        const bool by_key = __any_sync(0xffffffffu, k_least < 0.f || e_top > APART / 2);
+        float m_was = -INFINITY, e_was = NONE;       // the reference of the tile before
+        auto received = [&]() {
+          if (t == w.t0) return;
           ok = ptx::mbar_wait_warp(theirs, ((tile - 1) >> 1) & 1u);
-          if (!ok) break;
           const float2 x = hand[g ^ 1][row];
           m_was = x.x; e_was = x.y;
-        }
-        const float e0 = e_top > e_was ? e_top + 2.f : e_was, d = e_was == NONE ? 0.f : e0 - e_was, m_low = m_was - d;
-        float rise = -INFINITY, o[NG];
+        };
+        auto hand_over = [&](float m, float e) {
+          hand[g][row] = make_float2(m, e);
+          __syncwarp();
+          if (lane == 0) ptx::mbar_arrive(mine);
+          if (m_own != m) l = m_own == -INFINITY ? 0.f * l : ex2_scaled(l, m_own - m);
+          m_own = m;
+        };
+        auto product_done = [&]() {                  // that of the tile before: its probabilities may be written over
+          if (t == w.t0) return;
+          ok = ptx::mbar_wait_warp(bar(B_VFREE + (b ^ 1u)), ((tile - 1) >> 1) & 1u);
+          ptx::tc_fence_after_sync();
+        };
+        bool moved;
+        float fac;                                   // of O
+        if (!by_key) {
+          if (KEYS == HALF) release();
+          received();
+          if (!ok) break;
+          // E0 rises to a new largest exponent, M falls with it and moves where need be
+          const float e0 = e_top > e_was ? e_top + 2.f : e_was, d = e_was == NONE ? 0.f : e0 - e_was, m_low = m_was - d;
+          float rise = -INFINITY, o[NG];
 #pragma unroll
-        for (int i = 0; i < NG; ++i) {               // keys whose values are all 0 have no exponent
-          o[i] = ev[i] == NONE ? FLOOR : fmaxf(ev[i] - e0, FLOOR);
-          rise = fmaxf(rise, top[i] + o[i]);
-        }
-        // a copy whose keys all lie behind the end keeps an open reference
-        const bool open = m_was == -INFINITY;
-        const float m_ref = open || rise - m_low > LAZY ? rise : m_low;
-        hand[g][row] = make_float2(m_ref, e0);
-        __syncwarp();
-        if (lane == 0) ptx::mbar_arrive(mine);
-        const bool moved = t > w.t0 && m_was - m_ref != d;     // NaN where both are open; not m_low: beyond 2^24 it is no exact difference
-        if (m_own != m_ref) l = m_own == -INFINITY ? 0.f * l : ex2_scaled(l, m_own - m_ref);
-        m_own = m_ref;
-        const float m_use = m_ref == -INFINITY ? 0.f : m_ref;
-        // probabilities, the second half first
-#pragma unroll
-        for (int from = KEYS - HALF; from >= 0; from -= HALF) {
-          if (from != KEYS - HALF) {
-            load(from);
-            release();
+          for (int i = 0; i < NG; ++i) {             // keys whose values are all 0 have no exponent
+            o[i] = ev[i] == NONE ? FLOOR : fmaxf(ev[i] - e0, FLOOR);
+            rise = fmaxf(rise, top[i] + o[i]);
           }
-#pragma unroll
-          for (int i = 0; i < HG; ++i) {
-            const float kk = k[from / 32 + i], oo = o[from / 32 + i] - m_use;
-            float sum[2] = {0.f, 0.f};
-#pragma unroll
-            for (int j = 0; j < 32; j += 2) {
-              const float p0 = ptx::ex2(fmaf(__uint_as_float(s[32 * i + j]), kk, oo)), p1 = ptx::ex2(fmaf(__uint_as_float(s[32 * i + j + 1]), kk, oo));
-              sum[(j >> 1) & 1] += p0 + p1;
-              s[16 * i + (j >> 1)] = pair(p0, p1);
+          // a copy whose keys all lie behind the end keeps an open reference
+          const bool open = m_was == -INFINITY;
+          const float m_ref = open || rise - m_low > LAZY ? rise : m_low;
+          hand_over(m_ref, e0);
+          moved = t > w.t0 && m_was - m_ref != d;    // NaN where both are open; not m_low: beyond 2^24 it is no exact difference
+          fac = open ? 0.f : ptx::ex2(m_was - m_ref - d);
+          const float m_use = m_ref == -INFINITY ? 0.f : m_ref;
+          // probabilities, the second half first
+#pragma unroll TURNS
+          for (int from = KEYS - HALF; from >= 0; from -= HALF) {
+            if (from != KEYS - HALF) {
+              load(from);
+              release();
             }
-            l = fmaf(sum[0] + sum[1], ptx::ex2(-o[from / 32 + i] - LOG_L), l);
+#pragma unroll
+            for (int i = 0; i < HG; ++i) {
+              const float kk = from ? k[NG - HG + i] : k[i], oi = from ? o[NG - HG + i] : o[i], oo = oi - m_use;
+              float sum[2] = {0.f, 0.f};
+#pragma unroll
+              for (int j = 0; j < 32; j += 2) {
+                const float p0 = ptx::ex2(fmaf(__uint_as_float(s[32 * i + j]), kk, oo)), p1 = ptx::ex2(fmaf(__uint_as_float(s[32 * i + j + 1]), kk, oo));
+                sum[(j >> 1) & 1] += p0 + p1;
+                s[16 * i + (j >> 1)] = pair(p0, p1);
+              }
+              l = fmaf(sum[0] + sum[1], ptx::ex2(-oi - LOG_L), l);
+            }
+            if (from == KEYS - HALF) product_done();
+            ptx::tmem_st_x32(tPr + (copy * KEYS + from) / 2, s);
           }
-          if (from == KEYS - HALF && t > w.t0) {     // once the product of the tile before is complete
-            ok = ptx::mbar_wait_warp(bar(B_VFREE + (b ^ 1u)), ((tile - 1) >> 1) & 1u);
-            ptx::tc_fence_after_sync();
-          }
-          ptx::tmem_st_x32(tPr + (copy * KEYS + from) / 2, s);
+        } else {
+          // Key by key, 16 at a time, the parts of t apart.  (M, E0) become score and exponent of the key with the largest sum of both
+          float m_top = -INFINITY, e_best = NONE;
+          auto each_key = [&](auto &&use) {
+#pragma unroll 1
+            for (int c = 0; c < KEYS; c += 16) {
+              uint32_t v[16];
+              ptx::tmem_ld_x16(tSk + c, v);
+              const int grp = copy * NG + c / 32;
+              const bool own_k = ex.k[grp] < 0.f, own_v = ex.v[grp] > APART / 2;
+              const float kk = key_factor(cf, fabsf(ex.k[grp])), e = own_v ? ex.v[grp] - APART : ex.v[grp];
+              ptx::tmem_ld_wait();
+#pragma unroll
+              for (int j = 0; j < 16; ++j)
+                use(c, j, __fmul_rn(__uint_as_float(v[j]), own_k ? kk * pow2(max((int)ex.below_k[copy * KEYS + c + j], -126)) : kk),
+                    own_v ? e + (float)ex.below_v[copy * KEYS + c + j] : e);
+            }
+          };
+          each_key([&](int, int, float x, float e) {
+            if (m_top == -INFINITY || x - m_top + (e - e_best) > 0.f) { m_top = x; e_best = e; }
+          });
+          received();
+          if (!ok) break;
+          const bool open = m_was == -INFINITY, move = open || m_top - m_was + (e_best - e_was) > LAZY;
+          const float m_ref = move ? m_top : m_was, e_ref = move ? e_best : e_was, m_use = m_ref == -INFINITY ? 0.f : m_ref;
+          hand_over(m_ref, e_ref);
+          moved = t > w.t0 && move;
+          fac = open ? 0.f : ptx::ex2(m_was - m_ref + (e_was - e_ref));
+          product_done();
+          float sum = 0.f;
+          uint32_t packed[8];
+          float even = 0.f;
+          each_key([&](int c, int j, float x, float e) {
+            const float y = ptx::ex2(x - m_use + (e - e_ref));
+            sum += ptx::ex2(x - m_use - LOG_L);
+            if (j & 1) packed[j >> 1] = pair(even, y); else even = y;
+            if (j == 15) ptx::tmem_st_x8(tPr + (copy * KEYS + c) / 2, packed);
+          });
+          l += sum;
+          release();
         }
         if (!ok) break;
         if (__any_sync(0xffffffffu, moved)) {
-          const float fac = open ? 0.f : ptx::ex2(m_was - m_ref - d);
-#pragma unroll
+#pragma unroll 1
           for (int i = 0; i < DH; i += 32) {
             uint32_t v[32];
             ptx::tmem_ld_x32(tOr + i, v);
@@ -587,6 +679,7 @@ __global__ void __launch_bounds__(THREADS, 1) attention_kv4_tc_kernel(const Attn
 
 template <int DH, int COPIES> cudaError_t launch(cudaStream_t st, const AttnParams &p, int ctas) {
   constexpr int smem = Tc<DH>::BYTES + 1024;
+  static_assert(smem + 9888 <= 227 * 1024, "with what the kernel declares itself");
   static std::atomic<uint64_t> done{0};
   const cudaError_t e = allow_shared((const void *)attention_kv4_tc_kernel<DH, COPIES>, smem, done);
   if (e != cudaSuccess) return e;

@@ -303,6 +303,38 @@ def test_large_values_without_weight_leave_the_others(rows, dh, up, where):
     _check_by_key_sizes(out.transpose(1, 2).reshape(B * heads, rows, dh), lse.transpose(1, 2).reshape(B * heads, rows), q, k, v, 0.125)
 
 
+@pytest.mark.parametrize("up", [7, 8, 9, 12, 14, 20, 40, 90])
+@pytest.mark.parametrize("rows,dh", [(20, 128), (33, 128), (40, 64), (70, 64), (130, 128)])
+def test_one_large_row_beside_others(rows, dh, up):
+    """As above with one row of values in 32 larger, at other places in each 32, and rows of zeros, and values that fall off by 2^20 within 32;
+    and with one key in 32 larger."""
+    b = _b()
+    n = 700
+    c = b.KvCache4(1, 1, dh, n)
+    k, v = _rand(111, n, dh), _rand(112, n, dh)
+    q = _rand(113, rows, dh)
+    q[:, :8] = 4
+    k[:, :8] = 0.5
+    large = torch.arange(0, n, 37, device=DEV)
+    v[large] *= 2.0 ** up
+    k[large, :8] = -16
+    v[5:640:64] = 0
+    v[320:352] *= (2.0 ** -(torch.arange(32, device=DEV) * 0.7).float())[:, None].to(torch.bfloat16)
+    c.store(k[:, None], v[:, None])
+    out, lse = c.attention(q[:, None], _i32([n]), n, scale=0.125)
+    _check_by_key_sizes(out.transpose(0, 1), lse.transpose(0, 1), q, k, v, 0.125)
+    # scores are counted against each key's own size: a key without weight has no part in the others' error
+    v = _rand(114, n, dh)
+    k[large] = _rand(115, len(large), dh) * 0.01
+    k[large, :8] = -1
+    k[large] *= 2.0 ** min(up, 60)
+    c.store(k[:, None], v[:, None])
+    out, lse = c.attention(q[:, None], _i32([n]), n, scale=0.125)
+    few = torch.ones(n, dtype=torch.bool, device=DEV)
+    few[large] = False
+    _check_by_key_sizes(out.transpose(0, 1), lse.transpose(0, 1), q, k[few], v[few], 0.125)     # the large ones' scores: -512 and less
+
+
 @pytest.mark.parametrize("order", [1, -1])
 @pytest.mark.parametrize("rows,dh", [(2, 128), (12, 64), (20, 128), (40, 128), (40, 64), (130, 128)])
 def test_values_that_grow_as_their_weights_fall(rows, dh, order):
