@@ -8,7 +8,7 @@
 //        no number of a key's own is left for the softmax
 //     V: c s 2^-E + m 2^-E in one fused operation, rounded once (2^-12 relative, or 2^-20 of 2^E)
 // E belongs to 32 keys (a warp), unless one of them is 2^8 and more below the largest: then each has its own, and the softmax takes the
-// tile key by key (below), so that a key's bits do not hang on its neighbours' size.  A code reaches fp16 as it lies, as the subnormal
+// tile key by key (below; likewise where scores are millions), so that a key's bits do not hang on its neighbours' size.  A code reaches fp16 as it lies, as the subnormal
 // c 2^-24 (or 16 c 2^-24 from bits 4..7), and the multiplication by s 2^24 (2^20) lifts it.  Eight codes of a word come out in the order
 // 0 4 1 5 2 6 3 7: queries are written in that order, and outputs read in it.
 // Two groups of four softmax warps take the tiles alternately, a thread a lane: t = cf 2^E acc + (E_V - E0) - M, P = 2^t as fp16,
@@ -46,6 +46,7 @@ namespace {
 constexpr int RING = 3, NB = 2;                    // tiles of codes on their way; operand buffers
 constexpr uint32_t ATOM = TC_TILE * 128;           // 128 rows x 64 fp16
 constexpr float NONE = -1000.f;                    // no exponent
+constexpr float FAR = 1048576.f;                   // log2 scores beyond: M, which is rounded, would take the last bits of t in one step
 constexpr int SPREAD = 8;                          // 2^8 below the largest of 32, (c - 8) s is still exact and values are within 2^-11 of their row's largest
 constexpr int LDS_O = 20;                          // floats of a staged row of 16
 constexpr int THREADS = 640;
@@ -513,7 +514,7 @@ __global__ void __launch_bounds__(THREADS, 1) attention_kv4_tc_kernel(const Attn
           __syncwarp();
           if (lane == 0) ptx::mbar_arrive(bar(B_SREAD + b));
         };
-        float top[NG];                               // largest scores of the groups
+        float top[NG], hi = -INFINITY;               // largest scores of the groups, of all
 #pragma unroll 1
         for (int from = 0; from < KEYS; from += HALF) {
           load(from);
@@ -527,8 +528,11 @@ __global__ void __launch_bounds__(THREADS, 1) attention_kv4_tc_kernel(const Attn
           }
         }
 #pragma unroll
-        for (int i = 0; i < NG; ++i) top[i] *= k[i];
-        const bool by_key = __any_sync(0xffffffffu, k_least < 0.f || e_top > APART / 2);
+        for (int i = 0; i < NG; ++i) {
+          top[i] *= k[i];
+          hi = fmaxf(hi, top[i]);
+        }
+        const bool by_key = __any_sync(0xffffffffu, k_least < 0.f || e_top > APART / 2 || (fabsf(hi) > FAR && hi > -INFINITY));
         float m_was = -INFINITY, e_was = NONE;       // the reference of the tile before
         auto received = [&]() {
           if (t == w.t0) return;

@@ -374,6 +374,29 @@ def test_scores_beyond_24_bits_beside_growing_values(rows):
     assert (np.abs(_np(out.transpose(1, 2).reshape(B * heads, rows, dh)) - want) <= tol).all()
 
 
+@pytest.mark.parametrize("power", [16, 22, 40])
+@pytest.mark.parametrize("rows,dh", [(2, 128), (20, 64), (33, 128), (40, 64), (40, 128), (130, 128), (130, 64)])
+def test_scores_of_millions(rows, dh, power):
+    """Every third row of queries is 2^power larger: one key leads by far there and its value comes out as it is; other rows as ever."""
+    b = _b()
+    B, heads, n = 8, 32, 1024
+    c = b.KvCache4(B, heads, dh, n)
+    k, v = _rand(131, n, dh), _rand(132, n, dh)
+    v[512:] *= 2.0 ** 6
+    best = 700 - torch.arange(rows, device=DEV)
+    q = k[best] * 0.125
+    q[::3] *= 2.0 ** power
+    alike = lambda x: x[None, :, None].expand(B, -1, heads, -1).contiguous()
+    c.store(alike(k), alike(v))
+    out, lse = c.attention(alike(q), _i32([n] * B), n, scale=1.0)
+    out, lse = out.transpose(1, 2).reshape(B * heads, rows, dh), lse.transpose(1, 2).reshape(B * heads, rows)
+    want = plain.values(_np(v[best[::3]]))
+    tol = 2.0 ** -8 * np.abs(want) + 2.0 ** -10 * np.abs(want).max(-1, keepdims=True)
+    assert (np.abs(_np(out[:, ::3]) - want) <= tol).all()
+    others = torch.arange(rows, device=DEV) % 3 != 0
+    _check_by_key_sizes(out[:, others], lse[:, others], q[others], k, v, 1.0)
+
+
 @pytest.mark.parametrize("dh", [64, 128])
 @pytest.mark.parametrize("scale", [0.0, -0.1, 3.0])
 @pytest.mark.parametrize("rows", [2, 12, 20, 40, 130])
