@@ -6,8 +6,8 @@
 // product as they lie, by a mask (those in bits 4..7 as 16 c 2^-24, against queries divided by 16).  With q' = q scaled by a power
 // of two of its own into fp16's range (8 significant bits of 11), and cf what undoes it:
 //     t_j = log2 of exp(scale q . k_j) + e_j - E = cf (s_j sum(c q') + m_j sum(q')) + e_j - E
-// 2^e_j bounds the value row's s_j and |m_j| / 16, E is above all e_j so far.  Probabilities are taken as p'_j = 2^(t_j - M), M a reference at
-// most 2^6 below the running maximum of t, so that p'_j s_j 2^-e_j, what multiplies the codes of V, stays within fp16 whatever the
+// 2^e_j bounds the value row's s_j and |m_j| / 16, E is above all e_j so far.  Probabilities are taken as p'_j = 2^(t_j - M), M a reference
+// 2^9 to 2^15 below the running maximum of t, so that p'_j s_j 2^-e_j, what multiplies the codes of V, stays within fp16 whatever the
 // values' magnitude (attention_kv4.cuh has what becomes of M and the sums where E rises).  Rounding it to fp16 is the only step to less than 32 bits between the queries and the output.
 //
 // Work: the key tiles of all (sequence, head, chunk of columns) stand in one line and every CTA takes an equal run of it; a run
@@ -301,7 +301,8 @@ __global__ void __launch_bounds__(WARPS * 32, AttnShape<DH, NT>::CTAS) attention
               xa = fmaxf(xa, __shfl_xor_sync(0xffffffffu, xa, x));
               xb = fmaxf(xb, __shfl_xor_sync(0xffffffffu, xb, x));
             }
-            const float da = first ? (xa == -INFINITY ? 0.f : xa) : fmaxf(xa, 0.f), db = first ? (xb == -INFINITY ? 0.f : xb) : fmaxf(xb, 0.f);
+            const float least = first ? -3e38f : 0.f;        // afterwards references rise only
+            const float da = xa == -INFINITY ? 0.f : fmaxf(xa - BELOW, least), db = xb == -INFINITY ? 0.f : fmaxf(xb - BELOW, least);
             const float sa = first ? 0.f : ptx::ex2(-da), sb = first ? 0.f : ptx::ex2(-db);
             const F2 d = ptx::f2(-da, -db), sc = ptx::f2(sa, sb);
             neg_m[n] = ptx::add2(neg_m[n], d);

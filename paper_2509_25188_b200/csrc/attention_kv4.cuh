@@ -6,7 +6,9 @@
 namespace l2pd {
 namespace kv4 {
 
-constexpr float LAZY = 6.0f;         // log2 units the running maximum may pass the reference
+// Log2 units by which a reference is set below the largest, and by which the largest may pass it before it is moved.  A probability is below
+// 2^15 then, within fp16, and vanishes 2^34 below the largest (without the first, a million keys 2^25 below one would, with 3 % of the output).
+constexpr float BELOW = 9.0f, LAZY = 15.0f;
 
 // ---- one unit for values of any size -----------------------------------------------------------------------------------
 // A key's probability goes to the product as p' = 2^(log2 w - M + b), w its weight, b = the exponent of its values - E, E one that no value

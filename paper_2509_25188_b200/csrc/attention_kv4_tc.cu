@@ -568,7 +568,7 @@ __global__ void __launch_bounds__(THREADS, 1) attention_kv4_tc_kernel(const Attn
           }
           // a copy whose keys all lie behind the end keeps an open reference
           const bool open = m_was == -INFINITY;
-          const float m_ref = open || rise - m_low > LAZY ? rise : m_low;
+          const float m_ref = open || rise - m_low > LAZY ? rise - BELOW : m_low;
           hand_over(m_ref, e0);
           moved = t > w.t0 && m_was - m_ref != d;    // NaN where both are open; not m_low: beyond 2^24 it is no exact difference
           fac = open ? 0.f : ptx::ex2(m_was - m_ref - d);
@@ -619,7 +619,7 @@ __global__ void __launch_bounds__(THREADS, 1) attention_kv4_tc_kernel(const Attn
           received();
           if (!ok) break;
           const bool open = m_was == -INFINITY, move = open || m_top - m_was + (e_best - e_was) > LAZY;
-          const float m_ref = move ? m_top : m_was, e_ref = move ? e_best : e_was, m_use = m_ref == -INFINITY ? 0.f : m_ref;
+          const float m_ref = move ? m_top - BELOW : m_was, e_ref = move ? e_best : e_was, m_use = m_ref == -INFINITY ? 0.f : m_ref;
           hand_over(m_ref, e_ref);
           moved = t > w.t0 && move;
           fac = open ? 0.f : ptx::ex2(m_was - m_ref + (e_was - e_ref));

@@ -397,6 +397,36 @@ def test_scores_of_millions(rows, dh, power):
     _check_by_key_sizes(out[:, others], lse[:, others], q[others], k, v, 1.0)
 
 
+@pytest.mark.parametrize("less", [15.0, 24.0, 26.0])
+@pytest.mark.parametrize("rows,dh", [(2, 128), (12, 64), (20, 128), (40, 128), (40, 64), (130, 128)])
+def test_many_small_weights_beside_a_large_one(rows, dh, less):
+    """The first key leads by 2^less, and has no part in half of the dimensions: what is there comes from a thousand small weights."""
+    b = _b()
+    B, heads, n = 8, 32, 1024
+    c = b.KvCache4(B, heads, dh, n)
+    k, v = _rand(141, n, dh, scale=0.05), _rand(142, n, dh) + 1
+    k[:, 0] = 0
+    k[0] = 0
+    k[0, 0] = 2
+    v[0, :dh // 2], v[0, dh // 2:] = 0, 1                               # code 0 of 0: exactly nothing
+    q = _rand(143, rows, dh, scale=0.1)
+    q[:, 0] = float(np.float32(less * np.log(2) / 2))
+    alike = lambda x: x[None, :, None].expand(B, -1, heads, -1).contiguous()
+    c.store(alike(k), alike(v))
+    out, _ = c.attention(alike(q), _i32([n] * B), n, scale=1.0)
+    got = _np(out.transpose(1, 2).reshape(B * heads, rows, dh))[..., :dh // 2]
+    kk, vv, q = plain.values(_np(k)), plain.values(_np(v)), _np(q)
+    code, s, m = plain.quantise(_np(k))
+    x = q @ kk.T
+    p = np.exp(x - x.max(-1, keepdims=True))
+    p /= p.sum(-1, keepdims=True)
+    want, r = (p @ vv)[:, :dh // 2], np.abs(vv).max(-1)
+    d = (np.abs(q) @ (code * s + np.abs(m)).T).max(-1) * (dh / 16 + 8) * 2.0 ** -23
+    # as in _check_by_key_sizes, over the keys that count here; 2^-25 of fp16 is 2^-34 of the largest
+    tol = 2.0 ** -8 * np.abs(want) + ((2.0 ** -10 + 2 * d + 2.0 ** -19) * (p[:, 1:] @ r[1:]) + n * 2.0 ** -32 * (p * r).max(-1))[:, None]
+    assert (np.abs(got - want) <= tol).all(), float((np.abs(got - want) / tol).max())
+
+
 @pytest.mark.parametrize("dh", [64, 128])
 @pytest.mark.parametrize("scale", [0.0, -0.1, 3.0])
 @pytest.mark.parametrize("rows", [2, 12, 20, 40, 130])
