@@ -202,7 +202,7 @@ __global__ void __launch_bounds__(WARPS * 32, AttnShape<DH, NT>::CTAS) attention
         const bool real = lane < left;
         const uint32_t km = real ? *reinterpret_cast<const uint32_t *>(tile + kv4_off_kmeta(DH) + 4 * lane) : 0u;
         const uint32_t vm = real ? *reinterpret_cast<const uint32_t *>(tile + kv4_off_vmeta(DH) + 4 * lane) : 0u;
-        const int ex = min(max((int)((vm >> 7) & 255u), (int)((vm >> 23) & 255u) - 4) - 126, 100);
+        const int ex = min(max((int)((vm >> 7) & 255u), (int)((vm >> 23) & 255u) - 4) - 126, 125);   // NaN: 125
         const int ex_top = __reduce_max_sync(0xffffffffu, ex);
         if (ex_top > e0) {                         // rare
           const float d = e0 == -1000 ? 0.f : (float)(max(ex_top, -100) + 2 - e0);

@@ -268,6 +268,19 @@ def test_attention_whatever_the_magnitudes(vscale, qscale, rows):
     _check_attention(q, k, v, out, lse, 128 ** -0.5)
 
 
+@pytest.mark.parametrize("vscale", [1e32, 1e34, 1e36, 3e37])
+@pytest.mark.parametrize("rows,dh", [(1, 128), (12, 64), (30, 128), (40, 64), (70, 128)])
+def test_values_near_the_end_of_the_range(rows, dh, vscale):
+    b = _b()
+    c = b.KvCache4(1, 1, dh, 600)
+    k, v, q = _rand(151, 600, 1, dh), _rand(152, 600, 1, dh, scale=vscale), _rand(153, rows, 1, dh)
+    v[:40] *= 2.0 ** -100
+    c.store(k, v)
+    out, lse = c.attention(q, _i32([600]), 600)
+    assert out.isfinite().all()
+    _check_attention(q, k, v, out, lse, dh ** -0.5)
+
+
 @pytest.mark.parametrize("rows", [2, 20, 40])
 def test_rising_scores_move_the_reference(rows):
     b = _b()
