@@ -501,8 +501,10 @@ __global__ void __launch_bounds__(128) kv4_join_kernel(const AttnParams p, int n
 // against 21 / 47 / 128; heads of 64: 10 / 31 / 56 against 15 / 36 / 103, 12 / 29 / 83 against 17 / 37 / 103.)
 struct AttnPlan { int chunk, ctas, tc; };
 
-AttnPlan plan_attention(int heads, int B, int rows, int Hq, int max_len, int sms) {
+AttnPlan plan_attention(const Kv4View &c, int B, int rows, int Hq, int max_len, int sms) {
   AttnPlan pl;
+  const int heads = c.heads;
+  if (max_len > c.cap) max_len = c.cap;            // a max_len of 2^31 - 1 says no more
   const int cols = rows * (Hq / heads);
   pl.tc = cols > 32;
   pl.chunk = cols <= 8 ? 8 : cols <= 16 ? 16 : cols <= 32 ? 32 : cols <= 64 ? 64 : 128;
@@ -522,7 +524,7 @@ bool attention_kv4_fits(const Kv4View &c, int B, int rows, int Hq, int max_len) 
 }
 
 int64_t attention_kv4_scratch_floats(const Kv4View &c, int B, int rows, int Hq, int max_len, int sms) {
-  const AttnPlan pl = plan_attention(c.heads, B, rows, Hq, max_len, sms);
+  const AttnPlan pl = plan_attention(c, B, rows, Hq, max_len, sms);
   return (int64_t)2 * pl.ctas * part_floats(pl.chunk, c.dh);
 }
 
@@ -543,7 +545,7 @@ static cudaError_t launch_join(cudaStream_t st, const AttnParams &p, int ctas, i
 }
 
 cudaError_t launch_attention_kv4(cudaStream_t st, const Kv4AttnArgs &a, int sms) {
-  const AttnPlan pl = plan_attention(a.c.heads, a.b.B, a.b.rows, a.Hq, a.max_len, sms);
+  const AttnPlan pl = plan_attention(a.c, a.b.B, a.b.rows, a.Hq, a.max_len, sms);
   AttnParams p;
   p.c = a.c; p.Hq = a.Hq; p.q = a.q; p.out = a.out; p.lse = a.lse; p.q_stride = a.q_stride; p.out_stride = a.out_stride;
   p.scale_log2 = a.scale * 1.4426950408889634f; p.part = a.scratch; p.status = a.status;

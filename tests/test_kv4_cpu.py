@@ -99,6 +99,14 @@ def test_attention_refusals(kw, status):
         assert b.lib.l2pd_attention_kv4_scratch_bytes(C.byref(c), 2, 3, 8, 100) > 64
 
 
+@pytest.mark.parametrize("rows", [1, 3, 40])
+def test_a_length_beyond_the_capacity_plans_for_the_capacity(rows):
+    # partial results for as many CTAs as the capacity's tiles keep busy: 2^31 - 1 passed 32 bits in the count of tiles, and one CTA was left
+    b, c = _cache(slots=8, heads=8, cap=5000)
+    n = lambda max_len: b.lib.l2pd_attention_kv4_scratch_bytes(C.byref(c), 8, rows, 8, max_len)
+    assert n(2 ** 31 - 1) == n(2 ** 31 - 100) == n(5001) == n(5000) > n(40)
+
+
 @pytest.mark.parametrize("kw,status", [(dict(q=None), ARG), (dict(lse=None), ARG), (dict(w=None), ARG), (dict(o=None), ARG), (dict(hq=7), SHAPE),
                                        (dict(qs=8), SHAPE), (dict(B=0), 0), (dict(max_len=0), 0)])
 def test_weights_refusals(kw, status):
