@@ -1596,7 +1596,7 @@ static l2pd_status kv4_query_checks(const char *call, const Kv4View &c, const vo
 
 int64_t l2pd_attention_kv4_scratch_bytes(const l2pd_kv4 *cache, int32_t B, int32_t rows, int32_t Hq, int32_t max_len) {
   if (!cache || !kv4_sizes_ok(cache->slots, cache->heads, cache->head_dim, cache->capacity) || B < 0 || rows < 0 || Hq < 1 ||
-      Hq % cache->heads || max_len < 0)
+      Hq % cache->heads || max_len < 0 || (int64_t)rows * (Hq / cache->heads) > 0x7fffffff)
     return 0;
   Kv4View c{};
   c.heads = cache->heads; c.dh = cache->head_dim; c.cap = cache->capacity;

@@ -107,6 +107,12 @@ def test_a_length_beyond_the_capacity_plans_for_the_capacity(rows):
     assert n(2 ** 31 - 1) == n(2 ** 31 - 100) == n(5001) == n(5000) > n(40)
 
 
+def test_scratch_of_batches_that_are_refused():
+    b, c = _cache(slots=8, heads=2, cap=5000)
+    n = lambda rows, hq: b.lib.l2pd_attention_kv4_scratch_bytes(C.byref(c), 8, rows, hq, 5000)
+    assert n(2 ** 30, 2) > 0 and n(2 ** 30, 4) == n(2 ** 31 - 1, 6) == n(2 ** 31 - 1, 16) == n(3, 3) == 0
+
+
 @pytest.mark.parametrize("kw,status", [(dict(q=None), ARG), (dict(lse=None), ARG), (dict(w=None), ARG), (dict(o=None), ARG), (dict(hq=7), SHAPE),
                                        (dict(qs=8), SHAPE), (dict(B=0), 0), (dict(max_len=0), 0)])
 def test_weights_refusals(kw, status):
