@@ -1510,7 +1510,7 @@ static l2pd_status refuse(l2pd_status st, const char *call, const char *why) {
 static bool aligned16(const void *p) { return ((uintptr_t)p & 15u) == 0; }
 
 static bool kv4_sizes_ok(int32_t slots, int32_t heads, int32_t head_dim, int32_t capacity) {
-  return slots >= 1 && heads >= 1 && heads <= 65535 && (head_dim == 64 || head_dim == 128) && capacity >= 1 && capacity <= 0x7fffffc0;
+  return slots >= 1 && heads >= 1 && heads <= 65535 && (head_dim == 64 || head_dim == 128) && capacity >= 1 && capacity <= 0x7fffff80;   // keys rounded up to 128 fit 31 bits
 }
 
 int64_t l2pd_kv4_bytes(int32_t slots, int32_t heads, int32_t head_dim, int32_t capacity) {

@@ -55,6 +55,13 @@ def test_bytes_of_a_cache():
         assert n(*bad) == 0
 
 
+def test_largest_capacity():
+    # rounded up to the tiles of 128 keys that attention takes, a sequence has to fit 31 bits
+    b, _ = _cache()
+    assert b.lib.l2pd_kv4_bytes(1, 1, 64, 2 ** 31 - 128) == (2 ** 31 - 128) * 72 and b.lib.l2pd_kv4_bytes(1, 1, 64, 2 ** 31 - 127) == 0
+    assert _store(b, b.Kv4(P, 1, 1, 64, 2 ** 31 - 64)) == SHAPE
+
+
 def _store(b, c, **kw):
     a = dict(k=P, v=P, B=1, rows=1, ks=512, vs=512)
     a.update(kw)
