@@ -1585,7 +1585,8 @@ l2pd_status l2pd_kv4_load(void *stream, const l2pd_kv4 *cache, int32_t dtype, vo
 
 // What attention and the weights have in common
 static l2pd_status kv4_query_checks(const char *call, const Kv4View &c, const void *q, const int32_t *d_lens, int32_t rows, int32_t max_len,
-                                    int32_t Hq, int64_t q_stride) {
+                                    int32_t Hq, int64_t q_stride, float scale) {
+  if (!(fabsf(scale * 1.4426950408889634f) < INFINITY)) return refuse(L2PD_ERR_ARG, call, "a finite scale");
   if ((rows && !q) || !d_lens) return refuse(L2PD_ERR_ARG, call, "null pointer");
   if (Hq < 1 || Hq % c.heads || max_len < 0 || (int64_t)rows * (Hq / c.heads) > 0x7fffffff)
     return refuse(L2PD_ERR_SHAPE, call, "query heads a multiple of the cache's heads, max_len >= 0");
@@ -1612,7 +1613,7 @@ l2pd_status l2pd_attention_kv4(void *stream, const l2pd_kv4 *cache, const void *
   if (r == L2PD_OK) r = kv4_batch(call, B, rows, d_row_start, d_slots, d_lens, &a.b);
   if (r != L2PD_OK) return r;
   if (B == 0 || rows == 0) return L2PD_OK;
-  r = kv4_query_checks(call, a.c, q, d_lens, rows, max_len, Hq, q_stride);
+  r = kv4_query_checks(call, a.c, q, d_lens, rows, max_len, Hq, q_stride, scale);
   if (r != L2PD_OK) return r;
   if (!out || !scratch) return refuse(L2PD_ERR_ARG, call, "null pointer");
   if (out_stride < (int64_t)Hq * a.c.dh || out_stride % 8 || !aligned16(out) || !aligned16(scratch))
@@ -1638,7 +1639,7 @@ l2pd_status l2pd_kv4_weights(void *stream, const l2pd_kv4 *cache, const void *q,
   if (r == L2PD_OK) r = kv4_batch(call, B, rows, d_row_start, d_slots, d_lens, &a.b);
   if (r != L2PD_OK) return r;
   if (B == 0 || max_len == 0) return L2PD_OK;
-  r = kv4_query_checks(call, a.c, q, d_lens, rows, max_len, Hq, q_stride);
+  r = kv4_query_checks(call, a.c, q, d_lens, rows, max_len, Hq, q_stride, scale);
   if (r != L2PD_OK) return r;
   if ((rows && !d_lse) || !d_in || !d_out) return refuse(L2PD_ERR_ARG, call, "null pointer");
   const int64_t n = (int64_t)a.c.slots * a.c.heads * a.c.cap;

@@ -114,6 +114,16 @@ def test_a_length_beyond_the_capacity_plans_for_the_capacity(rows):
     assert n(2 ** 31 - 1) == n(2 ** 31 - 100) == n(5001) == n(5000) > n(40)
 
 
+@pytest.mark.parametrize("scale", [float("nan"), float("inf"), -float("inf"), 3e38])
+def test_scales_that_are_not_finite(scale):
+    # one kernel gave NaN for them, the other took them for 0
+    b, c = _cache()
+    assert b.lib.l2pd_attention_kv4(None, C.byref(c), P, P, None, 2, 3, None, None, P, 100, 8, 1024, 1024, scale, P, 1 << 30, 0) == ARG
+    assert b.lib.l2pd_last_error(None) == b"l2pd_attention_kv4: a finite scale"
+    assert b.lib.l2pd_kv4_weights(None, C.byref(c), P, P, P, P, 1, 1, None, None, P, 5, 8, 1024, scale) == ARG
+    assert b.lib.l2pd_last_error(None) == b"l2pd_kv4_weights: a finite scale"
+
+
 def test_scratch_of_batches_that_are_refused():
     b, c = _cache(slots=8, heads=2, cap=5000)
     n = lambda rows, hq: b.lib.l2pd_attention_kv4_scratch_bytes(C.byref(c), 8, rows, hq, 5000)
