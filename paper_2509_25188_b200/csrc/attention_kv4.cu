@@ -95,10 +95,11 @@ __device__ __forceinline__ float query_factor(float scale_log2, int u) { return 
 
 template <int DH, int NT> struct AttnShape {
   static constexpr int CH = 8 * NT, TILE = KV4_TILE * (DH + 8), STAGES = NT == 4 ? 4 : 3, RING = STAGES * TILE;
-  static constexpr int CTAS = NT == 1 ? 4 : NT == 2 ? 3 : 2;   // an SM's, as registers allow
+  static constexpr int CTAS = NT == 1 && DH == 64 ? 4 : NT <= 2 ? 3 : 2;   // an SM's, as registers and shared memory allow
   static constexpr bool Q_REGS = NT < 4;           // queries in registers; with 32 columns they are read from shared memory where they are used
   static constexpr int META = KV4_TILE * 24, QBYTES = NT * DH * 16;
   static constexpr int OFF_META = WARPS * RING, OFF_Q = OFF_META + WARPS * META, SMEM = OFF_Q + QBYTES;
+  static_assert(CTAS * (SMEM + 1536 + 1024) <= 228 * 1024, "with what the kernel declares itself (1536 at most) and what a CTA costs besides");
 };
 
 template <int DH, int NT>
@@ -511,7 +512,7 @@ AttnPlan plan_attention(const Kv4View &c, int B, int rows, int Hq, int max_len, 
   // no more CTAs than there are tiles for each, or for each warp of them
   const int64_t items = (int64_t)B * heads * ceil_div(cols, pl.chunk);
   const int64_t want = pl.tc ? items * ceil_div(max_len, TC_TILE) : ceil_div64(items * ceil_div(max_len, KV4_TILE), WARPS);
-  const int most = pl.tc ? sms : sms * (pl.chunk == 8 ? 4 : pl.chunk == 16 ? 3 : 2);
+  const int most = pl.tc ? sms : sms * (pl.chunk == 32 ? 2 : pl.chunk == 8 && c.dh == 64 ? AttnShape<64, 1>::CTAS : AttnShape<128, 1>::CTAS);
   pl.ctas = (int)(want < 1 ? 1 : want < most ? want : most);
   return pl;
 }

@@ -124,6 +124,16 @@ def test_scales_that_are_not_finite(scale):
     assert b.lib.l2pd_last_error(None) == b"l2pd_kv4_weights: a finite scale"
 
 
+def test_ctas_of_single_tokens_fit_an_sm():
+    # two partial results of eight columns for each CTA: four CTAs an SM for heads of 64, three for heads of 128, whose shared memory
+    # holds no more
+    n = {}
+    for dh in (64, 128):
+        b, c = _cache(slots=64, heads=8, dh=dh, cap=8000)
+        n[dh] = b.lib.l2pd_attention_kv4_scratch_bytes(C.byref(c), 64, 1, 32, 8000) // (2 * 8 * (dh + 4) * 4)
+    assert n[64] % 4 == 0 and n[128] == n[64] // 4 * 3
+
+
 def test_scratch_of_batches_that_are_refused():
     b, c = _cache(slots=8, heads=2, cap=5000)
     n = lambda rows, hq: b.lib.l2pd_attention_kv4_scratch_bytes(C.byref(c), 8, rows, hq, 5000)
