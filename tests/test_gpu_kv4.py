@@ -716,6 +716,38 @@ def test_weights(heads, group, dh, rows, keys):
         assert torch.equal(inplace[i, :, :keys[i]], out[i, :, :keys[i]])
 
 
+@pytest.mark.parametrize("B", [33, 64, 65, 300])
+@pytest.mark.parametrize("rows,group,dh", [(1, 4, 128), (3, 4, 64), (8, 3, 128), (20, 2, 64), (40, 3, 128)])
+@pytest.mark.parametrize("kind", ["equal", "ragged"])
+def test_more_sequences_than_a_warp_has_lanes(kind, rows, group, dh, B):
+    """Every warp surveys the batch 32 sequences at a time; sequences and their pieces must be found behind the first 32 too."""
+    b = _b()
+    heads, cap = 2, 330
+    c = b.KvCache4(B, heads, dh, cap)
+    k, v = _rand(161, B, cap, heads, dh), _rand(162, B, cap, heads, dh)
+    c.store(k, v)
+    counts = [rows] * B if kind == "equal" else [(rows * (5 * i % 7)) // 6 for i in range(B)]
+    keys = [257] * B if kind == "equal" else [0 if i % 9 == 4 else 1 + (i * 97) % cap for i in range(B)]
+    slots = [(7 * i + 3) % B for i in range(B)] if B % 7 else list(range(B))[::-1]
+    starts = np.concatenate(([0], np.cumsum(counts))).tolist()
+    q = _rand(163, starts[-1], heads * group, dh)
+    lens, rs, sl = _i32(keys), _i32(starts), _i32(slots)
+    out, lse = c.attention(q, lens, cap, row_start=rs, max_rows=rows, slots=sl, check=True)
+    base = torch.rand(B, heads, cap, device=DEV)
+    w = c.attention_weights(q, lse, lens, cap, base, out=torch.full_like(base, -1.0), row_start=rs, max_rows=rows, slots=sl)
+    for i in list(range(0, B, 13)) + [31, 32, 33 % B, 63 % B, B - 2, B - 1]:
+        lo, hi, n, s = starts[i], starts[i + 1], keys[i], slots[i]
+        assert (w[s, :, n:] == -1).all()
+        _, _, ww = plain.attention(_np(q[lo:hi]), plain.values(_np(k[s, :n])), plain.values(_np(v[s, :n])), dh ** -0.5)
+        got, was = _np(w[s, :, :n]), _np(base[s, :, :n])
+        if hi > lo:
+            _check_attention(q[lo:hi], k[s, :n], v[s, :n], out[lo:hi], lse[lo:hi], dh ** -0.5)
+        code, step, m = plain.quantise(_np(k[s, :n]))                   # as in test_weights
+        a = max((np.abs(_np(q[lo:hi])[:, h]) @ (code * step + np.abs(m))[:, h // group].T).max() for h in range(heads * group)) if hi > lo and n else 0.0
+        d = a * dh ** -0.5 * (dh / 16 + 8) * 2.0 ** -23
+        assert (np.abs(got - was - ww) <= (2 * d + 2.0 ** -19 + rows * group * 2.0 ** -24) * ww + 2.0 ** -23 * (was + ww)).all()
+
+
 # ---- eviction ----------------------------------------------------------------------------------------------------------------
 
 def _weights(kind, B, heads, cap):
