@@ -59,7 +59,8 @@ __device__ __forceinline__ uint32_t max_s2(uint32_t a, uint32_t b) {
   asm("max.s16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
   return d;
 }
-// x / 15, correctly rounded: the reciprocal's product and one correction (every fp32 mantissa was checked); for tiny x a division.
+// x / 15, correctly rounded: the reciprocal's product and one correction by the rest (P. W. Markstein, IBM J. Res. Dev. 34, 1990; the tests go
+// through every mantissa); for tiny x, whose rest would lose bits, a division.
 __device__ __forceinline__ float fifteenth(float x) {
   constexpr float R = 1.f / 15.f;
   const float q = x * R;

@@ -31,6 +31,17 @@ def test_plain_bf16_rounding():
     assert plain.bf16_round(np.float32(3.0e-40)) != 0
 
 
+def test_a_fifteenth_by_one_correction_is_the_rounded_quotient():
+    # the store's q + (x - 15 q) / 15, with 1 / 15 rounded, for every mantissa; 64 bits hold each step before its rounding: the rest
+    # is a few units of q's last place, its product with 24 bits ends 27 places below
+    x = np.arange(2 ** 23, 2 ** 24, dtype=np.float64)
+    r = np.float64(np.float32(1) / np.float32(15))
+    q = (x * r).astype(np.float32).astype(np.float64)
+    rest = (x - 15 * q).astype(np.float32).astype(np.float64)
+    got = (q + rest * r).astype(np.float32)
+    assert np.array_equal(got, x.astype(np.float32) / np.float32(15))
+
+
 def test_plain_keep():
     w = [1.0, 5.0, 5.0, float("nan"), 2.0, 0.0]
     assert plain.keep(w, range(6), 6, 3, 0, 99) == [4, 1, 2]
