@@ -425,9 +425,17 @@ l2pd_status l2pd_attention_bf16(void *stream, const void *q, const void *k, cons
  * within a row is contiguous; rows start on 16 bytes (strides multiples of 8), else L2PD_ERR_SHAPE.  Every call follows stream order,
  * allocates nothing, runs on the current device and may be captured into a graph (attention and weights: after a call of
  * either outside a capture on that device).
- * B = 0 or rows = 0 is L2PD_OK and does nothing.  2^31 tiles (of 32 keys, for each head and 8 of its query rows) in a call, or 2^37
- * rows times heads, are L2PD_ERR_SHAPE.  All arithmetic is fp32 or wider and the order of every sum is fixed: a call
- * repeated on the same device gives the same bits.
+ * B = 0 or rows = 0 is L2PD_OK and does nothing (weights: their sums are copied).  2^31 tiles (of 32 keys, for each head and 8 of its
+ * query rows) in a call, or 2^37 rows times heads, are L2PD_ERR_SHAPE.  slots and capacity: at least 1, capacity at most 2^31 - 128.
+ *
+ * Numbers.  Sums, references and logarithms are fp32, and the order of every sum is fixed: a call repeated on the same device gives the
+ * same bits.  Products take fp16 operands, each row with a power of two of its own, so that no row, key or value decides the bits of another:
+ *   queries     as they are, down to 2^-32 of the row's largest (attention and weights)
+ *   keys        codes as they are; with more than 32 columns (rows times query heads of a key head) (c - 8) s, exactly, and m + 8 s in
+ *               22 bits: scores as in fp32
+ *   output      probabilities times the s of their value row, or with more than 32 columns probabilities and values, are rounded to fp16:
+ *               |error| of about 2^-9 |out| (the store) + 2^-11 sum_j p_j R_j, R_j the largest |value| of key j's row.  Parts 2^34 below the
+ *               largest p_j R_j vanish; values more than 2^100 below the largest before them in their sequence do not count
  */
 typedef struct {
   void *data;
@@ -446,7 +454,7 @@ l2pd_status l2pd_kv4_load(void *stream, const l2pd_kv4 *cache, int32_t dtype, vo
 /* out[r, h] = softmax over the keys j < d_lens[i] of (scale q[r, h] . k_j) times v_j, without a causal mask: the rows of a block
  * see the whole cache, their own keys among it where they were stored before.  q, out: DEVICE bf16 [row, Hq, head_dim]; query head
  * h reads key head h / (Hq / heads).  d_lens: DEVICE int32 [B], clipped to [0, min(max_len, capacity)]; max_len (host) sizes the launch.
- * d_lse: DEVICE float [row, Hq] or NULL, the natural logarithm of the sum of exponentials.  No keys: out 0, d_lse -inf.
+ * scale: finite.  d_lse: DEVICE float [row, Hq] or NULL, the natural logarithm of the sum of exponentials.  No keys: out 0, d_lse -inf.
  * scratch: DEVICE, 16-byte aligned, of at least l2pd_attention_kv4_scratch_bytes(...) bytes (asked on the same device), for this
  * call alone until it has run: calls that may overlap, and captured graphs that may, need their own.  check as elsewhere. */
 int64_t l2pd_attention_kv4_scratch_bytes(const l2pd_kv4 *cache, int32_t B, int32_t rows, int32_t Hq, int32_t max_len);
@@ -455,7 +463,7 @@ l2pd_status l2pd_attention_kv4(void *stream, const l2pd_kv4 *cache, const void *
                                int64_t q_stride, int64_t out_stride, float scale, void *scratch, int64_t scratch_bytes, int32_t check);
 /* d_out[slot, h, j] = d_in[slot, h, j] + the attention weight exp(scale q . k_j - lse) that key j of key head h receives, summed over
  * the sequence's rows and the query heads of h; keys j < d_lens[i] alone.  d_in, d_out: DEVICE float [slots, heads, capacity], the same
- * array or two apart.  d_lse: what l2pd_attention_kv4 gave for the same rows.  No slot twice in a call where d_in == d_out. */
+ * array or two apart.  d_lse: what l2pd_attention_kv4 gave for the same rows.  No slot twice in a call: each key's sum is written once. */
 l2pd_status l2pd_kv4_weights(void *stream, const l2pd_kv4 *cache, const void *q, const float *d_lse, const float *d_in, float *d_out, int32_t B,
                              int32_t rows, const int32_t *d_row_start, const int32_t *d_slots, const int32_t *d_lens, int32_t max_len,
                              int32_t Hq, int64_t q_stride, float scale);

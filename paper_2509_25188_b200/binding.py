@@ -639,7 +639,7 @@ class KvCache4:
     def attention_weights(self, q: torch.Tensor, lse: torch.Tensor, lens: torch.Tensor, max_len: int, weights: torch.Tensor,
                           out: Optional[torch.Tensor] = None, row_start=None, max_rows=None, slots=None, scale: Optional[float] = None):
         """out = weights + what every key receives from these rows, weights [slots, heads, capacity] in fp32 (out None: in place).
-        lse is attention()'s.  Returns out; keys at and behind a sequence's length are not written."""
+        lse is attention()'s.  Returns out; keys at and behind a sequence's length are not written.  No slot twice in a call."""
         index = self._index
         if _device_now() != index:                  # runs again with the cache's device as the current one
             with torch.cuda.device(index):
