@@ -857,6 +857,49 @@ def test_evict_that_keeps_everything(keep):
     assert new.tolist() == [0] and (kept == -1).all()
 
 
+def test_a_captured_step_of_all_calls():
+    """Norm + rotation, store, attention, weights, eviction and load in one graph, replayed on new inputs, against the calls one by one."""
+    b = _b()
+    B, heads, group, dh, rows, cap, keep = 3, 2, 2, 128, 20, 5000, 1500
+    prompt = _rand(171, B, cap - rows, heads, dh), _rand(172, B, cap - rows, heads, dh)
+    pos = torch.arange(rows, dtype=torch.int32, device=DEV).repeat(B) + cap
+    q, k, v = (_rand(173 + i, B, rows, h, dh) for i, h in enumerate((heads * group, heads, heads)))
+    gain = torch.ones(dh, device=DEV)
+    start, lens = _i32([cap - rows, 4000, 70]), _i32([cap, 4020, 90])
+
+    def fresh():
+        c, d = b.KvCache4(B, heads, dh, cap), b.KvCache4(B, heads, dh, keep)
+        c.store(*prompt)
+        return c, d, torch.zeros(B, heads, cap, device=DEV), torch.zeros(B, heads, keep, device=DEV)
+
+    def step(c, d, w, wi):
+        qr, kr = b.qk_norm_rope(q.view(B * rows, -1, dh), k.view(B * rows, heads, dh), gain, gain, pos)
+        c.store(kr.view(k.shape), v, key_start=start)
+        out, lse = c.attention(qr.view(q.shape), lens, cap)
+        c.attention_weights(qr.view(q.shape), lse, lens, cap, w)
+        kept, left = c.evict(w, lens, cap, keep, first=4, into=d, weights_into=wi)
+        return (out, lse, kept, left, *d.load(keep, dtype=torch.float32))
+
+    state = fresh()
+    step(*state)                                                        # once outside
+    for x in (state[0].data, state[1].data, state[2], state[3]):
+        x.zero_()
+    state[0].store(*prompt)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = step(*state)
+    other = fresh()
+    for turn in range(3):
+        for i, x in enumerate((q, k, v)):
+            x.copy_(_rand(181 + 3 * turn + i, *x.shape))
+        lens.copy_(_i32([cap - turn, 4020, 90 + turn]))
+        graph.replay()
+        want = step(*other)
+        torch.cuda.synchronize()
+        for x, y in zip(got + (state[2], state[3], state[0].data, state[1].data), want + (other[2], other[3], other[0].data, other[1].data)):
+            assert torch.equal(x, y), turn
+
+
 # ---- norms and rotation ------------------------------------------------------------------------------------------------------
 
 @pytest.mark.parametrize("norm", [True, False])
