@@ -487,7 +487,7 @@ l2pd_status l2pd_kv4_evict(void *stream, const l2pd_kv4 *cache, const l2pd_kv4 *
  * attention: y = x g / sqrt(mean(x^2) + eps) over the head_dim numbers of a (row, head), then the pair (y_i, y_{i + head_dim/2})
  * is turned by the angle position * theta^(-2i/head_dim), as the transformer above pairs them; the angle is reduced in 64 bits, whatever
  * the position.  q [rows, Hq, head_dim], k [rows, Hk, head_dim]: DEVICE, L2PD_F32 or L2PD_BF16, row strides in elements; the outputs may
- * be the inputs (same strides).  q_gain, k_gain: DEVICE float [head_dim]; NULL: no norm, the rotation alone.  d_positions: DEVICE int32
+ * be the inputs (same strides).  Squares and their mean are fp32.  q_gain, k_gain: DEVICE float [head_dim]; NULL: no norm, the rotation alone.  d_positions: DEVICE int32
  * [rows]; NULL: the row's number.  head_dim even, at most 256; Hq or Hk may be 0.  One rounding, at the store.
  */
 l2pd_status l2pd_qk_norm_rope(void *stream, int32_t dtype, const void *q, const void *k, void *q_out, void *k_out, const float *q_gain,

@@ -8,7 +8,8 @@
 //     t_j = log2 of exp(scale q . k_j) + e_j - E = cf (s_j sum(c q') + m_j sum(q')) + e_j - E
 // 2^e_j bounds the value row's s_j and |m_j| / 16, E is above all e_j so far.  Probabilities are taken as p'_j = 2^(t_j - M), M a reference
 // 2^9 to 2^15 below the running maximum of t, so that p'_j s_j 2^-e_j, what multiplies the codes of V, stays within fp16 whatever the
-// values' magnitude (attention_kv4.cuh has what becomes of M and the sums where E rises).  Rounding it to fp16 is the only step to less than 32 bits between the queries and the output.
+// values' magnitude (attention_kv4.cuh has what becomes of M and the sums where E rises).  Rounding that to fp16 is the only step to less than 32
+// bits between the queries and the output.
 //
 // Work: the key tiles of all (sequence, head, chunk of columns) stand in one line and every CTA takes an equal run of it; a run
 // that starts or ends inside an item leaves a partial result, joined in the order of the tiles by a second kernel.  A warp takes
@@ -16,8 +17,8 @@
 // queries or brings its warps' sums together.
 //
 // What bounds it.  One row of 32/8 heads on 4000 keys: the latency of a few dependent steps and of two launches, 11 us.  Up to 8
-// columns on many keys: memory (64 rows of 32/8 heads on 8192 keys each: 116 us, 4.9 TB/s).  32 columns (8 x 32 rows of 32 heads of
-// 128 on 2048 keys, 42 us): products 512 cycles of a scheduler and 453 instructions for 16 keys, which take 1250; registers leave two
+// columns on many keys: memory (64 rows of 32/8 heads on 8192 keys each: 103 us, 5.5 TB/s).  32 columns (8 x 32 rows of 32 heads of
+// 128 on 2048 keys, 43 us; 255 registers, 36 bytes spilled): products 512 cycles of a scheduler and 453 instructions for 16 keys, which take 1250; registers leave two
 // warps a scheduler, and each goes through products, exponentials and products in turn.
 #include <cuda_fp16.h>
 #include <math.h>
@@ -497,9 +498,9 @@ __global__ void __launch_bounds__(128) kv4_join_kernel(const AttnParams p, int n
   if (lane == 0 && lse) *lse = (m + log2f(l)) * 0.6931471805599453f;
 }
 
-// Up to 32 columns: the warp-level kernel, whose operands never leave registers.  More: tcgen05 with 64 or 128 lanes.  (8 sequences
-// of 32 heads, us at 128 / 2048 / 8192 keys: 16 columns 13 / 42 / 83 against 20 / 45 / 124 on tcgen05, 32 columns 16 / 44 / 130
-// against 21 / 47 / 128; heads of 64: 10 / 31 / 56 against 15 / 36 / 103, 12 / 29 / 83 against 17 / 37 / 103.)
+// Up to 32 columns: the warp-level kernel, whose codes and probabilities never leave registers (queries of 32 columns do).  More: tcgen05
+// with 64 or 128 lanes.  (8 sequences of 32 heads, us at 128 / 2048 / 8192 keys: 16 columns 10 / 32 / 80 against 20 / 52 / 145 on tcgen05,
+// 32 columns 15 / 43 / 125 against 21 / 53 / 148; heads of 64: 7 / 32 / 57 against 17 / 42 / 116, 12 / 29 / 83 against 18 / 43 / 117.)
 struct AttnPlan { int chunk, ctas, tc; };
 
 AttnPlan plan_attention(const Kv4View &c, int B, int rows, int Hq, int max_len, int sms) {
@@ -568,8 +569,8 @@ cudaError_t launch_attention_kv4(cudaStream_t st, const Kv4AttnArgs &a, int sms)
 // of a cache tile, codes and (s, m) of K.  A warp keeps 32 keys as A fragments in registers and passes the columns by them, whose B
 // fragments lie in shared memory for all warps of the CTA; more than 64 columns in several passes over the CTA's run.
 //
-// Few columns: bound by memory (16 x 1 token of 32/8 heads on 30000 keys: 50 us, 4.6 TB/s with the sums).  Many: by the products, 16
-// MMAs of 8 cycles for 32 keys and 8 columns (8 x 32 rows of 32 heads on 2048 keys: 22 us, the products alone 7.8), and by the
+// Few columns: bound by memory (16 x 1 token of 32/8 heads on 30000 keys: 64 us, 4.6 TB/s with the sums).  Many: by the products, 16
+// MMAs of 8 cycles for 32 keys and 8 columns (8 x 32 rows of 32 heads on 2048 keys: 21 us, the products alone 7.8), and by the
 // launch, the queries' conversion in every CTA and the exponentials beside them.
 namespace {
 

@@ -57,8 +57,9 @@ struct Line {
   }
   // Tiles of the line and of a CTA's run; *before: tiles of the sequences ahead of `upto`.  `own` is seq(lane).  (Whole warp.)
   // Equal runs split items, and every piece of one costs a CTA its queries, its output and, split, a way through memory: about what
-  // an SM takes for `piece` tiles.  Sequences of one length: whole items where the SM with most of them is done sooner (8 x 16 rows of
-  // 32 heads on 512 keys: 22 us split, 16 whole; on 8192 keys 83 split; 8 x 32 rows on 2048 keys 43.7 split, 42.0 whole).  An SM with fewer CTAs than fit takes longer for a tile.
+  // an SM takes for `piece` tiles (measured, as is 1.15).  Sequences of one length: whole items where the SM with most of them is done sooner
+  // (8 x 16 rows of 32 heads on 512 keys: 19 us split, 16 whole; on 8192 keys 79 split; 8 x 32 rows on 2048 keys 43.8 split, 43.2 whole).
+  // An SM with fewer CTAs than fit takes longer for a tile.
   __device__ uint32_t survey(const Seq &own, uint32_t ctas, int upto, uint32_t *share, uint32_t *before) const {
     const int lane = threadIdx.x & 31;
     uint32_t total = 0, ahead = 0, lo = 0xffffffffu, hi = 0;

@@ -24,11 +24,12 @@
 //
 // What bounds it.  A tile of 128 keys of 128 numbers needs, in cycles: shared memory 1300 (17 KB of codes in and out, 64 KB of
 // operands out and in, at 128 bytes), products 1090, exponentials of 128 columns 1024, issue slots 1400 of each scheduler.  It
-// takes 2270 with 64 columns and 2850 with 128, no unit more than half busy: with five warps a scheduler, dependent instructions,
+// takes 2370 with 64 columns and 3090 with 128, no unit more than half busy: with five warps a scheduler, dependent instructions,
 // instruction fetches and waits on barriers (100 each, ready or not) add up.  With exponentials, operand stores and products all
-// left out the rest alone took 70 % of the time.  8 x 64 rows of 32/32 heads of 128 on 8192 keys: 148 us; 4 x 32 rows of 32/8 heads
-// on 65000 keys: 171 us of 128 numbers a head, 139 of 64.  No gain: a second issuing warp, P V in two halves, rolled loops,
-// waits that read no clock, packed f32x2 arithmetic, other register splits.
+// left out the rest alone took 70 % of the time.  8 x 64 rows of 32/32 heads of 128 on 8192 keys: 154 us; 4 x 32 rows of 32/8 heads
+// on 65000 keys: 186 us of 128 numbers a head, 155 of 64 (146, 170 and 140 without the look for rows apart from their neighbours and the
+// code that takes them; 48 to 64 bytes of a thread's registers are spilled).  No gain: a second issuing warp, P V in two halves,
+// waits that read no clock, packed f32x2 arithmetic, other register splits, all probabilities ahead of the wait for the product before.
 //
 // Warp roles (640 threads): 0-3 and 4-7 softmax and output, 4-7 the next piece's queries before that, 8-11 K, 12-15 V, 16 copies of
 // codes, 17 MMA issuer (owns tensor memory), 18 and 19 bring the next piece's queries near.  Tensor memory: S at 0 and 128, O at
