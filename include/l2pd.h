@@ -435,7 +435,8 @@ l2pd_status l2pd_attention_bf16(void *stream, const void *q, const void *k, cons
  *               22 bits: scores as in fp32
  *   output      probabilities times the s of their value row, or with more than 32 columns probabilities and values, are rounded to fp16:
  *               |error| of about 2^-9 |out| (the store) + 2^-11 sum_j p_j R_j, R_j the largest |value| of key j's row.  Parts 2^34 below the
- *               largest p_j R_j vanish; values more than 2^100 below the largest before them in their sequence do not count
+ *               largest p_j R_j vanish (with more than 32 columns a row of zeros has the R_j of the 32 keys it stands among); values more
+ *               than 2^100 below the largest before them in their sequence do not count
  */
 typedef struct {
   void *data;

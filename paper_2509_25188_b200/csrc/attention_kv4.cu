@@ -283,7 +283,7 @@ __global__ void __launch_bounds__(WARPS * 32, AttnShape<DH, NT>::CTAS) attention
               float *x = &acc[u][n][2 * e];
               F2 sum = cs[Sh::Q_REGS ? n : 0], factor = cf[Sh::Q_REGS ? n : 0];
               if (!Sh::Q_REGS) column_factors(n, sum, factor);
-              const F2 y = ptx::fma2(ptx::mul2(ptx::f2(x[0], x[1]), factor), ks, ptx::add2(ptx::fma2(km, sum, bias), neg_m[n]));
+              const F2 y = ptx::fma2(ptx::mul2(ptx::f2(x[0], x[1]), factor), ks, ptx::fma2(km, sum, ptx::add2(bias, neg_m[n])));   // exponents first: they cancel
               x[0] = ptx::f2_lo(y); x[1] = ptx::f2_hi(y);
               top = fmaxf(top, fmaxf(x[0], x[1]));
             }
